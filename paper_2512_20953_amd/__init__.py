@@ -5,7 +5,9 @@ import importlib
 
 _LAZY = ("AH_ARCH_GPT", "AH_ARCH_LLAMA", "AH_ARCH_BERT", "PARAM_INDEX", "AhError", "Stage", "StageConfig", "attention_bwd",
          "attention_fwd", "attention_bwd_static", "ATTENTION_STATIC_MAX_ROWS", "gemm_nn", "gemm_nn_swiglu", "gemm_nt", "gemm_plan", "gemm_tn", "gemm_tn_segmented", "lib", "library_path", "query_sizes", "cost_layers_time",
-         "cost_pipeline_time", "cost_iteration_time", "cost_idle_fractions", "cost_partition_layers")
+         "cost_pipeline_time", "cost_iteration_time", "cost_idle_fractions", "cost_partition_layers", "AdamW",
+         "attention_window_fwd", "attention_window_bwd", "attention_window_bwd_workspace", "qk_norm_rope_fwd", "qk_norm_rope_bwd",
+         "qk_norm_rope_bwd_workspace", "rope_table")
 
 
 def __getattr__(name):

@@ -18,7 +18,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-tar
 # And its kernels of more than 256 registers compute on their score tiles between matrix products: results of those
 # products go to the ordinary registers, not to the accumulation registers from which every element would have to be
 # copied (backward at 1 x 16 x 2048 x 128: 99 -> 91 us).
-EXTRA = {"attention.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+EXTRA = {f: ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form=1"] for f in ("attention.hip", "attention_window.hip")}
 
 
 def _compile(src):

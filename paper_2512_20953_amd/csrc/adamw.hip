@@ -1,0 +1,466 @@
+// Optimizer step over many tensors in few launches (declared in include/ah_ops.h): AdamW with moments in fp32 or in 8 bits, and the
+// norm of all gradients.  Bound by HBM: every value is read and written once.
+//
+// A launch takes up to kTensors tensors, whose descriptors travel in the kernel's arguments (no copy to the device, nothing
+// that a captured graph could find changed); a block takes one chunk of one tensor and finds it by counting the tensors that
+// begin at or before its number.
+#include "ah_ops.h"
+#include "capi_util.h"
+#include "common.h"
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <type_traits>
+
+using namespace ah;
+
+namespace {
+
+constexpr int NT = 256, kTensors = 48, VEC = 4, kReps = 2;
+constexpr int kChunk = NT * VEC * kReps;     // elements per block
+constexpr int kBlock = 32;                   // elements that share a scale
+constexpr uint64_t kMaxElements = 1ull << 34, kMaxBlocks = kMaxElements / kChunk;   // of a tensor; of a launch (2^23: its threads are counted in 32 bits)
+
+struct Entry {
+  void* param;
+  const void* grad;
+  void *m, *v;
+  uint8_t *ms, *vs;
+  float* master;
+  uint64_t n;
+  uint32_t number;   // of the first element, for the random bits
+  float wd;
+};
+
+struct Table {
+  uint32_t first[kTensors];   // the block at which a tensor begins; behind the last tensor: UINT32_MAX
+  Entry e[kTensors];
+};
+
+struct Hyper {
+  float c1, c2, eps, lr;      // 1 - beta1, 1 - beta2
+  float alpha, root;          // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+  double log_b1, log_b2;      // natural logarithms (for step_dev)
+  int64_t step;
+  const float *lr_dev, *grad_norm;
+  const int32_t* step_dev;
+  uint32_t seed;
+  int aligned;                // every pointer of the launch allows vector access
+};
+
+__device__ __forceinline__ int find_tensor(const Table& t, uint32_t block) {
+  int k = -1;
+#pragma unroll
+  for (int i = 0; i < kTensors; i++) k += block >= t.first[i];
+  return k;
+}
+
+// ---- VEC consecutive values of a tensor, from element i on; what lies behind its end reads as 0
+template <class T> struct Wide;
+template <> struct Wide<float> { typedef f32x4 type; };
+template <> struct Wide<bf16> { typedef bf16x4 type; };
+typedef uint8_t u8x4 __attribute__((ext_vector_type(4)));
+template <> struct Wide<uint8_t> { typedef u8x4 type; };
+
+template <class T>
+__device__ __forceinline__ typename Wide<T>::type load4v(const T* p, bool whole, int left) {
+  typename Wide<T>::type r = {};
+  if (whole) return *(const typename Wide<T>::type*)p;
+#pragma unroll
+  for (int j = 0; j < VEC; j++)
+    if (j < left) r[j] = p[j];
+  return r;
+}
+template <class T>
+__device__ __forceinline__ void store4v(T* p, typename Wide<T>::type r, bool whole, int left) {
+  if (whole) {
+    *(typename Wide<T>::type*)p = r;
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < VEC; j++)
+    if (j < left) p[j] = r[j];
+}
+
+// ---- 8-bit codes.  Seen as an fp32 number's exponent and upper mantissa bits, a code is its value times a power of two, binades,
+// gradual underflow and all (fp32 underflows gradually too): decoding is a shift and an exponent add, rounding at random an integer add below the
+// bits that stay.  BINS: binades of the code; the scale byte is the biased exponent of the top one.
+template <int BINS>
+__device__ __forceinline__ float decode(uint32_t code, int scale) {
+  return __builtin_amdgcn_ldexpf(__uint_as_float(code << 20), scale - BINS);
+}
+// |x| to a code; rnd: 16 random bits
+template <int BINS>
+__device__ __forceinline__ uint32_t encode(float ax, int scale, uint32_t rnd) {
+  const uint32_t u = __float_as_uint(__builtin_amdgcn_ldexpf(ax, BINS - scale));
+  return min((u + (rnd << 4)) >> 20, BINS == 15 ? 0x7eu : 0xffu);
+}
+// scale byte of a block whose largest magnitude has these bits; a block that is not finite gets 255
+template <int BINS>
+__device__ __forceinline__ int scale_of(uint32_t top) {
+  const uint32_t e = (top + (BINS == 15 ? 0x200000 - 1 : 0x100000 - 1)) >> 23;   // one up from 1.75 / 1.875 times a power of two on
+  return (int)min(max(e, (uint32_t)BINS + 1), 255u);
+}
+// the largest over the 8 lanes that hold a block of 32
+__device__ __forceinline__ uint32_t block_max(uint32_t x) {
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, true));    // lanes 1 0 3 2
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, true));    // lanes 2 3 0 1
+  return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xF, 0xF, true));   // lanes 7 6 5 4 3 2 1 0
+}
+__device__ __forceinline__ uint32_t random_bits(uint32_t number, uint32_t seed) {
+  uint32_t x = number * 0x9E3779B1u + seed;
+  x ^= x >> 16; x *= 0x7feb352du; x ^= x >> 15; x *= 0x846ca68bu;
+  return x ^ (x >> 16);
+}
+
+template <class P, class G, bool MASTER, bool BITS8>
+__global__ __launch_bounds__(NT) void adamw_step_kernel(Table t, Hyper h) {
+  float factor = 1.f;
+  if (h.grad_norm) {
+    factor = h.grad_norm[1];
+    if (factor != factor) return;
+  }
+  float lr = h.lr, alpha = h.alpha, root = h.root;
+  if (h.lr_dev || h.step_dev) {
+    const double step = h.step_dev ? (double)max(*h.step_dev, 1) : (double)h.step;
+    if (h.lr_dev) lr = *h.lr_dev;
+    alpha = (float)((double)lr / -expm1(step * h.log_b1));
+    root = (float)(1.0 / sqrt(-expm1(step * h.log_b2)));
+  }
+  const int k = find_tensor(t, blockIdx.x);
+  const Entry& e = t.e[k];
+  const uint64_t at = (uint64_t)(blockIdx.x - t.first[k]) * kChunk;
+  const uint32_t left = (uint32_t)min(e.n - at, (uint64_t)kChunk);   // elements of this chunk
+  typedef typename std::conditional<BITS8, uint8_t, float>::type S;
+  const G* g = (const G*)e.grad + at;
+  S *m = (S*)e.m + at, *v = (S*)e.v + at;
+  P* p = (P*)e.param + at;
+  float* w = MASTER ? e.master + at : nullptr;
+  const float keep = 1.f - lr * e.wd;
+
+  typename Wide<G>::type tg[kReps];
+  typename Wide<S>::type tm[kReps], tv[kReps];
+  typename Wide<P>::type tp[kReps];
+  f32x4 tw[kReps];
+  int sm[kReps], sv[kReps];
+#pragma unroll
+  for (int r = 0; r < kReps; r++) {
+    const uint32_t i = (r * NT + threadIdx.x) * VEC;
+    const int rest = i < left ? (int)(left - i) : 0;
+    const bool whole = h.aligned && rest >= VEC;
+    tg[r] = load4v<G>(g + i, whole, rest);
+    tm[r] = load4v<S>(m + i, whole, rest);
+    tv[r] = load4v<S>(v + i, whole, rest);
+    if constexpr (MASTER) tw[r] = load4v<float>(w + i, whole, rest);
+    else tp[r] = load4v<P>(p + i, whole, rest);
+    if constexpr (BITS8) {
+      sm[r] = rest ? e.ms[(at + i) / kBlock] : 0;
+      sv[r] = rest ? e.vs[(at + i) / kBlock] : 0;
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < kReps; r++) {
+    const uint32_t i = (r * NT + threadIdx.x) * VEC;
+    const int rest = i < left ? (int)(left - i) : 0;
+    const bool whole = h.aligned && rest >= VEC;
+    float nm[VEC], nv[VEC];
+    f32x4 nw;
+#pragma unroll
+    for (int j = 0; j < VEC; j++) {
+#pragma clang fp contract(off)
+      const float gr = (float)tg[r][j] * factor;
+      float om, ov;
+      if constexpr (BITS8) {
+        om = decode<15>(tm[r][j] & 127, sm[r]);
+        om = tm[r][j] & 128 ? -om : om;
+        ov = decode<31>(tv[r][j], sv[r]);
+      } else {
+        om = tm[r][j];
+        ov = tv[r][j];
+      }
+      nm[j] = om + h.c1 * (gr - om);
+      nv[j] = ov + h.c2 * (gr * gr - ov);
+    }
+#pragma unroll
+    for (int j = 0; j < VEC; j++) {
+      const float old = MASTER ? tw[r][j] : (float)tp[r][j];
+      const float denom = __builtin_fmaf(__builtin_amdgcn_sqrtf(nv[j]), root, h.eps);
+      nw[j] = __builtin_fmaf(old, keep, -alpha * nm[j] * __builtin_amdgcn_rcpf(denom));
+    }
+    typename Wide<S>::type om, ov;
+    if constexpr (BITS8) {
+      uint32_t am = 0, av = 0;
+#pragma unroll
+      for (int j = 0; j < VEC; j++) {
+        if (j < rest) {
+          am = max(am, __float_as_uint(nm[j]) & 0x7fffffffu);
+          av = max(av, __float_as_uint(nv[j]) & 0x7fffffffu);
+        }
+      }
+      const int s1 = scale_of<15>(block_max(am)), s2 = scale_of<31>(block_max(av));
+#pragma unroll
+      for (int j = 0; j < VEC; j++) {
+        const uint32_t bits = random_bits(e.number + (uint32_t)at + i + j, h.seed);
+        const uint32_t cm = s1 == 255 ? 0x7f : encode<15>(fabsf(nm[j]), s1, bits & 0xffff);
+        const uint32_t cv = s2 == 255 ? 0xff : max(encode<31>(nv[j], s2, bits >> 16), nv[j] > 0.f ? 1u : 0u);
+        om[j] = (uint8_t)(cm | (__float_as_uint(nm[j]) >> 31 << 7));
+        ov[j] = (uint8_t)cv;
+      }
+      if (rest && (threadIdx.x & 7) == 0) {
+        e.ms[(at + i) / kBlock] = (uint8_t)s1;
+        e.vs[(at + i) / kBlock] = (uint8_t)s2;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < VEC; j++) { om[j] = nm[j]; ov[j] = nv[j]; }
+    }
+    store4v<S>(m + i, om, whole, rest);
+    store4v<S>(v + i, ov, whole, rest);
+    if constexpr (MASTER) store4v<float>(w + i, nw, whole, rest);
+    typename Wide<P>::type np;
+#pragma unroll
+    for (int j = 0; j < VEC; j++) np[j] = (P)nw[j];
+    store4v<P>(p + i, np, whole, rest);
+  }
+}
+
+// ---- the norm of all gradients: a block's partial sum in fp64 for each of a fixed number of blocks, then one block adds those up in order
+constexpr int kNormReps = 8, kNormChunk = NT * VEC * kNormReps, kNormBlocks = 1024;
+
+template <class G>
+__global__ __launch_bounds__(NT) void grad_norm_kernel(Table t, uint32_t chunks, double* __restrict__ part, int aligned) {
+  __shared__ double red[NT / 64];
+  double s = 0;
+  for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
+    const int k = find_tensor(t, c);
+    const Entry& e = t.e[k];
+    const uint64_t at = (uint64_t)(c - t.first[k]) * kNormChunk;
+    const uint32_t left = (uint32_t)min(e.n - at, (uint64_t)kNormChunk);
+    const G* g = (const G*)e.grad + at;
+    typename Wide<G>::type x[kNormReps];
+#pragma unroll
+    for (int r = 0; r < kNormReps; r++) {
+      const uint32_t i = (r * NT + threadIdx.x) * VEC;
+      const int rest = i < left ? (int)(left - i) : 0;
+      x[r] = load4v<G>(g + i, aligned && rest >= VEC, rest);
+    }
+#pragma unroll
+    for (int r = 0; r < kNormReps; r++)
+#pragma unroll
+      for (int j = 0; j < VEC; j++) {
+        const double d = (double)(float)x[r][j];
+        s = __builtin_fma(d, d, s);
+      }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) part[blockIdx.x] = red[0] + red[1] + red[2] + red[3];
+}
+
+__global__ __launch_bounds__(NT) void norm_join_kernel(const double* __restrict__ part, int n, float max_norm, float* __restrict__ out) {
+  __shared__ double red[NT / 64];
+  double s = 0;
+  for (int i = threadIdx.x; i < n; i += NT) s += part[i];
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const float norm = (float)sqrt(red[0] + red[1] + red[2] + red[3]);
+    out[0] = norm;
+    out[1] = !__builtin_isfinite(norm) ? __builtin_nanf("") : max_norm > 0.f && norm > max_norm ? max_norm / norm : 1.f;
+  }
+}
+
+// ---- what 8-bit states stand for
+__global__ __launch_bounds__(NT) void state_values_kernel(Table t, int aligned) {
+  const int k = find_tensor(t, blockIdx.x);
+  const Entry& e = t.e[k];
+  const uint64_t at = (uint64_t)(blockIdx.x - t.first[k]) * kChunk;
+  const uint32_t left = (uint32_t)min(e.n - at, (uint64_t)kChunk);
+  const uint8_t *m = (const uint8_t*)e.m + at, *v = (const uint8_t*)e.v + at;
+  bf16 *mo = (bf16*)e.param + at, *vo = (bf16*)e.master + at;   // (the table's places for what a step writes)
+#pragma unroll
+  for (int r = 0; r < kReps; r++) {
+    const uint32_t i = (r * NT + threadIdx.x) * VEC;
+    const int rest = i < left ? (int)(left - i) : 0;
+    const bool whole = aligned && rest >= VEC;
+    if (rest == 0) break;
+    const u8x4 cm = load4v<uint8_t>(m + i, whole, rest), cv = load4v<uint8_t>(v + i, whole, rest);
+    const int sm = e.ms[(at + i) / kBlock], sv = e.vs[(at + i) / kBlock];
+    bf16x4 om, ov;
+#pragma unroll
+    for (int j = 0; j < VEC; j++) {
+      const float x = decode<15>(cm[j] & 127, sm);
+      om[j] = (bf16)(cm[j] & 128 ? -x : x);
+      ov[j] = (bf16)decode<31>(cv[j], sv);
+    }
+    store4v<bf16>(mo + i, om, whole, rest);
+    store4v<bf16>(vo + i, ov, whole, rest);
+  }
+}
+
+// Fills tables with the tensors that have elements and calls launch(table, blocks of `chunk` elements) for each.
+template <class F>
+hipError_t by_tables(const ah_adamw_tensor_t* x, int n, uint32_t chunk, void* const* m_out, void* const* v_out, const F& launch) {
+  Table t;
+  uint64_t number = 0, blocks = 0;
+  int count = 0;
+  auto flush = [&]() {
+    if (count == 0) return hipSuccess;
+    for (int i = count; i < kTensors; i++) t.first[i] = UINT32_MAX;
+    const hipError_t e = launch(t, (uint32_t)blocks);
+    count = 0;
+    blocks = 0;
+    return e;
+  };
+  for (int i = 0; i < n; i++) {
+    const uint64_t need = (x[i].n + chunk - 1) / chunk;
+    if (count == kTensors || blocks + need > kMaxBlocks) {
+      const hipError_t e = flush();
+      if (e != hipSuccess) return e;
+    }
+    if (need) {
+      t.first[count] = (uint32_t)blocks;
+      t.e[count++] = {m_out ? m_out[i] : x[i].param, x[i].grad, x[i].m, x[i].v, x[i].m_scale, x[i].v_scale,
+                      v_out ? (float*)v_out[i] : x[i].master, x[i].n, (uint32_t)number, x[i].weight_decay};
+      blocks += need;
+    }
+    number += (x[i].n + 63) / 64 * 64;
+  }
+  return flush();
+}
+
+// Launches that the workspace of a list's norm has room for: full tables, and some that end early for the number of their blocks (two of those
+// together hold 2^36 gradients)
+int norm_launches(int n) { return (n + kTensors - 1) / kTensors + 8; }
+
+inline bool off(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) != 0; }
+
+// Types of a tensor's gradients, parameters and states as bytes an element; vector access needs VEC of them aligned
+struct Widths { int p, g, s; };
+bool vectors(const ah_adamw_tensor_t& x, const Widths& w) {
+  return !(off(x.grad, VEC * w.g) || off(x.param, VEC * w.p) || off(x.m, VEC * w.s) || off(x.v, VEC * w.s) || off(x.master, VEC * 4));
+}
+
+int check_list(const char* who, const ah_adamw_tensor_t* x, int n) {
+  if (n < 0 || (n > 0 && !x)) return set_error(AH_EINVAL, "%s: bad tensor list", who);
+  for (int i = 0; i < n; i++)
+    if (x[i].n > kMaxElements) return set_error(AH_EUNSUPPORTED, "%s: tensor %d has %llu elements, more than 2^34", who, i, (unsigned long long)x[i].n);
+  return AH_OK;
+}
+
+}  // namespace
+
+extern "C" int ah_adamw_step(const ah_adamw_t* c, const ah_adamw_tensor_t* x, int n, void* stream) {
+  discard_stale_hip_error();
+  if (!c) return set_error(AH_EINVAL, "ah_adamw_step: config is NULL");
+  if (c->struct_size != sizeof(ah_adamw_t)) return set_error(AH_EINVAL, "ah_adamw_step: struct_size %u != %zu", c->struct_size, sizeof(ah_adamw_t));
+  if ((c->param_type != AH_BF16 && c->param_type != AH_FP32) || (c->grad_type != AH_BF16 && c->grad_type != AH_FP32))
+    return set_error(AH_EINVAL, "ah_adamw_step: types must be AH_BF16 or AH_FP32");
+  if (c->state_bits != 32 && c->state_bits != 8) return set_error(AH_EUNSUPPORTED, "ah_adamw_step: state_bits %d: 32 or 8", c->state_bits);
+  if (!(c->lr >= 0) || !std::isfinite(c->lr) || !(c->beta1 >= 0 && c->beta1 < 1) || !(c->beta2 >= 0 && c->beta2 < 1) || !(c->eps > 0) || !std::isfinite(c->eps))
+    return set_error(AH_EINVAL, "ah_adamw_step: need finite lr >= 0, betas in [0, 1) and eps > 0");
+  if (c->step < 1 && !c->step_dev) return set_error(AH_EINVAL, "ah_adamw_step: step must be >= 1");
+  if (off(c->lr_dev, 4) || off(c->step_dev, 4) || off(c->grad_norm, 4)) return set_error(AH_EINVAL, "ah_adamw_step: misaligned device scalar");
+  if (int rc = check_list("ah_adamw_step", x, n)) return rc;
+  const bool bits8 = c->state_bits == 8, p32 = c->param_type == AH_FP32, g32 = c->grad_type == AH_FP32;
+  const Widths w = {p32 ? 4 : 2, g32 ? 4 : 2, bits8 ? 1 : 4};
+  bool master = false, aligned = true, any = false;
+  for (int i = 0; i < n; i++) {
+    if (!x[i].n) continue;
+    if (!x[i].param || !x[i].grad || !x[i].m || !x[i].v || (bits8 && (!x[i].m_scale || !x[i].v_scale))) return set_error(AH_EINVAL, "ah_adamw_step: tensor %d has a NULL pointer", i);
+    if (off(x[i].param, w.p) || off(x[i].grad, w.g) || off(x[i].m, w.s) || off(x[i].v, w.s) || off(x[i].master, 4)) return set_error(AH_EINVAL, "ah_adamw_step: tensor %d is not aligned to its elements", i);
+    if (!std::isfinite(x[i].weight_decay)) return set_error(AH_EINVAL, "ah_adamw_step: tensor %d: weight_decay is not finite", i);
+    if (any && master != (x[i].master != nullptr)) return set_error(AH_EINVAL, "ah_adamw_step: either all tensors have a master copy or none");
+    master = x[i].master != nullptr;
+    any = true;
+    aligned = aligned && vectors(x[i], w);
+  }
+  if (master && p32) return set_error(AH_EINVAL, "ah_adamw_step: master copies go with bf16 parameters");
+  if (!any) return AH_OK;
+  Hyper h = {};
+  h.c1 = (float)(1 - c->beta1); h.c2 = (float)(1 - c->beta2); h.eps = (float)c->eps; h.lr = (float)c->lr;
+  h.log_b1 = std::log(c->beta1); h.log_b2 = std::log(c->beta2);
+  h.step = c->step;
+  if (c->step >= 1) {
+    h.alpha = (float)(c->lr / -std::expm1((double)c->step * h.log_b1));
+    h.root = (float)(1.0 / std::sqrt(-std::expm1((double)c->step * h.log_b2)));
+  }
+  h.lr_dev = c->lr_dev; h.step_dev = c->step_dev; h.grad_norm = c->grad_norm; h.seed = c->seed; h.aligned = aligned;
+  const hipError_t e = by_tables(x, n, kChunk, nullptr, nullptr, [&](const Table& t, uint32_t blocks) {
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(NT), 0, (hipStream_t)stream, t, h); };
+    auto by_state = [&](auto p, auto g, auto has_master) {
+      typedef decltype(p) PT;
+      typedef decltype(g) GT;
+      if (bits8) go(adamw_step_kernel<PT, GT, decltype(has_master)::value, true>);
+      else go(adamw_step_kernel<PT, GT, decltype(has_master)::value, false>);
+    };
+    auto by_param = [&](auto g) {
+      if (p32) by_state(float(), g, std::false_type());
+      else if (master) by_state(bf16(), g, std::true_type());
+      else by_state(bf16(), g, std::false_type());
+    };
+    if (g32) by_param(float());
+    else by_param(bf16());
+    return hipGetLastError();
+  });
+  return hip_status(e, "ah_adamw_step");
+}
+
+extern "C" int ah_grad_norm_workspace(int n_tensors, uint64_t* bytes) {
+  if (!bytes || n_tensors < 0) return set_error(AH_EINVAL, "ah_grad_norm_workspace: bad argument");
+  *bytes = (uint64_t)kNormBlocks * sizeof(double) * (uint64_t)norm_launches(n_tensors);
+  return AH_OK;
+}
+
+extern "C" int ah_grad_norm(const ah_adamw_tensor_t* x, int n, int grad_type, double max_norm, float* out, void* workspace, void* stream) {
+  discard_stale_hip_error();
+  if (!out || !workspace || off(out, 4) || off(workspace, 8)) return set_error(AH_EINVAL, "ah_grad_norm: out or workspace is NULL or misaligned");
+  if (grad_type != AH_BF16 && grad_type != AH_FP32) return set_error(AH_EINVAL, "ah_grad_norm: grad_type must be AH_BF16 or AH_FP32");
+  if (!(max_norm >= 0) || !std::isfinite(max_norm)) return set_error(AH_EINVAL, "ah_grad_norm: max_norm must be finite and >= 0");
+  if (int rc = check_list("ah_grad_norm", x, n)) return rc;
+  const bool g32 = grad_type == AH_FP32;
+  bool aligned = true;
+  for (int i = 0; i < n; i++) {
+    if (!x[i].n) continue;
+    if (!x[i].grad || off(x[i].grad, g32 ? 4 : 2)) return set_error(AH_EINVAL, "ah_grad_norm: gradient of tensor %d is NULL or misaligned", i);
+    aligned = aligned && !off(x[i].grad, VEC * (g32 ? 4 : 2));
+  }
+  double* part = (double*)workspace;
+  int parts = 0;
+  hipError_t e = by_tables(x, n, kNormChunk, nullptr, nullptr, [&](const Table& t, uint32_t chunks) {
+    const int blocks = (int)std::min<uint32_t>(chunks, kNormBlocks);
+    if (parts + blocks > kNormBlocks * norm_launches(n)) return hipErrorInvalidValue;
+    auto kernel = g32 ? grad_norm_kernel<float> : grad_norm_kernel<bf16>;
+    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(NT), 0, (hipStream_t)stream, t, chunks, part + parts, (int)aligned);
+    parts += blocks;
+    return hipGetLastError();
+  });
+  if (e == hipSuccess) {
+    hipLaunchKernelGGL(norm_join_kernel, dim3(1), dim3(NT), 0, (hipStream_t)stream, part, parts, (float)max_norm, out);
+    e = hipGetLastError();
+  }
+  return hip_status(e, "ah_grad_norm");
+}
+
+extern "C" int ah_adamw_state_values(const ah_adamw_tensor_t* x, int n, void* const* m_out, void* const* v_out, void* stream) {
+  discard_stale_hip_error();
+  if (int rc = check_list("ah_adamw_state_values", x, n)) return rc;
+  if (n > 0 && (!m_out || !v_out)) return set_error(AH_EINVAL, "ah_adamw_state_values: output lists are NULL");
+  bool aligned = true;
+  for (int i = 0; i < n; i++) {
+    if (!x[i].n) continue;
+    if (!x[i].m || !x[i].v || !x[i].m_scale || !x[i].v_scale || !m_out[i] || !v_out[i]) return set_error(AH_EINVAL, "ah_adamw_state_values: tensor %d has a NULL pointer", i);
+    if (off(m_out[i], 2) || off(v_out[i], 2)) return set_error(AH_EINVAL, "ah_adamw_state_values: output %d is misaligned", i);
+    aligned = aligned && !(off(x[i].m, VEC) || off(x[i].v, VEC) || off(m_out[i], VEC * 2) || off(v_out[i], VEC * 2));
+  }
+  const hipError_t e = by_tables(x, n, kChunk, m_out, v_out, [&](const Table& t, uint32_t blocks) {
+    hipLaunchKernelGGL(state_values_kernel, dim3(blocks), dim3(NT), 0, (hipStream_t)stream, t, (int)aligned);
+    return hipGetLastError();
+  });
+  return hip_status(e, "ah_adamw_state_values");
+}
