@@ -363,57 +363,63 @@ def cost_partition_layers(n_layers, t_layer, mem_bytes, fixed_per_layer, act_per
 
 
 # ---- operators beside the stage (include/ah_ops.h).  What the library cannot see is checked here: that a tensor lies on the current device, its
-# type, its size, and that its rows are as the call takes them
+# type, its size, and that its rows are as the call takes them.  The smallest calls last as long as these checks: each looks at a tensor's
+# attributes once.
+import torch  # noqa: E402  (loaded above, before the library)
+
+_BF16, _F32, _I32, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
+_WINDOW_SIZE, _QK_SIZE = C.sizeof(_WindowConfig), C.sizeof(_QkNormConfig)
+
+
 def _refuse(msg, *args):
     raise AhError(1, msg % args)
 
 
 def _on_device(what, t):
-    import torch
-    if not t.is_cuda:
+    at = t.get_device()
+    if at < 0:
         _refuse("%s is not in device memory", what)
-    if t.device.index != torch._C._cuda_getDevice():
-        _refuse("%s lies on device %d, which is not the current one", what, t.device.index)
+    if at != torch._C._cuda_getDevice():
+        _refuse("%s lies on device %d, which is not the current one", what, at)
 
 
-def _dense(what, t, dtypes, n=None):
+def _dense(what, t, dtype, n=None):
+    """Address of a contiguous tensor of n elements."""
     _on_device(what, t)
-    if t.dtype not in dtypes or not t.is_contiguous() or (n is not None and t.numel() != n):
-        _refuse("%s: %s of shape %s (contiguous: %s), wanted a contiguous tensor of %s%s", what, t.dtype, tuple(t.shape), t.is_contiguous(),
-                " or ".join(str(d) for d in dtypes), "" if n is None else " with %d elements" % n)
+    if t.dtype is not dtype or not t.is_contiguous() or (n is not None and t.numel() != n):
+        _refuse("%s: %s of shape %s (contiguous: %s), wanted a contiguous tensor of %s%s", what, t.dtype, tuple(t.shape), t.is_contiguous(), dtype,
+                "" if n is None else " with %d elements" % n)
+    return t.data_ptr()
 
 
 def _rows(what, t, rows, cols):
-    """A bf16 matrix whose rows are dense and 16-byte aligned, at any distance from each other; returns that distance."""
-    import torch
+    """(address, columns from row to row) of a bf16 matrix whose rows are dense and 16-byte aligned, at any distance from each other."""
     _on_device(what, t)
-    if t.dtype != torch.bfloat16 or t.dim() != 2 or t.shape[1] != cols or (rows is not None and t.shape[0] != rows):
-        _refuse("%s: %s of shape %s, wanted bf16 [%s, %d]", what, t.dtype, tuple(t.shape), "rows" if rows is None else rows, cols)
-    if t.shape[0] <= 1:
-        ld = cols
-    else:
-        ld = t.stride(0)
-    if (cols > 1 and t.stride(1) != 1) or ld < cols or ld % 8 or t.data_ptr() % 16:
-        _refuse("%s: rows must be dense, 16-byte aligned and a multiple of 8 columns apart (strides %s)", what, t.stride())
-    return ld
+    shape, stride, at = t.shape, t.stride(), t.data_ptr()
+    if t.dtype is not _BF16 or len(shape) != 2 or shape[1] != cols or shape[0] != rows:
+        _refuse("%s: %s of shape %s, wanted bf16 [%d, %d]", what, t.dtype, tuple(shape), rows, cols)
+    ld = stride[0] if rows > 1 else cols
+    if stride[1] != 1 or ld < cols or ld & 7 or at & 15:
+        _refuse("%s: rows must be dense, 16-byte aligned and a multiple of 8 columns apart (strides %s)", what, stride)
+    return at, ld
 
 
 def _window_config(n_seq, seq_len, nh, nh_kv, d, window, sinks):
-    return _WindowConfig(struct_size=C.sizeof(_WindowConfig), n_seq=n_seq, seq_len=seq_len, n_heads=nh, n_kv_heads=nh_kv, head_dim=d, window=window, sinks=sinks)
+    return _WindowConfig(_WINDOW_SIZE, n_seq, seq_len, nh, nh_kv, d, window, sinks)
 
 
 def _window_args(c, q, k, v, o, lse, offsets):
-    import torch
     wq, wk = c.n_heads * c.head_dim, c.n_kv_heads * c.head_dim
-    T = q.shape[0] if q.dim() == 2 else -1
-    c.ld_q, c.ld_k, c.ld_v, c.ld_o = _rows("q", q, None, wq), _rows("k", k, T, wk), _rows("v", v, T, wk), _rows("o", o, T, wq)
-    _dense("lse", lse, (torch.float32,), c.n_seq * c.n_heads * c.seq_len)
-    c.rows = T
+    c.rows = T = q.shape[0]
+    pq, c.ld_q = _rows("q", q, T, wq)
+    pk, c.ld_k = _rows("k", k, T, wk)
+    pv, c.ld_v = _rows("v", v, T, wk)
+    po, c.ld_o = _rows("o", o, T, wq)
     if offsets is not None:
-        _dense("offsets", offsets, (torch.int32,), c.n_seq + 1)
-        c.offsets = offsets.data_ptr()
+        c.offsets = _dense("offsets", offsets, _I32, c.n_seq + 1)
     elif T != c.n_seq * c.seq_len:
         _refuse("attention_window: %d rows for %d sequences of %d", T, c.n_seq, c.seq_len)
+    return pq, pk, pv, po, _dense("lse", lse, _F32, c.n_seq * c.n_heads * c.seq_len)
 
 
 def attention_window_fwd(q, k, v, o, lse, n_seq, seq_len, nh, nh_kv, d, window, sinks=0, offsets=None, stream=None):
@@ -421,91 +427,85 @@ def attention_window_fwd(q, k, v, o, lse, n_seq, seq_len, nh, nh_kv, d, window, 
     k, v: [T, nh_kv * d], rows at any distance (columns of a packed projection, for one); lse: fp32 [n_seq, nh, seq_len].
     offsets: int32 [n_seq + 1], where packed sequences of at most seq_len rows begin and the last one ends."""
     c = _window_config(n_seq, seq_len, nh, nh_kv, d, window, sinks)
-    _window_args(c, q, k, v, o, lse, offsets)
-    _check(lib.ah_attention_window_fwd(C.byref(c), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _stream(stream)))
+    at = _window_args(c, q, k, v, o, lse, offsets)
+    _check(lib.ah_attention_window_fwd(c, *at, _stream(stream)))
 
 
 def attention_window_bwd_workspace(n_seq, seq_len, nh, nh_kv, d, window, sinks=0):
     """Bytes of scratch memory that attention_window_bwd takes."""
     n = C.c_uint64()
-    _check(lib.ah_attention_window_bwd_workspace(C.byref(_window_config(n_seq, seq_len, nh, nh_kv, d, window, sinks)), C.byref(n)))
+    _check(lib.ah_attention_window_bwd_workspace(_window_config(n_seq, seq_len, nh, nh_kv, d, window, sinks), n))
     return n.value
 
 
 def attention_window_bwd(q, k, v, o, lse, d_o, dq, dk, dv, workspace, n_seq, seq_len, nh, nh_kv, d, window, sinks=0, offsets=None, stream=None):
     """dq, dk, dv of attention_window_fwd from its inputs, its results and d_o.  workspace: uint8, attention_window_bwd_workspace(...) bytes."""
-    import torch
     c = _window_config(n_seq, seq_len, nh, nh_kv, d, window, sinks)
-    _window_args(c, q, k, v, o, lse, offsets)
-    wq, wk = nh * d, nh_kv * d
-    c.ld_do, c.ld_dq, c.ld_dk, c.ld_dv = _rows("d_o", d_o, c.rows, wq), _rows("dq", dq, c.rows, wq), _rows("dk", dk, c.rows, wk), _rows("dv", dv, c.rows, wk)
-    _dense("workspace", workspace, (torch.uint8,))
-    if workspace.numel() < attention_window_bwd_workspace(n_seq, seq_len, nh, nh_kv, d, window, sinks):
+    at = _window_args(c, q, k, v, o, lse, offsets)
+    wq, wk, T = nh * d, nh_kv * d, c.rows
+    pdo, c.ld_do = _rows("d_o", d_o, T, wq)
+    pdq, c.ld_dq = _rows("dq", dq, T, wq)
+    pdk, c.ld_dk = _rows("dk", dk, T, wk)
+    pdv, c.ld_dv = _rows("dv", dv, T, wk)
+    work, need = _dense("workspace", workspace, _U8), C.c_uint64()
+    _check(lib.ah_attention_window_bwd_workspace(c, need))
+    if workspace.numel() < need.value:
         _refuse("attention_window_bwd: the workspace holds %d bytes, too few", workspace.numel())
-    _check(lib.ah_attention_window_bwd(C.byref(c), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(d_o), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(workspace),
-                                       _stream(stream)))
+    _check(lib.ah_attention_window_bwd(c, *at, pdo, pdq, pdk, pdv, work, _stream(stream)))
 
 
 def rope_table(cos_sin, d, base=10000.0, stream=None):
     """Fills cos_sin, fp32 [n_pos, d / 2, 2], with the angles of the stage's rotary embedding."""
-    import torch
     if cos_sin.dim() != 3 or cos_sin.shape[1:] != (d // 2, 2):
         _refuse("rope_table: cos_sin is %s, wanted [n_pos, %d, 2]", tuple(cos_sin.shape), d // 2)
-    _dense("cos_sin", cos_sin, (torch.float32,))
-    _check(lib.ah_rope_table(_ptr(cos_sin), cos_sin.shape[0], d, float(base), _stream(stream)))
+    _check(lib.ah_rope_table(_dense("cos_sin", cos_sin, _F32), cos_sin.shape[0], d, float(base), _stream(stream)))
 
 
-def _qk_config(x, other, gain_q, gain_k, cos_sin, seq_len, nh, nh_kv, d, eps, positions):
-    import torch
-    c = _QkNormConfig(struct_size=C.sizeof(_QkNormConfig), seq_len=seq_len, n_heads=nh, n_kv_heads=nh_kv, head_dim=d, eps=eps)
-    w = (nh + nh_kv) * d
-    c.ld_x = _rows("x", x, None, w)
-    c.rows = x.shape[0]
-    c.ld_y = _rows("y or dy", other, c.rows, w)
-    for name, g, n in (("gain_q", gain_q, nh), ("gain_k", gain_k, nh_kv)):
-        if n:
-            _dense(name, g, (torch.bfloat16,), d)
-            setattr(c, name, g.data_ptr())
+def _qk_args(x, other, gain_q, gain_k, cos_sin, seq_len, nh, nh_kv, d, eps, positions):
+    w, T = (nh + nh_kv) * d, x.shape[0]
+    px, ld_x = _rows("x", x, T, w)
+    po, ld_o = _rows("y or dy", other, T, w)
+    pq = _dense("gain_q", gain_q, _BF16, d) if nh else None
+    pk = _dense("gain_k", gain_k, _BF16, d) if nh_kv else None
+    table = pos = None
+    n_pos = 0
     if cos_sin is not None:
-        if cos_sin.dim() != 3 or cos_sin.shape[1:] != (d // 2, 2):
+        n_pos = cos_sin.shape[0]
+        table = _dense("cos_sin", cos_sin, _F32, n_pos * d)
+        if cos_sin.shape != (n_pos, d // 2, 2):
             _refuse("cos_sin is %s, wanted [n_pos, %d, 2]", tuple(cos_sin.shape), d // 2)
-        _dense("cos_sin", cos_sin, (torch.float32,))
-        c.cos_sin, c.n_pos = cos_sin.data_ptr(), cos_sin.shape[0]
         if positions is not None:
-            _dense("positions", positions, (torch.int32,), c.rows)
-            c.positions = positions.data_ptr()
-    return c
+            pos = _dense("positions", positions, _I32, T)
+    return _QkNormConfig(_QK_SIZE, T, seq_len, nh, nh_kv, d, n_pos, eps, ld_x, ld_o, 0, pq, pk, table, pos), px, po
 
 
 def qk_norm_rope_fwd(x, gain_q, gain_k, cos_sin, y, seq_len, nh, nh_kv, d, eps=1e-6, positions=None, stream=None):
     """RMS norm of every head with its gain, then the rotation (ah_qk_norm_rope_fwd).  x, y: [T, (nh + nh_kv) * d], query heads then key heads, rows at
     any distance (the first columns of a packed projection); y may be x.  cos_sin: see rope_table; None: no rotation.  positions: int32 [T], without them
     row t has position t % seq_len."""
-    c = _qk_config(x, y, gain_q, gain_k, cos_sin, seq_len, nh, nh_kv, d, eps, positions)
-    _check(lib.ah_qk_norm_rope_fwd(C.byref(c), _ptr(x), _ptr(y), _stream(stream)))
+    c, px, py = _qk_args(x, y, gain_q, gain_k, cos_sin, seq_len, nh, nh_kv, d, eps, positions)
+    _check(lib.ah_qk_norm_rope_fwd(c, px, py, _stream(stream)))
 
 
 def qk_norm_rope_bwd_workspace(rows, nh, nh_kv, d):
     """Bytes of scratch memory that qk_norm_rope_bwd takes."""
     n = C.c_uint64()
-    c = _QkNormConfig(struct_size=C.sizeof(_QkNormConfig), rows=rows, n_heads=nh, n_kv_heads=nh_kv, head_dim=d)
-    _check(lib.ah_qk_norm_rope_bwd_workspace(C.byref(c), C.byref(n)))
+    _check(lib.ah_qk_norm_rope_bwd_workspace(_QkNormConfig(_QK_SIZE, rows, 0, nh, nh_kv, d), n))
     return n.value
 
 
 def qk_norm_rope_bwd(x, gain_q, gain_k, cos_sin, dy, dx, d_gain_q, d_gain_k, workspace, seq_len, nh, nh_kv, d, eps=1e-6, positions=None, beta=0,
                      stream=None):
     """dx from x and dy (dx may be either), and d_gain = beta * d_gain + the gain's gradient (fp32 [d]).  workspace: uint8, qk_norm_rope_bwd_workspace(...) bytes."""
-    import torch
-    c = _qk_config(x, dy, gain_q, gain_k, cos_sin, seq_len, nh, nh_kv, d, eps, positions)
-    c.ld_dx = _rows("dx", dx, c.rows, (nh + nh_kv) * d)
-    for name, g, n in (("d_gain_q", d_gain_q, nh), ("d_gain_k", d_gain_k, nh_kv)):
-        if n:
-            _dense(name, g, (torch.float32,), d)
-    _dense("workspace", workspace, (torch.uint8,))
-    if workspace.numel() < qk_norm_rope_bwd_workspace(c.rows, nh, nh_kv, d):
+    c, px, pdy = _qk_args(x, dy, gain_q, gain_k, cos_sin, seq_len, nh, nh_kv, d, eps, positions)
+    pdx, c.ld_dx = _rows("dx", dx, c.rows, (nh + nh_kv) * d)
+    pgq = _dense("d_gain_q", d_gain_q, _F32, d) if nh else None
+    pgk = _dense("d_gain_k", d_gain_k, _F32, d) if nh_kv else None
+    work, need = _dense("workspace", workspace, _U8), C.c_uint64()
+    _check(lib.ah_qk_norm_rope_bwd_workspace(c, need))
+    if workspace.numel() < need.value:
         _refuse("qk_norm_rope_bwd: the workspace holds %d bytes, too few", workspace.numel())
-    _check(lib.ah_qk_norm_rope_bwd(C.byref(c), _ptr(x), _ptr(dy), _ptr(dx), _ptr(d_gain_q), _ptr(d_gain_k), int(beta), _ptr(workspace), _stream(stream)))
+    _check(lib.ah_qk_norm_rope_bwd(c, px, pdy, pdx, pgq, pgk, int(beta), work, _stream(stream)))
 
 
 class AdamW:
@@ -520,7 +520,6 @@ class AdamW:
 
     def __init__(self, params, grads, betas=(0.9, 0.95), eps=1e-8, weight_decay=0.0, state_bits=32, master=None, m=None, v=None,
                  m_scale=None, v_scale=None):
-        import torch
         params, grads = list(params), list(grads)
         n = len(params)
         if n == 0 or len(grads) != n:
@@ -530,16 +529,15 @@ class AdamW:
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
         if len(decay) != n:
             _refuse("AdamW: %d weight decays for %d parameters", len(decay), n)
-        kinds = (torch.bfloat16, torch.float32)
         p_type, g_type = params[0].dtype, grads[0].dtype
+        if p_type not in (_BF16, _F32) or g_type not in (_BF16, _F32):
+            _refuse("AdamW: parameters of %s and gradients of %s, wanted bf16 or fp32", p_type, g_type)
         self._device = params[0].device
         sizes = [p.numel() for p in params]
         for k in range(n):
-            _dense("AdamW: parameter %d" % k, params[k], kinds)
-            _dense("AdamW: gradient %d" % k, grads[k], kinds, sizes[k])
-            if params[k].dtype != p_type or grads[k].dtype != g_type:
-                _refuse("AdamW: parameters (and gradients) of one call are of one type")
-        wide = torch.float32 if state_bits == 32 else torch.uint8
+            _dense("AdamW: parameter %d" % k, params[k], p_type)
+            _dense("AdamW: gradient %d" % k, grads[k], g_type, sizes[k])
+        wide = _F32 if state_bits == 32 else _U8
 
         def state(what, given, dtype, per):
             counts = [(x + per - 1) // per for x in sizes]
@@ -553,18 +551,18 @@ class AdamW:
             if len(given) != n:
                 _refuse("AdamW: %d tensors of %s for %d parameters", len(given), what, n)
             for k in range(n):
-                _dense("AdamW: %s %d" % (what, k), given[k], (dtype,), counts[k])
+                _dense("AdamW: %s %d" % (what, k), given[k], dtype, counts[k])
             return given
 
-        self.params, self.grads = params, grads
+        self.params, self.grads, self._sizes = params, grads, sizes
         self.m, self.v = state("m", m, wide, 1), state("v", v, wide, 1)
-        self.m_scale = state("m_scale", m_scale, torch.uint8, 32) if state_bits == 8 else None
-        self.v_scale = state("v_scale", v_scale, torch.uint8, 32) if state_bits == 8 else None
+        self.m_scale = state("m_scale", m_scale, _U8, 32) if state_bits == 8 else None
+        self.v_scale = state("v_scale", v_scale, _U8, 32) if state_bits == 8 else None
         self.master = None
         if master is not None and master is not False:
-            if p_type != torch.bfloat16:
+            if p_type != _BF16:
                 _refuse("AdamW: master copies go with bf16 parameters")
-            self.master = state("master", None if master is True else master, torch.float32, 1)
+            self.master = state("master", None if master is True else master, _F32, 1)
             if master is True:
                 for a, b in zip(self.master, params):
                     a.copy_(b.reshape(-1))
@@ -577,53 +575,50 @@ class AdamW:
             if self.master is not None:
                 e.master = self.master[k].data_ptr()
             e.weight_decay = float(decay[k])
-        self._cfg = _AdamWConfig(struct_size=C.sizeof(_AdamWConfig), param_type=int(p_type == torch.float32), grad_type=int(g_type == torch.float32),
+        self._cfg = _AdamWConfig(struct_size=C.sizeof(_AdamWConfig), param_type=int(p_type == _F32), grad_type=int(g_type == _F32),
                                  state_bits=state_bits, beta1=float(betas[0]), beta2=float(betas[1]), eps=float(eps))
         need = C.c_uint64()
         _check(lib.ah_grad_norm_workspace(n, C.byref(need)))
-        self._norm_work = torch.empty(need.value, dtype=torch.uint8, device=self._device)
+        self._norm_work = torch.empty(need.value, dtype=_U8, device=self._device)
         self._norm = torch.zeros(2, device=self._device)
 
     def grad_norm(self, max_norm=0.0, stream=None):
         """Device tensor [norm of all gradients, factor that brings it down to max_norm] (the object's own: the next call rewrites it).  0: no limit."""
         _on_device("AdamW: parameters", self._norm)
-        _check(lib.ah_grad_norm(self._list, len(self._list), self._cfg.grad_type, float(max_norm), _ptr(self._norm), _ptr(self._norm_work), _stream(stream)))
+        _check(lib.ah_grad_norm(self._list, len(self._list), self._cfg.grad_type, float(max_norm), self._norm.data_ptr(), self._norm_work.data_ptr(), _stream(stream)))
         return self._norm
 
     def step(self, lr, step, grad_norm=None, seed=0, stream=None):
         """One step, number `step` (from 1 on).  lr: a number, or an fp32 tensor of one element on the device; step: likewise, int32 (a captured
         step reads them anew when it is replayed).  grad_norm: what grad_norm() gave: gradients are multiplied by its factor, and where that is NaN
         nothing changes.  seed: of the rounding of 8-bit states, another one for every step."""
-        import torch
         c = self._cfg
         _on_device("AdamW: parameters", self._norm)
         c.lr_dev = c.step_dev = c.grad_norm = None
         if isinstance(lr, torch.Tensor):
-            _dense("AdamW.step: lr", lr, (torch.float32,), 1)
-            c.lr, c.lr_dev = 0.0, lr.data_ptr()
+            c.lr, c.lr_dev = 0.0, _dense("AdamW.step: lr", lr, _F32, 1)
         else:
             c.lr = lr
         if isinstance(step, torch.Tensor):
-            _dense("AdamW.step: step", step, (torch.int32,), 1)
-            c.step, c.step_dev = 1, step.data_ptr()
+            c.step, c.step_dev = 1, _dense("AdamW.step: step", step, _I32, 1)
         else:
             c.step = step
         if grad_norm is not None:
-            _dense("AdamW.step: grad_norm", grad_norm, (torch.float32,), 2)
-            c.grad_norm = grad_norm.data_ptr()
+            c.grad_norm = _dense("AdamW.step: grad_norm", grad_norm, _F32, 2)
         c.seed = seed & 0xFFFFFFFF
-        _check(lib.ah_adamw_step(C.byref(c), self._list, len(self._list), _stream(stream)))
+        _check(lib.ah_adamw_step(c, self._list, len(self._list), _stream(stream)))
 
     def state_values(self, m_out, v_out, stream=None):
         """What 8-bit states stand for, into two lists of bf16 tensors (which hold them exactly)."""
-        import torch
         if self.m_scale is None:
             _refuse("AdamW.state_values: the states are in fp32 (m, v)")
-        n = len(self._list)
-        if len(m_out) != n or len(v_out) != n:
-            _refuse("AdamW.state_values: %d and %d outputs for %d parameters", len(m_out), len(v_out), n)
-        for k in range(n):
-            _dense("AdamW.state_values: m %d" % k, m_out[k], (torch.bfloat16,), self._list[k].n)
-            _dense("AdamW.state_values: v %d" % k, v_out[k], (torch.bfloat16,), self._list[k].n)
-        pm, pv = (C.c_void_p * n)(*[t.data_ptr() for t in m_out]), (C.c_void_p * n)(*[t.data_ptr() for t in v_out])
-        _check(lib.ah_adamw_state_values(self._list, n, pm, pv, _stream(stream)))
+        n, device = len(self._list), self._norm.get_device()
+        _on_device("AdamW: parameters", self._norm)
+        both = [*m_out, *v_out]
+        if len(m_out) != n or [t.numel() for t in both] != self._sizes * 2:
+            _refuse("AdamW.state_values: the outputs are not of the parameters' sizes")
+        for t in both:
+            if t.dtype is not _BF16 or t.get_device() != device or not t.is_contiguous():
+                _refuse("AdamW.state_values: outputs are contiguous bf16 tensors on the parameters' device")
+        at = [t.data_ptr() for t in both]
+        _check(lib.ah_adamw_state_values(self._list, n, (C.c_void_p * n)(*at[:n]), (C.c_void_p * n)(*at[n:]), _stream(stream)))

@@ -17,10 +17,11 @@ using namespace ah;
 
 namespace {
 
-constexpr int NT = 256, kTensors = 48, VEC = 4, kReps = 2;
-constexpr int kChunk = NT * VEC * kReps;     // elements per block
+constexpr int NT = 256, kTensors = 48;
+constexpr int VEC = 4, kReps = 2, kChunk = NT * VEC * kReps;            // elements of a lane at once, times a lane, elements per block
+constexpr int VEC8 = 8, kReps8 = 1, kChunk8 = NT * VEC8 * kReps8;       // with states in 8 bits, of which four elements fill no load
 constexpr int kBlock = 32;                   // elements that share a scale
-constexpr uint64_t kMaxElements = 1ull << 34, kMaxBlocks = kMaxElements / kChunk;   // of a tensor; of a launch (2^23: its threads are counted in 32 bits)
+constexpr uint64_t kMaxElements = 1ull << 34, kMaxBlocks = kMaxElements / 2048;   // of a tensor; of a launch (2^23: its threads are counted in 32 bits)
 
 struct Entry {
   void* param;
@@ -56,30 +57,26 @@ __device__ __forceinline__ int find_tensor(const Table& t, uint32_t block) {
   return k;
 }
 
-// ---- VEC consecutive values of a tensor, from element i on; what lies behind its end reads as 0
-template <class T> struct Wide;
-template <> struct Wide<float> { typedef f32x4 type; };
-template <> struct Wide<bf16> { typedef bf16x4 type; };
-typedef uint8_t u8x4 __attribute__((ext_vector_type(4)));
-template <> struct Wide<uint8_t> { typedef u8x4 type; };
+// ---- N consecutive values of a tensor; what lies behind its end reads as 0
+template <class T, int N> struct Wide { typedef T type __attribute__((ext_vector_type(N))); };
 
-template <class T>
-__device__ __forceinline__ typename Wide<T>::type load4v(const T* p, bool whole, int left) {
-  typename Wide<T>::type r = {};
-  if (whole) return *(const typename Wide<T>::type*)p;
+template <int N, class T>
+__device__ __forceinline__ typename Wide<T, N>::type load_n(const T* p, bool whole, int left) {
+  typename Wide<T, N>::type r = {};
+  if (whole) return *(const typename Wide<T, N>::type*)p;
 #pragma unroll
-  for (int j = 0; j < VEC; j++)
+  for (int j = 0; j < N; j++)
     if (j < left) r[j] = p[j];
   return r;
 }
-template <class T>
-__device__ __forceinline__ void store4v(T* p, typename Wide<T>::type r, bool whole, int left) {
+template <int N, class T>
+__device__ __forceinline__ void store_n(T* p, typename Wide<T, N>::type r, bool whole, int left) {
   if (whole) {
-    *(typename Wide<T>::type*)p = r;
+    *(typename Wide<T, N>::type*)p = r;
     return;
   }
 #pragma unroll
-  for (int j = 0; j < VEC; j++)
+  for (int j = 0; j < N; j++)
     if (j < left) p[j] = r[j];
 }
 
@@ -102,14 +99,15 @@ __device__ __forceinline__ int scale_of(uint32_t top) {
   const uint32_t e = (top + (BINS == 15 ? 0x200000 - 1 : 0x100000 - 1)) >> 23;   // one up from 1.75 / 1.875 times a power of two on
   return (int)min(max(e, (uint32_t)BINS + 1), 255u);
 }
-// the largest over the 8 lanes that hold a block of 32
+// the largest over the 4 lanes that hold a block of 32
+static_assert(VEC8 * 4 == kBlock, "lanes of a block");
 __device__ __forceinline__ uint32_t block_max(uint32_t x) {
-  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, true));    // lanes 1 0 3 2
-  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, true));    // lanes 2 3 0 1
-  return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xF, 0xF, true));   // lanes 7 6 5 4 3 2 1 0
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, true));           // lanes 1 0 3 2
+  return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, true));        // lanes 2 3 0 1
 }
-__device__ __forceinline__ uint32_t random_bits(uint32_t number, uint32_t seed) {
-  uint32_t x = number * 0x9E3779B1u + seed;
+// 32 bits from the product of an element's number with an odd constant plus the seed
+constexpr uint32_t kNumber = 0x9E3779B1u;
+__device__ __forceinline__ uint32_t random_bits(uint32_t x) {
   x ^= x >> 16; x *= 0x7feb352du; x ^= x >> 15; x *= 0x846ca68bu;
   return x ^ (x >> 16);
 }
@@ -130,8 +128,9 @@ __global__ __launch_bounds__(NT) void adamw_step_kernel(Table t, Hyper h) {
   }
   const int k = find_tensor(t, blockIdx.x);
   const Entry& e = t.e[k];
-  const uint64_t at = (uint64_t)(blockIdx.x - t.first[k]) * kChunk;
-  const uint32_t left = (uint32_t)min(e.n - at, (uint64_t)kChunk);   // elements of this chunk
+  constexpr int V = BITS8 ? VEC8 : VEC, R = BITS8 ? kReps8 : kReps;
+  const uint64_t at = (uint64_t)(blockIdx.x - t.first[k]) * (NT * V * R);
+  const uint32_t left = (uint32_t)min(e.n - at, (uint64_t)(NT * V * R));   // elements of this chunk
   typedef typename std::conditional<BITS8, uint8_t, float>::type S;
   const G* g = (const G*)e.grad + at;
   S *m = (S*)e.m + at, *v = (S*)e.v + at;
@@ -139,35 +138,35 @@ __global__ __launch_bounds__(NT) void adamw_step_kernel(Table t, Hyper h) {
   float* w = MASTER ? e.master + at : nullptr;
   const float keep = 1.f - lr * e.wd;
 
-  typename Wide<G>::type tg[kReps];
-  typename Wide<S>::type tm[kReps], tv[kReps];
-  typename Wide<P>::type tp[kReps];
-  f32x4 tw[kReps];
-  int sm[kReps], sv[kReps];
+  typename Wide<G, V>::type tg[R];
+  typename Wide<S, V>::type tm[R], tv[R];
+  typename Wide<P, V>::type tp[R];
+  typename Wide<float, V>::type tw[R];
+  int sm[R], sv[R];
 #pragma unroll
-  for (int r = 0; r < kReps; r++) {
-    const uint32_t i = (r * NT + threadIdx.x) * VEC;
+  for (int r = 0; r < R; r++) {
+    const uint32_t i = (r * NT + threadIdx.x) * V;
     const int rest = i < left ? (int)(left - i) : 0;
-    const bool whole = h.aligned && rest >= VEC;
-    tg[r] = load4v<G>(g + i, whole, rest);
-    tm[r] = load4v<S>(m + i, whole, rest);
-    tv[r] = load4v<S>(v + i, whole, rest);
-    if constexpr (MASTER) tw[r] = load4v<float>(w + i, whole, rest);
-    else tp[r] = load4v<P>(p + i, whole, rest);
+    const bool whole = h.aligned && rest >= V;
+    tg[r] = load_n<V, G>(g + i, whole, rest);
+    tm[r] = load_n<V, S>(m + i, whole, rest);
+    tv[r] = load_n<V, S>(v + i, whole, rest);
+    if constexpr (MASTER) tw[r] = load_n<V, float>(w + i, whole, rest);
+    else tp[r] = load_n<V, P>(p + i, whole, rest);
     if constexpr (BITS8) {
       sm[r] = rest ? e.ms[(at + i) / kBlock] : 0;
       sv[r] = rest ? e.vs[(at + i) / kBlock] : 0;
     }
   }
 #pragma unroll
-  for (int r = 0; r < kReps; r++) {
-    const uint32_t i = (r * NT + threadIdx.x) * VEC;
+  for (int r = 0; r < R; r++) {
+    const uint32_t i = (r * NT + threadIdx.x) * V;
     const int rest = i < left ? (int)(left - i) : 0;
-    const bool whole = h.aligned && rest >= VEC;
-    float nm[VEC], nv[VEC];
-    f32x4 nw;
+    const bool whole = h.aligned && rest >= V;
+    float nm[V], nv[V];
+    typename Wide<float, V>::type nw;
 #pragma unroll
-    for (int j = 0; j < VEC; j++) {
+    for (int j = 0; j < V; j++) {
 #pragma clang fp contract(off)
       const float gr = (float)tg[r][j] * factor;
       float om, ov;
@@ -183,50 +182,60 @@ __global__ __launch_bounds__(NT) void adamw_step_kernel(Table t, Hyper h) {
       nv[j] = ov + h.c2 * (gr * gr - ov);
     }
 #pragma unroll
-    for (int j = 0; j < VEC; j++) {
+    for (int j = 0; j < V; j++) {
       const float old = MASTER ? tw[r][j] : (float)tp[r][j];
       const float denom = __builtin_fmaf(__builtin_amdgcn_sqrtf(nv[j]), root, h.eps);
       nw[j] = __builtin_fmaf(old, keep, -alpha * nm[j] * __builtin_amdgcn_rcpf(denom));
     }
-    typename Wide<S>::type om, ov;
+    typename Wide<S, V>::type om, ov;
     if constexpr (BITS8) {
       uint32_t am = 0, av = 0;
 #pragma unroll
-      for (int j = 0; j < VEC; j++) {
+      for (int j = 0; j < V; j++) {
         if (j < rest) {
           am = max(am, __float_as_uint(nm[j]) & 0x7fffffffu);
           av = max(av, __float_as_uint(nv[j]) & 0x7fffffffu);
         }
       }
       const int s1 = scale_of<15>(block_max(am)), s2 = scale_of<31>(block_max(av));
+      const uint32_t first = (e.number + (uint32_t)at + i) * kNumber + h.seed;
 #pragma unroll
-      for (int j = 0; j < VEC; j++) {
-        const uint32_t bits = random_bits(e.number + (uint32_t)at + i + j, h.seed);
+      for (int j = 0; j < V; j++) {
+        const uint32_t bits = random_bits(first + j * kNumber);
         const uint32_t cm = s1 == 255 ? 0x7f : encode<15>(fabsf(nm[j]), s1, bits & 0xffff);
         const uint32_t cv = s2 == 255 ? 0xff : max(encode<31>(nv[j], s2, bits >> 16), nv[j] > 0.f ? 1u : 0u);
         om[j] = (uint8_t)(cm | (__float_as_uint(nm[j]) >> 31 << 7));
         ov[j] = (uint8_t)cv;
       }
-      if (rest && (threadIdx.x & 7) == 0) {
+      if (rest && (threadIdx.x & 3) == 0) {
         e.ms[(at + i) / kBlock] = (uint8_t)s1;
         e.vs[(at + i) / kBlock] = (uint8_t)s2;
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < VEC; j++) { om[j] = nm[j]; ov[j] = nv[j]; }
+      for (int j = 0; j < V; j++) { om[j] = nm[j]; ov[j] = nv[j]; }
     }
-    store4v<S>(m + i, om, whole, rest);
-    store4v<S>(v + i, ov, whole, rest);
-    if constexpr (MASTER) store4v<float>(w + i, nw, whole, rest);
-    typename Wide<P>::type np;
+    store_n<V, S>(m + i, om, whole, rest);
+    store_n<V, S>(v + i, ov, whole, rest);
+    if constexpr (MASTER) store_n<V, float>(w + i, nw, whole, rest);
+    typename Wide<P, V>::type np;
 #pragma unroll
-    for (int j = 0; j < VEC; j++) np[j] = (P)nw[j];
-    store4v<P>(p + i, np, whole, rest);
+    for (int j = 0; j < V; j++) np[j] = (P)nw[j];
+    store_n<V, P>(p + i, np, whole, rest);
   }
 }
 
-// ---- the norm of all gradients: a block's partial sum in fp64 for each of a fixed number of blocks, then one block adds those up in order
+// ---- the norm of all gradients: a partial sum in fp64 for each of a fixed number of blocks, which a second launch adds up in order.  (Added up by the
+// block that finishes last, a launch less: 8.8 us for 1.6 M gradients and 158 for 100 M instead of 6.4 and 120: the ordering at the end of every block flushes caches.)
 constexpr int kNormReps = 8, kNormChunk = NT * VEC * kNormReps, kNormBlocks = 1024;
+
+__device__ __forceinline__ double block_sum(double s, double* red) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  return red[0] + red[1] + red[2] + red[3];
+}
 
 template <class G>
 __global__ __launch_bounds__(NT) void grad_norm_kernel(Table t, uint32_t chunks, double* __restrict__ part, int aligned) {
@@ -238,12 +247,12 @@ __global__ __launch_bounds__(NT) void grad_norm_kernel(Table t, uint32_t chunks,
     const uint64_t at = (uint64_t)(c - t.first[k]) * kNormChunk;
     const uint32_t left = (uint32_t)min(e.n - at, (uint64_t)kNormChunk);
     const G* g = (const G*)e.grad + at;
-    typename Wide<G>::type x[kNormReps];
+    typename Wide<G, VEC>::type x[kNormReps];
 #pragma unroll
     for (int r = 0; r < kNormReps; r++) {
       const uint32_t i = (r * NT + threadIdx.x) * VEC;
       const int rest = i < left ? (int)(left - i) : 0;
-      x[r] = load4v<G>(g + i, aligned && rest >= VEC, rest);
+      x[r] = load_n<VEC, G>(g + i, aligned && rest >= VEC, rest);
     }
 #pragma unroll
     for (int r = 0; r < kNormReps; r++)
@@ -253,54 +262,44 @@ __global__ __launch_bounds__(NT) void grad_norm_kernel(Table t, uint32_t chunks,
         s = __builtin_fma(d, d, s);
       }
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
-  __syncthreads();
-  if (threadIdx.x == 0) part[blockIdx.x] = red[0] + red[1] + red[2] + red[3];
+  s = block_sum(s, red);
+  if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
 __global__ __launch_bounds__(NT) void norm_join_kernel(const double* __restrict__ part, int n, float max_norm, float* __restrict__ out) {
   __shared__ double red[NT / 64];
   double s = 0;
+#pragma unroll 4
   for (int i = threadIdx.x; i < n; i += NT) s += part[i];
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
-  __syncthreads();
+  s = block_sum(s, red);
   if (threadIdx.x == 0) {
-    const float norm = (float)sqrt(red[0] + red[1] + red[2] + red[3]);
+    const float norm = (float)sqrt(s);
     out[0] = norm;
     out[1] = !__builtin_isfinite(norm) ? __builtin_nanf("") : max_norm > 0.f && norm > max_norm ? max_norm / norm : 1.f;
   }
 }
 
 // ---- what 8-bit states stand for
+// 16 codes a lane (half a block's).
+constexpr int kValues = 16, kValueChunk = NT * kValues;
 __global__ __launch_bounds__(NT) void state_values_kernel(Table t, int aligned) {
   const int k = find_tensor(t, blockIdx.x);
   const Entry& e = t.e[k];
-  const uint64_t at = (uint64_t)(blockIdx.x - t.first[k]) * kChunk;
-  const uint32_t left = (uint32_t)min(e.n - at, (uint64_t)kChunk);
-  const uint8_t *m = (const uint8_t*)e.m + at, *v = (const uint8_t*)e.v + at;
-  bf16 *mo = (bf16*)e.param + at, *vo = (bf16*)e.master + at;   // (the table's places for what a step writes)
+  const uint64_t at = (uint64_t)(blockIdx.x - t.first[k]) * kValueChunk + threadIdx.x * kValues;
+  if (at >= e.n) return;
+  const int rest = (int)min(e.n - at, (uint64_t)kValues);
+  const bool whole = aligned && rest == kValues;
+  const auto cm = load_n<kValues, uint8_t>((const uint8_t*)e.m + at, whole, rest), cv = load_n<kValues, uint8_t>((const uint8_t*)e.v + at, whole, rest);
+  const int sm = e.ms[at / kBlock], sv = e.vs[at / kBlock];
+  typename Wide<bf16, kValues>::type om, ov;
 #pragma unroll
-  for (int r = 0; r < kReps; r++) {
-    const uint32_t i = (r * NT + threadIdx.x) * VEC;
-    const int rest = i < left ? (int)(left - i) : 0;
-    const bool whole = aligned && rest >= VEC;
-    if (rest == 0) break;
-    const u8x4 cm = load4v<uint8_t>(m + i, whole, rest), cv = load4v<uint8_t>(v + i, whole, rest);
-    const int sm = e.ms[(at + i) / kBlock], sv = e.vs[(at + i) / kBlock];
-    bf16x4 om, ov;
-#pragma unroll
-    for (int j = 0; j < VEC; j++) {
-      const float x = decode<15>(cm[j] & 127, sm);
-      om[j] = (bf16)(cm[j] & 128 ? -x : x);
-      ov[j] = (bf16)decode<31>(cv[j], sv);
-    }
-    store4v<bf16>(mo + i, om, whole, rest);
-    store4v<bf16>(vo + i, ov, whole, rest);
+  for (int j = 0; j < kValues; j++) {
+    const float x = decode<15>(cm[j] & 127, sm);
+    om[j] = (bf16)(cm[j] & 128 ? -x : x);
+    ov[j] = (bf16)decode<31>(cv[j], sv);
   }
+  store_n<kValues, bf16>((bf16*)e.param + at, om, whole, rest);    // (the table's places for what a step writes)
+  store_n<kValues, bf16>((bf16*)e.master + at, ov, whole, rest);
 }
 
 // Fills tables with the tensors that have elements and calls launch(table, blocks of `chunk` elements) for each.
@@ -319,7 +318,7 @@ hipError_t by_tables(const ah_adamw_tensor_t* x, int n, uint32_t chunk, void* co
   };
   for (int i = 0; i < n; i++) {
     const uint64_t need = (x[i].n + chunk - 1) / chunk;
-    if (count == kTensors || blocks + need > kMaxBlocks) {
+    if (need && (count == kTensors || blocks + need > kMaxBlocks)) {
       const hipError_t e = flush();
       if (e != hipSuccess) return e;
     }
@@ -340,10 +339,11 @@ int norm_launches(int n) { return (n + kTensors - 1) / kTensors + 8; }
 
 inline bool off(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) != 0; }
 
-// Types of a tensor's gradients, parameters and states as bytes an element; vector access needs VEC of them aligned
+// Types of a tensor's gradients, parameters and states as bytes an element; vector access needs n of them aligned, to 16 bytes at most
 struct Widths { int p, g, s; };
-bool vectors(const ah_adamw_tensor_t& x, const Widths& w) {
-  return !(off(x.grad, VEC * w.g) || off(x.param, VEC * w.p) || off(x.m, VEC * w.s) || off(x.v, VEC * w.s) || off(x.master, VEC * 4));
+bool vectors(const ah_adamw_tensor_t& x, const Widths& w, int n) {
+  auto bad = [&](const void* p, int width) { return off(p, std::min(n * width, 16)); };
+  return !(bad(x.grad, w.g) || bad(x.param, w.p) || bad(x.m, w.s) || bad(x.v, w.s) || bad(x.master, 4));
 }
 
 int check_list(const char* who, const ah_adamw_tensor_t* x, int n) {
@@ -378,7 +378,7 @@ extern "C" int ah_adamw_step(const ah_adamw_t* c, const ah_adamw_tensor_t* x, in
     if (any && master != (x[i].master != nullptr)) return set_error(AH_EINVAL, "ah_adamw_step: either all tensors have a master copy or none");
     master = x[i].master != nullptr;
     any = true;
-    aligned = aligned && vectors(x[i], w);
+    aligned = aligned && vectors(x[i], w, bits8 ? VEC8 : VEC);
   }
   if (master && p32) return set_error(AH_EINVAL, "ah_adamw_step: master copies go with bf16 parameters");
   if (!any) return AH_OK;
@@ -391,7 +391,7 @@ extern "C" int ah_adamw_step(const ah_adamw_t* c, const ah_adamw_tensor_t* x, in
     h.root = (float)(1.0 / std::sqrt(-std::expm1((double)c->step * h.log_b2)));
   }
   h.lr_dev = c->lr_dev; h.step_dev = c->step_dev; h.grad_norm = c->grad_norm; h.seed = c->seed; h.aligned = aligned;
-  const hipError_t e = by_tables(x, n, kChunk, nullptr, nullptr, [&](const Table& t, uint32_t blocks) {
+  const hipError_t e = by_tables(x, n, bits8 ? kChunk8 : kChunk, nullptr, nullptr, [&](const Table& t, uint32_t blocks) {
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(NT), 0, (hipStream_t)stream, t, h); };
     auto by_state = [&](auto p, auto g, auto has_master) {
       typedef decltype(p) PT;
@@ -413,7 +413,7 @@ extern "C" int ah_adamw_step(const ah_adamw_t* c, const ah_adamw_tensor_t* x, in
 
 extern "C" int ah_grad_norm_workspace(int n_tensors, uint64_t* bytes) {
   if (!bytes || n_tensors < 0) return set_error(AH_EINVAL, "ah_grad_norm_workspace: bad argument");
-  *bytes = (uint64_t)kNormBlocks * sizeof(double) * (uint64_t)norm_launches(n_tensors);
+  *bytes = sizeof(double) * (uint64_t)kNormBlocks * norm_launches(n_tensors);
   return AH_OK;
 }
 
@@ -456,9 +456,9 @@ extern "C" int ah_adamw_state_values(const ah_adamw_tensor_t* x, int n, void* co
     if (!x[i].n) continue;
     if (!x[i].m || !x[i].v || !x[i].m_scale || !x[i].v_scale || !m_out[i] || !v_out[i]) return set_error(AH_EINVAL, "ah_adamw_state_values: tensor %d has a NULL pointer", i);
     if (off(m_out[i], 2) || off(v_out[i], 2)) return set_error(AH_EINVAL, "ah_adamw_state_values: output %d is misaligned", i);
-    aligned = aligned && !(off(x[i].m, VEC) || off(x[i].v, VEC) || off(m_out[i], VEC * 2) || off(v_out[i], VEC * 2));
+    aligned = aligned && !(off(x[i].m, 16) || off(x[i].v, 16) || off(m_out[i], 16) || off(v_out[i], 16));
   }
-  const hipError_t e = by_tables(x, n, kChunk, m_out, v_out, [&](const Table& t, uint32_t blocks) {
+  const hipError_t e = by_tables(x, n, kValueChunk, m_out, v_out, [&](const Table& t, uint32_t blocks) {
     hipLaunchKernelGGL(state_values_kernel, dim3(blocks), dim3(NT), 0, (hipStream_t)stream, t, (int)aligned);
     return hipGetLastError();
   });
