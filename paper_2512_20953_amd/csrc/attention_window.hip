@@ -22,12 +22,13 @@ namespace {
 struct WinArgs {
   const bf16 *q, *k, *v, *o, *d_o;
   bf16 *out, *dq, *dk, *dv;
-  float *lse, *delta, *part;
+  float *lse, *delta, *part, *far_part;
   const int32_t* offsets;
   size_t ld_q, ld_k, ld_v, ld_o, ld_do, ld_dq, ld_dk, ld_dv;
   int64_t rows;
   int n_seq, S, nh, nkv, rep, W, sinks;
-  int chunks, sink_rows;   // shares of the far queries of the first keys (0: not shared), rows of partial sums
+  int near;                // blocks that share the walk of 128 keys (1: none do)
+  int chunks, far_waves;   // shares of the far queries of the first keys (0: not shared), and into how many the waves of a block share them further
   float sc2, scale;
 };
 
@@ -312,6 +313,15 @@ struct QueryTiles {
   }
 };
 
+// Partial sums [share][key][dk | dv][D] in fp32.  Near the keys: all keys of a sequence, where a small launch shares the walk of a block between
+// several (near > 1).  Far: the first keys, of the blocks that walk the queries behind their window; share 0 is the near walk's where that is not shared.
+__device__ __forceinline__ float* near_part(const WinArgs& a, int bk, int share, int key, int width) {
+  return a.part + (((size_t)bk * a.near + share) * a.S + key) * width;
+}
+__device__ __forceinline__ float* far_part(const WinArgs& a, int bk, int share, int key, int width) {
+  return a.far_part + (((size_t)bk * (1 + a.chunks * a.far_waves) + share) * a.sinks + key) * width;
+}
+
 template <int D>
 __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void win_dkv_kernel(WinArgs a) {
   constexpr int TILEB = 64 * 2 * D, STAGE = 2 * TILEB + 1024, NK = D / 16, ND = D / 32;
@@ -319,26 +329,51 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void win_dkv_kernel(WinArgs a
   const int lane = threadIdx.x & 63, hf = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int nbk = a.n_seq * a.nkv;
-  // the blocks with the queries far behind the first keys come first, then one block per 128 keys
+  // a block (or `near` of them) per 128 keys, and behind them those with the queries far behind the first keys, which are short and fill the last round
   const int rank = blockIdx.x / nbk, bk = blockIdx.x - rank * nbk, b = bk / a.nkv, kvh = bk - b * a.nkv;
-  const int sink_blocks = (a.sinks + 127) / 128, far = rank - sink_blocks * a.chunks;
-  const int kb = far >= 0 ? far : rank % sink_blocks, chunk = far >= 0 ? 0 : 1 + rank / sink_blocks;
+  const int near_blocks = (a.S + 127) / 128 * a.near, sink_blocks = (a.sinks + 127) / 128, far = rank - near_blocks;
+  const int kb = far < 0 ? rank / a.near : far % sink_blocks, chunk = far < 0 ? 0 : 1 + far / sink_blocks, share = far < 0 ? rank % a.near : 0;
   const Seq sq = sequence(a, b);
   const int k0 = kb * 128;
   if (k0 >= sq.len) return;
   const QueryTiles qt(a, k0, sq.len);
-  const bool sink = k0 < a.sinks;
-  int t0 = qt.first, t1 = qt.near;
-  if (sink && a.chunks == 0) t1 = qt.end;
+  int t0 = qt.first, t1 = k0 < a.sinks && a.chunks == 0 ? qt.end : qt.near;
   if (chunk > 0) {
     const int each = (qt.end - qt.near + a.chunks - 1) / a.chunks;
     t0 = min(qt.end, qt.near + (chunk - 1) * each);
     t1 = min(qt.end, t0 + each);
   }
-  const int per_head = t1 - t0, count = per_head * a.rep;
+  // items of the walk: tile t0 + i % per_head of query head i / per_head
+  const int per_head = t1 - t0, all = per_head * a.rep, each = chunk > 0 ? all : (all + a.near - 1) / a.near;
+  const int i0 = share * each, i1 = min(all, i0 + each);
 
-  const int kw0 = k0 + wave * 32, key = kw0 + (lane & 31);
+  // With at most 32 first keys the four waves of a far block take those same keys and every fourth run of 32 queries each, else 32 keys each
+  const bool same_keys = chunk > 0 && a.far_waves > 1;
+  const int pick = same_keys ? 3 : 0, mine = same_keys ? wave : 0;
+  const int kw0 = k0 + (same_keys ? 0 : wave * 32), key = kw0 + (lane & 31);
   const size_t krow = (size_t)(sq.r0 + min(key, sq.len - 1));
+  uint32_t offq[ND], offo[ND];
+#pragma unroll
+  for (int i = 0; i < ND; i++) {
+    offq[i] = tile_src_offset<D>(wave + 4 * i, lane, a.ld_q);
+    offo[i] = tile_src_offset<D>(wave + 4 * i, lane, a.ld_do);
+  }
+  // (head and tile of the next item to load and tile of the one at hand are counted along: a division costs as much as a tenth of a tile)
+  int load_head = kvh * a.rep, load_tile_at = t0 + i0, tile = t0 + i0, fill = 0;
+  if (a.near > 1 && per_head > 0) {
+    load_head += i0 / per_head;
+    tile = load_tile_at = t0 + i0 % per_head;
+  }
+  auto load = [&]() {
+    const int head = load_head, r0 = load_tile_at * 64, left = sq.len - r0;
+    if (++load_tile_at == t1) { load_tile_at = t0; load_head++; }
+    char* slot = ring + fill * STAGE;
+    fill ^= 1;
+    load_tile<D>(a.q + (size_t)(sq.r0 + r0) * a.ld_q + head * D, offq, a.ld_q, left, slot, wave, lane);
+    load_tile<D>(a.d_o + (size_t)(sq.r0 + r0) * a.ld_do + head * D, offo, a.ld_do, left, slot + TILEB, wave, lane);
+    // 64 log-sum-exps, 64 -deltas (waves 2 and 3 repeat them into spare bytes)
+    load4(((wave & 1) ? a.delta : a.lse) + ((size_t)b * a.nh + head) * a.S + r0, (uint32_t)min(lane, left - 1) * 4u, slot + 2 * TILEB + wave * 256);
+  };
   bf16x8 kf[NK], vf[NK];
   f32x16 dk[ND], dv[ND];
 #pragma unroll
@@ -350,34 +385,24 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void win_dkv_kernel(WinArgs a
   for (int dt = 0; dt < ND; dt++)
 #pragma unroll
     for (int r = 0; r < 16; r++) { dk[dt][r] = 0.f; dv[dt][r] = 0.f; }
-  uint32_t offq[ND], offo[ND];
-#pragma unroll
-  for (int i = 0; i < ND; i++) {
-    offq[i] = tile_src_offset<D>(wave + 4 * i, lane, a.ld_q);
-    offo[i] = tile_src_offset<D>(wave + 4 * i, lane, a.ld_do);
-  }
-  auto load = [&](int i) {
-    const int h = i / per_head, head = kvh * a.rep + h, r0 = (t0 + i - h * per_head) * 64, left = sq.len - r0;
-    char* slot = ring + (i & 1) * STAGE;
-    load_tile<D>(a.q + (size_t)(sq.r0 + r0) * a.ld_q + head * D, offq, a.ld_q, left, slot, wave, lane);
-    load_tile<D>(a.d_o + (size_t)(sq.r0 + r0) * a.ld_do + head * D, offo, a.ld_do, left, slot + TILEB, wave, lane);
-    // 64 log-sum-exps, 64 -deltas (waves 2 and 3 repeat them into spare bytes)
-    load4(((wave & 1) ? a.delta : a.lse) + ((size_t)b * a.nh + head) * a.S + r0, (uint32_t)min(lane, left - 1) * 4u, slot + 2 * TILEB + wave * 256);
-  };
-  if (count > 0) {
-    load(0);
+  if (i0 < i1) {
+    load();
     AH_NEXT_TILE();
   }
-  for (int i = 0; i < count; i++) {
-    if (i + 1 < count) load(i + 1);
-    const char *cQ = ring + (i & 1) * STAGE, *cO = cQ + TILEB;
+  int at = 0;
+  for (int i = i0; i < i1; i++) {
+    if (i + 1 < i1) load();
+    const char *cQ = ring + at * STAGE, *cO = cQ + TILEB;
+    at ^= 1;
     const float* stat = (const float*)(cQ + 2 * TILEB);
-    const int r0 = (t0 + i % per_head) * 64;
+    const int r0 = tile * 64;
+    if (++tile == t1) tile = t0;
 #pragma unroll
     for (int t = 0; t < 64; t += 32) {
       const int qw0 = r0 + t;   // 32 queries against the wave's 32 keys
+      if (((2 * i + t / 32) & pick) != mine) continue;
       if (kw0 > qw0 + 31 || qw0 >= sq.len || (qw0 - (kw0 + 31) >= a.W && kw0 >= a.sinks)) continue;
-      const bool all = kw0 + 31 <= qw0 && qw0 + 32 <= sq.len && (qw0 + 31 - kw0 < a.W || kw0 + 32 <= a.sinks);
+      const bool every = kw0 + 31 <= qw0 && qw0 + 32 <= sq.len && (qw0 + 31 - kw0 < a.W || kw0 + 32 <= a.sinks);
       f32x16 s, dp;
 #pragma unroll
       for (int r = 0; r < 16; r++) { s[r] = 0.f; dp[r] = stat[64 + t + 4 * hf + 8 * (r >> 2) + (r & 3)]; }
@@ -388,7 +413,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void win_dkv_kernel(WinArgs a
       }
 #pragma unroll
       for (int r = 0; r < 16; r++) s[r] = fexp2(__builtin_fmaf(s[r], a.sc2, -stat[t + 4 * hf + 8 * (r >> 2) + (r & 3)] * LOG2E));
-      if (!all) {
+      if (!every) {
         // query qw0 + 4 hf + c sees the lane's key iff lo <= c <= hi
         const int lo = key - qw0 - 4 * hf, end = sq.len - 1 - qw0 - 4 * hf, hi = key < a.sinks ? end : min(end, lo + a.W - 1);
 #pragma unroll
@@ -413,9 +438,13 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void win_dkv_kernel(WinArgs a
   }
   const int rows = sq.len - kw0;
   if (rows <= 0) return;
-  if (a.chunks > 0 && kw0 < a.sinks) {   // the lane's key and half of its columns, element by element (a few rows)
-    if (key < a.sinks && key < sq.len) {
-      float* p = a.part + (((size_t)bk * (1 + a.chunks) + chunk) * a.sink_rows + key) * (2 * D);
+  const bool far_sums = a.chunks > 0 && kw0 < a.sinks;
+  if (far_sums || a.near > 1) {   // the lane's key and half of its columns
+    const bool kept = key < sq.len && (a.near > 1 || key < a.sinks);
+    float* p = nullptr;
+    if (chunk > 0) p = key < a.sinks ? far_part(a, bk, 1 + (chunk - 1) * a.far_waves + (same_keys ? wave : 0), key, 2 * D) : nullptr;
+    else p = a.near > 1 ? near_part(a, bk, share, key, 2 * D) : far_part(a, bk, 0, key, 2 * D);
+    if (kept && p) {
 #pragma unroll
       for (int dt = 0; dt < ND; dt++)
 #pragma unroll
@@ -426,43 +455,72 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void win_dkv_kernel(WinArgs a
         }
     }
   }
-  if (chunk > 0) return;
+  if (chunk > 0 || a.near > 1) return;
   // (first keys whose sums are shared are written here too, and again by the kernel that adds the shares up)
   char* strip = ring + wave * strip_bytes<D>();
   store_rows_to<D>([&](int dt, int r) { return dk[dt][r] * a.scale; }, strip, a.dk + (size_t)(sq.r0 + kw0) * a.ld_dk + kvh * D, a.ld_dk, rows, lane);
   store_rows_to<D>([&](int dt, int r) { return dv[dt][r]; }, strip, a.dv + (size_t)(sq.r0 + kw0) * a.ld_dv + kvh * D, a.ld_dv, rows, lane);
 }
 
-// dK and dV of the first keys from the shares, in their order.  A thread per (key, column).
+// dK and dV from the shares, in their order: of all keys where the near walks were shared, else of the first ones.  A thread takes four columns of a key.
+constexpr int JOIN_KEYS = 4;
 template <int D>
-__global__ __launch_bounds__(2 * D) void win_join_kernel(WinArgs a) {
-  const int key = blockIdx.x, bk = blockIdx.y, b = bk / a.nkv, kvh = bk - b * a.nkv;
+__global__ __launch_bounds__(JOIN_KEYS * D / 2) void win_join_kernel(WinArgs a) {
+  const int key = blockIdx.x * JOIN_KEYS + threadIdx.x / (D / 2), c = threadIdx.x % (D / 2) * 4, bk = blockIdx.y, b = bk / a.nkv, kvh = bk - b * a.nkv;
   const Seq sq = sequence(a, b);
-  if (key >= sq.len) return;
-  const float* p = a.part + ((size_t)bk * (1 + a.chunks) * a.sink_rows + key) * (2 * D) + threadIdx.x;
-  float s = 0.f;
-  for (int c = 0; c <= a.chunks; c++) s += p[(size_t)c * a.sink_rows * (2 * D)];
+  if (key >= sq.len || (a.near == 1 && key >= a.sinks)) return;
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  if (a.near > 1) {
+#pragma unroll 4
+    for (int i = 0; i < a.near; i++) s += *(const f32x4*)(near_part(a, bk, i, key, 2 * D) + c);
+  }
+  if (a.chunks > 0 && key < a.sinks) {
+#pragma unroll 4
+    for (int i = a.near > 1; i <= a.chunks * a.far_waves; i++) s += *(const f32x4*)(far_part(a, bk, i, key, 2 * D) + c);
+  }
   const size_t row = sq.r0 + key;
-  if (threadIdx.x < D) a.dk[row * a.ld_dk + kvh * D + threadIdx.x] = f2bf(s * a.scale);
-  else a.dv[row * a.ld_dv + kvh * D + threadIdx.x - D] = f2bf(s);
+  bf16x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; i++) v[i] = f2bf(c < D ? s[i] * a.scale : s[i]);
+  if (c < D) *(bf16x4*)(a.dk + row * a.ld_dk + kvh * D + c) = v;
+  else *(bf16x4*)(a.dv + row * a.ld_dv + kvh * D + c - D) = v;
 }
 
 // ---------------------------------------------------------------------------------------- host
 inline bool off16(const void* p) { return ((uintptr_t)p & 15) != 0; }
 
+int far_waves(const ah_attention_window_t* c) { return c->sinks <= 32 ? 4 : 1; }
+
 // Shares of the queries behind the window of the first keys: none where no position lies there, or where the blocks of the first keys fill the
-// chip by themselves; else as many as make a share about as long as an ordinary block's walk.
+// chip by themselves; else as many as make a share about as long as an
+// ordinary block's walk, or a quarter of it where the waves of a block split the queries further.  (Whole backward, us, with 2, 4 and 8 shares and by this
+// rule: 1 x 4096 x 32 heads in groups of four x 64, window 512, 202, 146, 129, 117; 1 x 8192 x 32 in groups of four x 128, window 1024, 832, 664, 650, 619; 1 x 4096 x
+// 32 x 128, window 1024, 321, 310, 311, 313.)
 int far_chunks(const ah_attention_window_t* c) {
   const long blocks = (long)c->n_seq * c->n_kv_heads * ((std::min(c->sinks, c->seq_len) + 127) / 128);
   const long far = ((long)c->seq_len - c->window) / 64, usual = (128 + std::min(c->window, c->seq_len)) / 64 + 1;
   if (c->sinks == 0 || far <= usual / 2 || blocks >= 512) return 0;
-  return (int)std::min(8L, std::max(1L, (far + usual - 1) / usual));
+  return far_waves(c) > 1 ? (int)std::min(32L, (4 * far + usual - 1) / usual) : (int)std::min(8L, (far + usual - 1) / usual);
+}
+
+// Blocks that share the walk of 128 keys: as many as bring a launch that leaves CUs idle to one block (two of 64-wide heads) each, with two tiles at least for
+// each of them
+int near_shares(const ah_attention_window_t* c) {
+  const long blocks = (long)c->n_seq * c->n_kv_heads * ((c->seq_len + 127) / 128), want = c->head_dim == 64 ? 512 : 256;
+  const long tiles = ((128L + std::min(c->window, c->seq_len) - 1) / 64 + 1) * (c->n_heads / c->n_kv_heads);
+  return (int)std::max(1L, std::min({want / blocks, tiles / 2, 8L}));
 }
 
 size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 
-size_t part_bytes(const ah_attention_window_t* c) {
-  return (size_t)c->n_seq * c->n_kv_heads * (1 + far_chunks(c)) * std::min(c->sinks, c->seq_len) * 2 * c->head_dim * sizeof(float);
+// partial sums: near the keys, and of the far queries of the first ones
+size_t near_bytes(const ah_attention_window_t* c) {
+  const int n = near_shares(c);
+  return n > 1 ? (size_t)c->n_seq * c->n_kv_heads * n * c->seq_len * 2 * c->head_dim * sizeof(float) : 0;
+}
+size_t far_bytes(const ah_attention_window_t* c) {
+  const int n = far_chunks(c);
+  return n > 0 ? (size_t)c->n_seq * c->n_kv_heads * (1 + n * far_waves(c)) * std::min(c->sinks, c->seq_len) * 2 * c->head_dim * sizeof(float) : 0;
 }
 size_t delta_bytes(const ah_attention_window_t* c) { return align256((size_t)c->n_seq * c->n_heads * c->seq_len * sizeof(float)); }
 
@@ -526,7 +584,7 @@ extern "C" int ah_attention_window_fwd(const ah_attention_window_t* c, const voi
 extern "C" int ah_attention_window_bwd_workspace(const ah_attention_window_t* c, uint64_t* bytes) {
   if (!bytes) return set_error(AH_EINVAL, "ah_attention_window_bwd_workspace: bytes is NULL");
   if (int rc = check_sizes("ah_attention_window_bwd_workspace", c)) return rc;
-  *bytes = delta_bytes(c) + (far_chunks(c) ? part_bytes(c) : 0);
+  *bytes = delta_bytes(c) + near_bytes(c) + far_bytes(c);
   return AH_OK;
 }
 
@@ -542,19 +600,23 @@ extern "C" int ah_attention_window_bwd(const ah_attention_window_t* c, const voi
   a.dq = (bf16*)dq; a.dk = (bf16*)dk; a.dv = (bf16*)dv;
   a.delta = (float*)workspace;
   a.chunks = far_chunks(c);
-  a.sink_rows = a.sinks;
+  a.far_waves = far_waves(c);
+  a.near = near_shares(c);
   a.part = (float*)((char*)workspace + delta_bytes(c));
+  a.far_part = (float*)((char*)a.part + near_bytes(c));
   const int key_blocks = (a.S + 127) / 128, sink_blocks = (a.sinks + 127) / 128;
-  const dim3 gq((unsigned)(a.n_seq * a.nh * key_blocks)), gk((unsigned)(a.n_seq * a.nkv * (key_blocks + sink_blocks * a.chunks)));
+  const dim3 gq((unsigned)(a.n_seq * a.nh * key_blocks)), gk((unsigned)(a.n_seq * a.nkv * (key_blocks * a.near + sink_blocks * a.chunks)));
+  const dim3 gj((unsigned)(((a.near > 1 ? a.S : a.sinks) + JOIN_KEYS - 1) / JOIN_KEYS), (unsigned)(a.n_seq * a.nkv));
+  const bool join = a.near > 1 || a.chunks > 0;   // (both only where n_seq * nkv is below 512)
   const hipStream_t s = (hipStream_t)stream;
   if (c->head_dim == 128) {
     hipLaunchKernelGGL(win_dq_kernel<128>, gq, dim3(256), 0, s, a);
     hipLaunchKernelGGL(win_dkv_kernel<128>, gk, dim3(256), 0, s, a);
-    if (a.chunks) hipLaunchKernelGGL(win_join_kernel<128>, dim3(a.sinks, a.n_seq * a.nkv), dim3(256), 0, s, a);
+    if (join) hipLaunchKernelGGL(win_join_kernel<128>, gj, dim3(JOIN_KEYS * 64), 0, s, a);
   } else {
     hipLaunchKernelGGL(win_dq_kernel<64>, gq, dim3(256), 0, s, a);
     hipLaunchKernelGGL(win_dkv_kernel<64>, gk, dim3(256), 0, s, a);
-    if (a.chunks) hipLaunchKernelGGL(win_join_kernel<64>, dim3(a.sinks, a.n_seq * a.nkv), dim3(128), 0, s, a);
+    if (join) hipLaunchKernelGGL(win_join_kernel<64>, gj, dim3(JOIN_KEYS * 32), 0, s, a);
   }
   return hip_status(hipGetLastError(), "ah_attention_window_bwd");
 }
