@@ -73,7 +73,9 @@ typedef enum {
  * WQKV columns are [Q | K | V], each block head-major. */
 typedef enum {
   AH_P_LN1_G = 0, AH_P_LN1_B, AH_P_WQKV, AH_P_BQKV, AH_P_WO, AH_P_BO,
-  AH_P_LN2_G, AH_P_LN2_B, AH_P_W1, AH_P_B1, AH_P_W2, AH_P_B2, AH_P_COUNT
+  AH_P_LN2_G, AH_P_LN2_B, AH_P_W1, AH_P_B1, AH_P_W2, AH_P_B2,
+  AH_P_QN_G, AH_P_KN_G,   /* with qk_norm: gains [head_dim] of the query and of the key heads' norms, behind the layer's other tensors (128 elements each) */
+  AH_P_COUNT
 } ah_param_t;
 
 typedef struct {
@@ -108,6 +110,11 @@ typedef struct {
                              * boundary stay bf16): each layer then adds its two blocks to an unrounded sum, which removes the
                              * largest single source of forward error of a deep stage (the error of a stage of l_i layers,
                              * Section III-C Eq. 4, grows with l_i) at the cost of 4*T*hidden more bytes per saved layer. */
+  /* Fields from here on may be left out: a struct_size that ends before attn_window is taken as all three 0. */
+  int32_t attn_window;      /* 0: a query attends to all earlier positions.  >= 1 (GPT, LLaMA): to the last attn_window ones, its own among them ... */
+  int32_t attn_sinks;       /* ... and to the first attn_sinks of its sequence (ah_attention_window_fwd in ah_ops.h); needs attn_window */
+  int32_t qk_norm;          /* 1: every query and key head is normed (RMS, norm_eps, gains AH_P_QN_G / AH_P_KN_G) before the attention, and before the
+                             * rotary embedding where there is one (ah_qk_norm_rope_fwd in ah_ops.h); 4*T*(local attention width) more bytes per saved layer. */
 } ah_stage_config_t;
 
 typedef struct {

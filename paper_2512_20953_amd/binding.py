@@ -13,7 +13,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 AH_ARCH_GPT, AH_ARCH_LLAMA, AH_ARCH_BERT = 0, 1, 2
 _ARCH = {"gpt": AH_ARCH_GPT, "llama": AH_ARCH_LLAMA, "bert": AH_ARCH_BERT}
 PARAM_INDEX = {"ln1_g": 0, "ln1_b": 1, "wqkv": 2, "bqkv": 3, "wo": 4, "bo": 5,
-               "ln2_g": 6, "ln2_b": 7, "w1": 8, "b1": 9, "w2": 10, "b2": 11}
+               "ln2_g": 6, "ln2_b": 7, "w1": 8, "b1": 9, "w2": 10, "b2": 11, "qn_g": 12, "kn_g": 13}
 # names the layer's tensors go by elsewhere (LLaMA: fused gate|up and down)
 PARAM_ALIASES = {"wgu": "w1", "wd": "w2"}
 
@@ -29,13 +29,16 @@ class StageConfig(C.Structure):
                 ("n_heads", C.c_int32), ("head_dim", C.c_int32), ("ffn_hidden", C.c_int32), ("tp_degree", C.c_int32),
                 ("tp_rank", C.c_int32), ("seq_len", C.c_int32), ("microbatch_size", C.c_int32),
                 ("n_microbatches", C.c_int32), ("max_in_flight", C.c_int32), ("recompute", C.c_int32),
-                ("wgrad_group", C.c_int32), ("norm_eps", C.c_float), ("rope_base", C.c_float), ("residual_fp32", C.c_int32)]
+                ("wgrad_group", C.c_int32), ("norm_eps", C.c_float), ("rope_base", C.c_float), ("residual_fp32", C.c_int32),
+                ("attn_window", C.c_int32), ("attn_sinks", C.c_int32), ("qk_norm", C.c_int32)]
 
     @classmethod
     def make(cls, arch="gpt", n_layers=1, hidden=256, n_heads=4, head_dim=64, ffn=1024, tp=1, tp_rank=0, seq=128, mb=1,
-             n_mb=1, max_in_flight=1, recompute=0, wgrad_group=0, norm_eps=0.0, rope_base=0.0, residual_fp32=0):
+             n_mb=1, max_in_flight=1, recompute=0, wgrad_group=0, norm_eps=0.0, rope_base=0.0, residual_fp32=0,
+             attn_window=0, attn_sinks=0, qk_norm=0):
         return cls(C.sizeof(cls), _ARCH[arch], n_layers, hidden, n_heads, head_dim,
-                   ffn, tp, tp_rank, seq, mb, n_mb, max_in_flight, recompute, wgrad_group, norm_eps, rope_base, residual_fp32)
+                   ffn, tp, tp_rank, seq, mb, n_mb, max_in_flight, recompute, wgrad_group, norm_eps, rope_base, residual_fp32,
+                   attn_window, attn_sinks, qk_norm)
 
 
 class _Sizes(C.Structure):
@@ -242,6 +245,20 @@ class Stage:
         n = C.c_int()
         _check(lib.ah_stage_backward_streams(self._h, C.byref(n)))
         return n.value
+
+    def adamw(self, weight_decay=0.1, **options):
+        """An AdamW over the stage's parameters and gradients (state_bits, master, betas, eps as there); weight_decay acts on the matrices, not on
+        biases, gains and offsets.  Its step goes behind the last backward (or flush_grads) of an iteration, on the same stream."""
+        params, grads, decay = [], [], []
+        for layer in range(self.cfg.n_layers):
+            for which in PARAM_INDEX.values():
+                off, r, c = C.c_uint64(), C.c_int32(), C.c_int32()
+                if lib.ah_stage_param_layout(self._h, layer, which, C.byref(off), C.byref(r), C.byref(c)) == 0:    # (not every architecture has each)
+                    at = slice(off.value, off.value + r.value * c.value)
+                    params.append(self.params[at])
+                    grads.append(self.grads[at])
+                    decay.append(weight_decay if r.value > 1 else 0.0)
+        return AdamW(params, grads, weight_decay=decay, **options)
 
     def grads_ptr(self):
         p, n = C.c_void_p(), C.c_uint64()

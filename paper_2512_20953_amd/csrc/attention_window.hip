@@ -11,6 +11,7 @@
 #include "ah_ops.h"
 #include "attention_tile.h"
 #include "capi_util.h"
+#include "kernels.h"
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
@@ -565,7 +566,80 @@ WinArgs args(const ah_attention_window_t* c, const void* q, const void* k, const
   return a;
 }
 
+hipError_t run_fwd(const WinArgs& a, int d, hipStream_t s) {
+  const dim3 grid((unsigned)(a.n_seq * a.nh * ((a.S + 127) / 128)));
+  if (d == 128) hipLaunchKernelGGL(win_fwd_kernel<128>, grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(win_fwd_kernel<64>, grid, dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+size_t bwd_bytes(const ah_attention_window_t* c) { return delta_bytes(c) + near_bytes(c) + far_bytes(c); }
+
+hipError_t run_bwd(WinArgs a, const ah_attention_window_t* c, void* workspace, hipStream_t s) {
+  a.delta = (float*)workspace;
+  a.chunks = far_chunks(c);
+  a.far_waves = far_waves(c);
+  a.near = near_shares(c);
+  a.part = (float*)((char*)workspace + delta_bytes(c));
+  a.far_part = (float*)((char*)a.part + near_bytes(c));
+  const int key_blocks = (a.S + 127) / 128, sink_blocks = (a.sinks + 127) / 128;
+  const dim3 gq((unsigned)(a.n_seq * a.nh * key_blocks)), gk((unsigned)(a.n_seq * a.nkv * (key_blocks * a.near + sink_blocks * a.chunks)));
+  const dim3 gj((unsigned)(((a.near > 1 ? a.S : a.sinks) + JOIN_KEYS - 1) / JOIN_KEYS), (unsigned)(a.n_seq * a.nkv));
+  const bool join = a.near > 1 || a.chunks > 0;   // (both only where n_seq * nkv is below 512)
+  if (c->head_dim == 128) {
+    hipLaunchKernelGGL(win_dq_kernel<128>, gq, dim3(256), 0, s, a);
+    hipLaunchKernelGGL(win_dkv_kernel<128>, gk, dim3(256), 0, s, a);
+    if (join) hipLaunchKernelGGL(win_join_kernel<128>, gj, dim3(JOIN_KEYS * 64), 0, s, a);
+  } else {
+    hipLaunchKernelGGL(win_dq_kernel<64>, gq, dim3(256), 0, s, a);
+    hipLaunchKernelGGL(win_dkv_kernel<64>, gk, dim3(256), 0, s, a);
+    if (join) hipLaunchKernelGGL(win_join_kernel<64>, gj, dim3(JOIN_KEYS * 32), 0, s, a);
+  }
+  return hipGetLastError();
+}
+
+// a stage's configuration: B sequences of S rows in a packed projection
+ah_attention_window_t stage_config(int B, int S, int nh, int d, int window, int sinks) {
+  ah_attention_window_t c = {};
+  c.struct_size = sizeof c;
+  c.n_seq = B; c.seq_len = S; c.n_heads = nh; c.n_kv_heads = nh; c.head_dim = d; c.window = window; c.sinks = sinks;
+  c.ld_q = c.ld_k = c.ld_v = c.ld_dq = c.ld_dk = c.ld_dv = 3 * nh * d;
+  return c;
+}
+WinArgs stage_args(const ah_attention_window_t& c, const void* qkv, float* lse) {
+  const size_t w = (size_t)c.n_heads * c.head_dim;
+  WinArgs a = args(&c, qkv, (const bf16*)qkv + w, (const bf16*)qkv + 2 * w);
+  a.lse = lse;
+  return a;
+}
+
 }  // namespace
+
+namespace ah {
+
+hipError_t launch_attention_window_fwd(const void* qkv, void* o, float* lse, int B, int S, int nh, int d, int window, int sinks, hipStream_t s) {
+  const ah_attention_window_t c = stage_config(B, S, nh, d, window, sinks);
+  WinArgs a = stage_args(c, qkv, lse);
+  a.out = (bf16*)o;
+  return run_fwd(a, d, s);
+}
+
+hipError_t launch_attention_window_bwd(const void* qkv, const void* o, const float* lse, const void* d_o, void* dqkv, void* work, int B, int S, int nh, int d,
+                                       int window, int sinks, hipStream_t s) {
+  const ah_attention_window_t c = stage_config(B, S, nh, d, window, sinks);
+  WinArgs a = stage_args(c, qkv, (float*)lse);
+  const size_t w = (size_t)nh * d;
+  a.o = (const bf16*)o; a.d_o = (const bf16*)d_o;
+  a.dq = (bf16*)dqkv; a.dk = a.dq + w; a.dv = a.dq + 2 * w;
+  return run_bwd(a, &c, work, s);
+}
+
+size_t attention_window_bwd_bytes(int B, int S, int nh, int d, int window, int sinks) {
+  const ah_attention_window_t c = stage_config(B, S, nh, d, window, sinks);
+  return bwd_bytes(&c);
+}
+
+}  // namespace ah
 
 extern "C" int ah_attention_window_fwd(const ah_attention_window_t* c, const void* q, const void* k, const void* v, void* o, float* lse, void* stream) {
   discard_stale_hip_error();
@@ -575,16 +649,13 @@ extern "C" int ah_attention_window_fwd(const ah_attention_window_t* c, const voi
   WinArgs a = args(c, q, k, v);
   a.out = (bf16*)o;
   a.lse = lse;
-  const dim3 grid((unsigned)(a.n_seq * a.nh * ((a.S + 127) / 128)));
-  if (c->head_dim == 128) hipLaunchKernelGGL(win_fwd_kernel<128>, grid, dim3(256), 0, (hipStream_t)stream, a);
-  else hipLaunchKernelGGL(win_fwd_kernel<64>, grid, dim3(256), 0, (hipStream_t)stream, a);
-  return hip_status(hipGetLastError(), "ah_attention_window_fwd");
+  return hip_status(run_fwd(a, c->head_dim, (hipStream_t)stream), "ah_attention_window_fwd");
 }
 
 extern "C" int ah_attention_window_bwd_workspace(const ah_attention_window_t* c, uint64_t* bytes) {
   if (!bytes) return set_error(AH_EINVAL, "ah_attention_window_bwd_workspace: bytes is NULL");
   if (int rc = check_sizes("ah_attention_window_bwd_workspace", c)) return rc;
-  *bytes = delta_bytes(c) + near_bytes(c) + far_bytes(c);
+  *bytes = bwd_bytes(c);
   return AH_OK;
 }
 
@@ -598,25 +669,5 @@ extern "C" int ah_attention_window_bwd(const ah_attention_window_t* c, const voi
   WinArgs a = args(c, q, k, v);
   a.o = (const bf16*)o; a.d_o = (const bf16*)d_o; a.lse = (float*)lse;
   a.dq = (bf16*)dq; a.dk = (bf16*)dk; a.dv = (bf16*)dv;
-  a.delta = (float*)workspace;
-  a.chunks = far_chunks(c);
-  a.far_waves = far_waves(c);
-  a.near = near_shares(c);
-  a.part = (float*)((char*)workspace + delta_bytes(c));
-  a.far_part = (float*)((char*)a.part + near_bytes(c));
-  const int key_blocks = (a.S + 127) / 128, sink_blocks = (a.sinks + 127) / 128;
-  const dim3 gq((unsigned)(a.n_seq * a.nh * key_blocks)), gk((unsigned)(a.n_seq * a.nkv * (key_blocks * a.near + sink_blocks * a.chunks)));
-  const dim3 gj((unsigned)(((a.near > 1 ? a.S : a.sinks) + JOIN_KEYS - 1) / JOIN_KEYS), (unsigned)(a.n_seq * a.nkv));
-  const bool join = a.near > 1 || a.chunks > 0;   // (both only where n_seq * nkv is below 512)
-  const hipStream_t s = (hipStream_t)stream;
-  if (c->head_dim == 128) {
-    hipLaunchKernelGGL(win_dq_kernel<128>, gq, dim3(256), 0, s, a);
-    hipLaunchKernelGGL(win_dkv_kernel<128>, gk, dim3(256), 0, s, a);
-    if (join) hipLaunchKernelGGL(win_join_kernel<128>, gj, dim3(JOIN_KEYS * 64), 0, s, a);
-  } else {
-    hipLaunchKernelGGL(win_dq_kernel<64>, gq, dim3(256), 0, s, a);
-    hipLaunchKernelGGL(win_dkv_kernel<64>, gk, dim3(256), 0, s, a);
-    if (join) hipLaunchKernelGGL(win_join_kernel<64>, gj, dim3(JOIN_KEYS * 32), 0, s, a);
-  }
-  return hip_status(hipGetLastError(), "ah_attention_window_bwd");
+  return hip_status(run_bwd(a, c, workspace, (hipStream_t)stream), "ah_attention_window_bwd");
 }

@@ -91,6 +91,20 @@ hipError_t launch_attention_fwd(const void* qkv, void* o, float* lse, int B, int
 hipError_t launch_attention_bwd(const void* qkv, const void* o, const float* lse, const void* d_o, void* dqkv,
                                 float* delta, int B, int S, int nh, int d, bool causal, hipStream_t s);
 
+// The same over a sliding window of `window` positions with `sinks` visible first ones, on a packed qkv; any S.  work: attention_window_bwd_bytes(...), 256-byte aligned
+hipError_t launch_attention_window_fwd(const void* qkv, void* o, float* lse, int B, int S, int nh, int d, int window, int sinks, hipStream_t s);
+hipError_t launch_attention_window_bwd(const void* qkv, const void* o, const float* lse, const void* d_o, void* dqkv, void* work, int B, int S, int nh, int d,
+                                       int window, int sinks, hipStream_t s);
+size_t attention_window_bwd_bytes(int B, int S, int nh, int d, int window, int sinks);
+
+// ---- RMS norm and rotation of nh query heads and as many key heads in the first columns of rows x (ld_x columns apart) to y; cos_sin NULL: no rotation
+hipError_t launch_qk_norm_fwd(const void* x, int ld_x, const void* gain_q, const void* gain_k, const float* cos_sin, void* y, int ld_y, int T, int S, int nh, int d,
+                              float eps, hipStream_t s);
+// dy becomes dx in place; partial sums of the gains' gradients to part[2][qk_norm_bwd_blocks][d] (query gain, key gain), written or (acc) added to what is there
+hipError_t launch_qk_norm_bwd(const void* x, int ld_x, const void* gain_q, const void* gain_k, const float* cos_sin, void* dy, int ld_y, float* part, int acc, int T, int S,
+                              int nh, int d, float eps, hipStream_t s);
+int qk_norm_bwd_blocks(int T, int nh, int d);
+
 // ---- row-wise / element-wise kernels (bf16 I/O, fp32 math) ----
 // a = norm(x) * gamma (+ beta); stats[2*T] = (mean, rstd) per row (RMS: mean slot unused = 0)
 // x_f32: x is fp32 (the residual stream kept in fp32) instead of bf16
@@ -110,7 +124,7 @@ hipError_t launch_norm_bwd(bool rms, const void* da, const void* x, const float*
 int norm_bwd_blocks(int T);
 // g[c] = beta * g[c] + sum_b part[b][c] for the vectors of a list (n a multiple of 64), in one launch
 struct FoldList {
-  static constexpr int kMax = 8;   // a layer's vector gradients
+  static constexpr int kMax = 10;   // a layer's vector gradients
   const float* part[kMax];
   float* g[kMax];
   int n[kMax], nblk[kMax], first[kMax + 1], count;   // first: block of the launch at which a vector begins
@@ -129,6 +143,8 @@ struct FoldList {
 };
 hipError_t launch_fold(const FoldList& a, int beta, hipStream_t s);
 // rotary embedding in place on the Q and K blocks of qkv[T, 3*nh*d]; sign = +1 forward, -1 backward
+// cos_sin[pos][i] = (cos, sin)(pos base^(-2 i / d)) for pos < S, in fp64 rounded to fp32
+hipError_t launch_rope_table(float* cos_sin, int S, int d, double base, hipStream_t s);
 hipError_t launch_rope(void* qkv, const float* cos_sin, int T, int S, int nh, int d, float sign, hipStream_t s);
 // device-to-device copy of a multiple of 16 bytes
 hipError_t launch_copy(void* dst, const void* src, size_t bytes, hipStream_t s);

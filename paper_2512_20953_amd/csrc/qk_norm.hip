@@ -30,6 +30,7 @@ struct QkArgs {
   int T, S, nh, heads, n_pos;
   int slots;                 // heads side by side in a wave (a power of two), of (1024 / d) / slots tokens
   int passes;                // heads of a lane: ceil(heads / slots)
+  int acc;                   // partial sums are added to what is there
   float eps;
 };
 
@@ -207,17 +208,9 @@ __global__ __launch_bounds__(NT) void qk_norm_bwd_kernel(QkArgs a) {
     float s = red[0][which][c];
 #pragma unroll
     for (int w = 1; w < NW; w++) s += red[w][which][c];
-    a.part[((size_t)which * gridDim.x + blockIdx.x) * D + c] = s;
+    float* to = a.part + ((size_t)which * gridDim.x + blockIdx.x) * D + c;
+    *to = a.acc ? *to + s : s;
   }
-}
-
-__global__ void table_kernel(float* cs, int n, int half, int d, double log_base) {
-  const size_t idx = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
-  if (idx >= (size_t)n * half) return;
-  const int pos = (int)(idx / half), i = (int)(idx % half);
-  const double ang = pos * exp(-(2.0 * i / d) * log_base);
-  cs[2 * idx] = (float)cos(ang);
-  cs[2 * idx + 1] = (float)sin(ang);
 }
 
 inline bool off16(const void* p) { return ((uintptr_t)p & 15) != 0; }
@@ -264,16 +257,63 @@ int bwd_blocks(const ah_qk_norm_rope_t* c) {
   return std::max(1, std::min(kBwdBlocks, (c->rows + per_block - 1) / per_block));
 }
 
+hipError_t run_fwd(const QkArgs& a, int d, hipStream_t s) {
+  const int tokens = NW * (1024 / d / a.slots);
+  const dim3 grid((a.T + tokens - 1) / tokens, (a.passes + kFwdPasses - 1) / kFwdPasses);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(NT), 0, s, a); };
+  if (d == 128) { if (a.cs) go(qk_norm_fwd_kernel<128, true>); else go(qk_norm_fwd_kernel<128, false>); }
+  else { if (a.cs) go(qk_norm_fwd_kernel<64, true>); else go(qk_norm_fwd_kernel<64, false>); }
+  return hipGetLastError();
+}
+
+hipError_t run_bwd(const QkArgs& a, int d, int blocks, hipStream_t s) {
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(NT), 0, s, a); };
+  if (d == 128) { if (a.cs) go(qk_norm_bwd_kernel<128, true>); else go(qk_norm_bwd_kernel<128, false>); }
+  else { if (a.cs) go(qk_norm_bwd_kernel<64, true>); else go(qk_norm_bwd_kernel<64, false>); }
+  return hipGetLastError();
+}
+
+// a stage's configuration: as many key heads as query heads, a table of S positions
+ah_qk_norm_rope_t stage_config(int ld_x, const void* gain_q, const void* gain_k, const float* cos_sin, int ld_y, int T, int S, int nh, int d, float eps) {
+  ah_qk_norm_rope_t c = {};
+  c.struct_size = sizeof c;
+  c.rows = T; c.seq_len = S; c.n_heads = nh; c.n_kv_heads = nh; c.head_dim = d; c.n_pos = S; c.eps = eps;
+  c.ld_x = ld_x; c.ld_y = ld_y; c.ld_dx = ld_y;
+  c.gain_q = gain_q; c.gain_k = gain_k; c.cos_sin = cos_sin;
+  return c;
+}
+
 }  // namespace
+
+namespace ah {
+
+hipError_t launch_qk_norm_fwd(const void* x, int ld_x, const void* gain_q, const void* gain_k, const float* cos_sin, void* y, int ld_y, int T, int S, int nh, int d,
+                              float eps, hipStream_t s) {
+  const ah_qk_norm_rope_t c = stage_config(ld_x, gain_q, gain_k, cos_sin, ld_y, T, S, nh, d, eps);
+  return run_fwd(args(&c, x, nullptr, y, ld_y, nullptr), d, s);
+}
+
+hipError_t launch_qk_norm_bwd(const void* x, int ld_x, const void* gain_q, const void* gain_k, const float* cos_sin, void* dy, int ld_y, float* part, int acc, int T, int S,
+                              int nh, int d, float eps, hipStream_t s) {
+  const ah_qk_norm_rope_t c = stage_config(ld_x, gain_q, gain_k, cos_sin, ld_y, T, S, nh, d, eps);
+  QkArgs a = args(&c, x, dy, dy, ld_y, part);
+  a.acc = acc;
+  return run_bwd(a, d, bwd_blocks(&c), s);
+}
+
+int qk_norm_bwd_blocks(int T, int nh, int d) {
+  const ah_qk_norm_rope_t c = stage_config(0, nullptr, nullptr, nullptr, 0, T, T, nh, d, 1.f);
+  return bwd_blocks(&c);
+}
+
+}  // namespace ah
 
 extern "C" int ah_rope_table(float* cos_sin, int n_pos, int head_dim, double base, void* stream) {
   discard_stale_hip_error();
   if (!cos_sin || ((uintptr_t)cos_sin & 3)) return set_error(AH_EINVAL, "ah_rope_table: cos_sin is NULL or misaligned");
-  if (n_pos < 1 || n_pos > (1 << 24) || head_dim < 2 || head_dim % 2 || head_dim > 1024 || !(base > 0) || !std::isfinite(base))
-    return set_error(AH_EINVAL, "ah_rope_table: need 1 <= n_pos <= 2^24, an even head_dim <= 1024 and base > 0");
-  const size_t n = (size_t)n_pos * (head_dim / 2);
-  hipLaunchKernelGGL(table_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, (hipStream_t)stream, cos_sin, n_pos, head_dim / 2, head_dim, std::log(base));
-  return hip_status(hipGetLastError(), "ah_rope_table");
+  if (n_pos < 1 || n_pos > (1 << 24) || head_dim < 2 || head_dim % 2 || head_dim > 256 || !(base > 0) || !std::isfinite(base))
+    return set_error(AH_EINVAL, "ah_rope_table: need 1 <= n_pos <= 2^24, an even head_dim <= 256 and base > 0");
+  return hip_status(launch_rope_table(cos_sin, n_pos, head_dim, base, (hipStream_t)stream), "ah_rope_table");
 }
 
 extern "C" int ah_qk_norm_rope_fwd(const ah_qk_norm_rope_t* c, const void* x, void* y, void* stream) {
@@ -282,12 +322,7 @@ extern "C" int ah_qk_norm_rope_fwd(const ah_qk_norm_rope_t* c, const void* x, vo
   if (c->rows == 0) return AH_OK;
   if (!x || !y || off16(x) || off16(y)) return set_error(AH_EINVAL, "ah_qk_norm_rope_fwd: x or y is NULL or not 16-byte aligned");
   const QkArgs a = args(c, x, nullptr, y, c->ld_y, nullptr);
-  const int tokens = NW * (1024 / c->head_dim / a.slots);
-  const dim3 grid((c->rows + tokens - 1) / tokens, (a.passes + kFwdPasses - 1) / kFwdPasses);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(NT), 0, (hipStream_t)stream, a); };
-  if (c->head_dim == 128) { if (a.cs) go(qk_norm_fwd_kernel<128, true>); else go(qk_norm_fwd_kernel<128, false>); }
-  else { if (a.cs) go(qk_norm_fwd_kernel<64, true>); else go(qk_norm_fwd_kernel<64, false>); }
-  return hip_status(hipGetLastError(), "ah_qk_norm_rope_fwd");
+  return hip_status(run_fwd(a, c->head_dim, (hipStream_t)stream), "ah_qk_norm_rope_fwd");
 }
 
 extern "C" int ah_qk_norm_rope_bwd_workspace(const ah_qk_norm_rope_t* c, uint64_t* bytes) {
@@ -310,10 +345,7 @@ extern "C" int ah_qk_norm_rope_bwd(const ah_qk_norm_rope_t* c, const void* x, co
   const int blocks = bwd_blocks(c), d = c->head_dim;
   float* part = (float*)workspace;
   const QkArgs a = args(c, x, dy, dx, c->ld_dx, part);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(NT), 0, (hipStream_t)stream, a); };   // (no rows: writes zeros)
-  if (d == 128) { if (a.cs) go(qk_norm_bwd_kernel<128, true>); else go(qk_norm_bwd_kernel<128, false>); }
-  else { if (a.cs) go(qk_norm_bwd_kernel<64, true>); else go(qk_norm_bwd_kernel<64, false>); }
-  hipError_t e = hipGetLastError();
+  hipError_t e = run_bwd(a, d, blocks, (hipStream_t)stream);   // (no rows: writes zeros)
   if (e == hipSuccess) {
     FoldList f = {};
     if (c->n_heads) f.add(part, blocks, d, d_gain_q);

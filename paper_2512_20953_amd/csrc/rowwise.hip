@@ -582,6 +582,16 @@ __global__ __launch_bounds__(NT) void rope_kernel(bf16* __restrict__ qkv, const 
   *(bf16x8*)(p + half) = ob;
 }
 
+__global__ void rope_table_kernel(float* cs, int S, int half, int d, double base) {
+  const size_t idx = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
+  if (idx >= (size_t)S * half) return;
+  const int pos = (int)(idx / half), i = (int)(idx % half);
+  const double theta = exp(-(2.0 * i / d) * log(base));
+  const double ang = pos * theta;
+  cs[2 * idx] = (float)cos(ang);
+  cs[2 * idx + 1] = (float)sin(ang);
+}
+
 // ---------------------------------------------------------------- plain copy, 16 bytes per lane
 __global__ __launch_bounds__(NT) void copy16_kernel(const uint4* __restrict__ src, uint4* __restrict__ dst, size_t n16) {
   const size_t i = (size_t)blockIdx.x * NT + threadIdx.x;
@@ -712,6 +722,12 @@ int colsum_blocks(int T) { return (T + CS_ROWS - 1) / CS_ROWS; }
 hipError_t launch_colsum_partial(const ColsumJob& c, int T, hipStream_t s) {
   if (c.n % 8) return hipErrorInvalidValue;
   hipLaunchKernelGGL(colsum_partial_kernel, dim3((c.n + 511) / 512, colsum_blocks(T)), dim3(NT), 0, s, c, T);
+  return hipGetLastError();
+}
+
+hipError_t launch_rope_table(float* cos_sin, int S, int d, double base, hipStream_t s) {
+  const size_t n = (size_t)S * (d / 2);
+  hipLaunchKernelGGL(rope_table_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, cos_sin, S, d / 2, d, base);
   return hipGetLastError();
 }
 

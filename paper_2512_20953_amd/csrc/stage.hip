@@ -9,6 +9,7 @@
 #include <algorithm>
 #include <array>
 #include <cmath>
+#include <cstddef>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -26,18 +27,18 @@ struct ParamEntry { uint64_t off; int rows, cols; };  // cols == 0: tensor absen
 
 // byte offsets of one layer's saved activations
 struct ActLayout {
-  size_t x_in, a, qkv, o, lse, x_mid, c, u, g, stats1, stats2, bytes;
+  size_t x_in, a, qkv, qk_raw, o, lse, x_mid, c, u, g, stats1, stats2, bytes;
 };
 
 struct Workspace {
-  size_t d0, d1, dmid, dbig, dsm, delta, part_n2, part_n1, part_b1, part_bqkv, rope, prof_x, prof_dy, prof_y, prof_dx, layer_ws, pend, vec_part, k_part, bytes;
+  size_t d0, d1, dmid, dbig, dsm, delta, part_n2, part_n1, part_b1, part_bqkv, part_qk, rope, prof_x, prof_dy, prof_y, prof_dx, layer_ws, pend, vec_part, k_part, bytes;
 };
 
 // Output-gradient operands of one layer's four weight-gradient products, kept per (position in the group, layer)
 // while those products wait for the rest of the group: byte offsets inside one such block.
 struct PendLayout { size_t dy, dmid, du, dqkv, bytes; };
 // Partial sums of one layer's vector gradients, shared by the micro-batches of a group (byte offsets in its block).
-struct VecPartLayout { size_t n2, n1, b1, bqkv, bytes; };
+struct VecPartLayout { size_t n2, n1, b1, bqkv, qk, bytes; };
 
 }  // namespace
 
@@ -45,7 +46,7 @@ struct ah_stage {
   ah_stage_config_t cfg;
   ah_stage_buffers_t bufs;
   int T, h, nh, d, hl, F, L;
-  bool llama, causal, recompute, res32;
+  bool llama, causal, recompute, res32, qk_norm;
   bool rope_in_gemm;  // the QKV product's tiles hold whole heads per wave: the rotary embedding runs in its epilogue
   float eps, rope_base;
   ParamEntry ptab[AH_P_COUNT];
@@ -83,9 +84,18 @@ struct ah_stage {
 
 namespace {
 
-int validate(const ah_stage_config_t* c) {
-  if (!c) return set_error(AH_EINVAL, "config is NULL");
-  if (c->struct_size != sizeof(ah_stage_config_t)) return set_error(AH_EINVAL, "config.struct_size %u != %zu", c->struct_size, sizeof(ah_stage_config_t));
+// The configuration with the fields that the caller's struct may end before, checked
+int validate(const ah_stage_config_t* given, ah_stage_config_t* out) {
+  if (!given) return set_error(AH_EINVAL, "config is NULL");
+  const size_t first = offsetof(ah_stage_config_t, attn_window);
+  if (given->struct_size != sizeof(ah_stage_config_t) && given->struct_size != first) return set_error(AH_EINVAL, "config.struct_size %u != %zu", given->struct_size, sizeof(ah_stage_config_t));
+  *out = {};
+  memcpy(out, given, given->struct_size);
+  out->struct_size = sizeof *out;
+  const ah_stage_config_t* c = out;
+  if (c->attn_window < 0 || c->attn_sinks < 0 || (c->attn_sinks > 0 && c->attn_window == 0)) return set_error(AH_EINVAL, "attn_window and attn_sinks must be >= 0, and attn_sinks needs a window");
+  if (c->qk_norm != 0 && c->qk_norm != 1) return set_error(AH_EINVAL, "qk_norm must be 0 or 1");
+  if (c->attn_window > 0 && c->arch == AH_ARCH_BERT) return set_error(AH_EUNSUPPORTED, "attn_window goes with causal attention");
   if (c->arch != AH_ARCH_GPT && c->arch != AH_ARCH_LLAMA && c->arch != AH_ARCH_BERT) return set_error(AH_EINVAL, "unknown arch %d", c->arch);
   if (c->n_layers < 1 || c->n_layers > 1024) return set_error(AH_EINVAL, "n_layers %d out of range [1, 1024]", c->n_layers);
   if (c->tp_degree < 1 || c->tp_rank < 0 || c->tp_rank >= c->tp_degree) return set_error(AH_EINVAL, "bad tp_degree/tp_rank %d/%d", c->tp_degree, c->tp_rank);
@@ -107,6 +117,8 @@ int validate(const ah_stage_config_t* c) {
   if (hl % 128 || F % 128) return set_error(AH_EUNSUPPORTED, "local attention width %ld and local FFN width %ld must be multiples of 128", hl, F);
   if ((long)c->microbatch_size * c->seq_len > (1L << 24)) return set_error(AH_EUNSUPPORTED, "microbatch_size * seq_len too large");
   if (hl > 65536 || F > 262144) return set_error(AH_EUNSUPPORTED, "local widths too large");
+  if (c->attn_window > 0 && (long)c->microbatch_size * (hl / c->head_dim) * (c->seq_len / 128 + 8L * ((std::min(c->attn_sinks, c->seq_len) + 127) / 128)) > (1L << 23))
+    return set_error(AH_EUNSUPPORTED, "microbatch_size * heads * seq_len too large for attn_window");
   return AH_OK;
 }
 
@@ -181,6 +193,7 @@ void plan(ah_stage* s, const ah_stage_config_t* c) {
   s->causal = c->arch != AH_ARCH_BERT;
   s->recompute = c->recompute != 0;
   s->res32 = c->residual_fp32 != 0;
+  s->qk_norm = c->qk_norm != 0;
   s->group = c->wgrad_group > 1 ? c->wgrad_group : 1;
   {
     // Per-micro-batch products on the second stream hide the launches' tails and fill idle CUs (13B layer 3.86 -> 3.68
@@ -200,7 +213,7 @@ void plan(ah_stage* s, const ah_stage_config_t* c) {
     s->side_pays = gflop >= (e ? atof(e) : 12.0) && !getenv("AH_NO_SIDE_STREAM");
     s->defer = wgrads_wait(s);
   }
-  s->rope_in_gemm = s->llama && gemm_rope_pays(s->T, 3 * s->hl, s->h, s->d, 2 * s->hl) && !getenv("AH_ROPE_KERNEL");  // the variable: tuning aid
+  s->rope_in_gemm = s->llama && !s->qk_norm && gemm_rope_pays(s->T, 3 * s->hl, s->h, s->d, 2 * s->hl) && !getenv("AH_ROPE_KERNEL");  // the variable: tuning aid
   s->eps = c->norm_eps > 0 ? c->norm_eps : (s->llama ? 1e-6f : 1e-5f);
   s->rope_base = c->rope_base > 0 ? c->rope_base : 10000.f;
   const int h = s->h, hl = s->hl, F = s->F;
@@ -221,6 +234,12 @@ void plan(ah_stage* s, const ah_stage_config_t* c) {
     put(AH_P_LN1_G, 1, h); put(AH_P_WQKV, h, 3 * hl); put(AH_P_WO, hl, h); put(AH_P_LN2_G, 1, h);
     put(AH_P_W1, h, 2 * F); put(AH_P_W2, F, h);
   }
+  if (s->qk_norm) {
+    put(AH_P_QN_G, 1, s->d);
+    off = (off + 127) & ~(uint64_t)127;
+    put(AH_P_KN_G, 1, s->d);
+    off = (off + 127) & ~(uint64_t)127;
+  }
   s->layer_elems = off;
 
   // ---- activations saved for backward, per layer
@@ -233,6 +252,7 @@ void plan(ah_stage* s, const ah_stage_config_t* c) {
   const size_t keep_only_input = o;
   a.a = take(T * h * 2);
   a.qkv = take(T * 3 * hl * 2);
+  a.qk_raw = take(s->qk_norm ? T * 2 * hl * 2 : 0);
   a.o = take(T * hl * 2);
   a.lse = take(T * s->nh * 4);
   a.x_mid = take(T * h * rsz);
@@ -253,12 +273,13 @@ void plan(ah_stage* s, const ah_stage_config_t* c) {
   w.dmid = take(T * h * 2);
   w.dbig = take(T * std::max<size_t>(Fu, 3 * hl) * 2);
   w.dsm = take(T * std::max<size_t>({(size_t)h, (size_t)hl, (size_t)F}) * 2);
-  w.delta = take(T * s->nh * 4);
+  w.delta = take(c->attn_window ? attention_window_bwd_bytes(c->microbatch_size, c->seq_len, s->nh, s->d, c->attn_window, c->attn_sinks) : T * s->nh * 4);
   // partial column sums: one region per producer, so that the reductions can trail behind on the side stream
   w.part_n2 = take((size_t)3 * norm_bwd_blocks(s->T) * h * 4);
   w.part_n1 = take((size_t)3 * norm_bwd_blocks(s->T) * h * 4);
   w.part_b1 = take(s->llama ? 0 : (size_t)colsum_blocks(s->T) * F * 4);
   w.part_bqkv = take(s->llama ? 0 : (size_t)colsum_blocks(s->T) * 3 * hl * 4);
+  w.part_qk = take(s->qk_norm ? (size_t)2 * qk_norm_bwd_blocks(s->T, s->nh, s->d) * s->d * 4 : 0);
   w.rope = take(s->llama ? (size_t)c->seq_len * s->d * 4 : 0);
   w.prof_x = take(T * h * 2);
   w.prof_dy = take(T * h * 2);
@@ -280,6 +301,7 @@ void plan(ah_stage* s, const ah_stage_config_t* c) {
   s->vpart.n1 = take((size_t)3 * norm_bwd_blocks(s->T) * h * 4);
   s->vpart.b1 = take(s->llama ? 0 : (size_t)colsum_blocks(s->T) * F * 4);
   s->vpart.bqkv = take(s->llama ? 0 : (size_t)colsum_blocks(s->T) * 3 * hl * 4);
+  s->vpart.qk = take(s->qk_norm ? (size_t)2 * qk_norm_bwd_blocks(s->T, s->nh, s->d) * s->d * 4 : 0);
   s->vpart.bytes = o;
   o = before_vec;
   w.vec_part = take(s->group > 1 ? (size_t)s->L * s->vpart.bytes : 0);
@@ -291,16 +313,6 @@ void plan(ah_stage* s, const ah_stage_config_t* c) {
 inline char* P(void* base, size_t off) { return (char*)base + off; }
 
 // ------------------------------------------------------------------ small device helpers
-__global__ void rope_table_kernel(float* cs, int S, int half, int d, double base) {
-  const int idx = blockIdx.x * blockDim.x + threadIdx.x;
-  if (idx >= S * half) return;
-  const int pos = idx / half, i = idx % half;
-  const double theta = exp(-(2.0 * i / d) * log(base));
-  const double ang = pos * theta;
-  cs[2 * idx] = (float)cos(ang);
-  cs[2 * idx + 1] = (float)sin(ang);
-}
-
 __global__ void fill_pattern_kernel(__bf16* p, size_t n, uint32_t seed) {
   const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
   if (i >= n) return;
@@ -313,12 +325,13 @@ __global__ void fill_pattern_kernel(__bf16* p, size_t n, uint32_t seed) {
 enum Site {
   SITE_QKV_FWD, SITE_WO_FWD, SITE_FC1_FWD, SITE_FC2_FWD, SITE_FC2_WGRAD, SITE_FC2_DGRAD, SITE_FC1_WGRAD, SITE_FC1_DGRAD,
   SITE_WO_WGRAD, SITE_WO_DGRAD, SITE_QKV_WGRAD, SITE_QKV_DGRAD, SITE_ATTN_FWD, SITE_ATTN_BWD, SITE_NORM_FWD, SITE_NORM_BWD,
-  SITE_COLSUM, SITE_ROPE, SITE_MLP_WGRAD, SITE_ATTN_WGRAD, SITE_LAYER_WGRAD, SITE_COUNT
+  SITE_COLSUM, SITE_ROPE, SITE_MLP_WGRAD, SITE_ATTN_WGRAD, SITE_LAYER_WGRAD, SITE_QK_NORM_FWD, SITE_QK_NORM_BWD, SITE_COUNT
 };
 const char* const kSiteNames[SITE_COUNT] = {
   "gemm_nn.qkv_fwd", "gemm_nn.wo_fwd", "gemm_nn.fc1_fwd", "gemm_nn.fc2_fwd", "gemm_tn.fc2_wgrad", "gemm_nt.fc2_dgrad",
   "gemm_tn.fc1_wgrad", "gemm_nt.fc1_dgrad", "gemm_tn.wo_wgrad", "gemm_nt.wo_dgrad", "gemm_tn.qkv_wgrad", "gemm_nt.qkv_dgrad",
-  "attention_fwd", "attention_bwd", "norm_fwd", "norm_bwd", "colsum", "rope", "gemm_tn.mlp_wgrads", "gemm_tn.attn_wgrads", "gemm_tn.layer_wgrads"};
+  "attention_fwd", "attention_bwd", "norm_fwd", "norm_bwd", "colsum", "rope", "gemm_tn.mlp_wgrads", "gemm_tn.attn_wgrads", "gemm_tn.layer_wgrads",
+  "qk_norm_fwd", "qk_norm_bwd"};
 
 // brackets the launches issued while it lives with an event pair when tracing
 struct SiteTimer {
@@ -349,7 +362,8 @@ struct SiteTimer {
 };
 
 struct LayerPtrs {
-  const char *ln1_g, *ln1_b, *wqkv, *bqkv, *wo, *bo, *ln2_g, *ln2_b, *w1, *b1, *w2, *b2;
+  const char *ln1_g, *ln1_b, *wqkv, *bqkv, *wo, *bo, *ln2_g, *ln2_b, *w1, *b1, *w2, *b2, *qn_g, *kn_g;
+  float *g_qn_g, *g_kn_g;
   float *g_ln1_g, *g_ln1_b, *g_wqkv, *g_bqkv, *g_wo, *g_bo, *g_ln2_g, *g_ln2_b, *g_w1, *g_b1, *g_w2, *g_b2;
 };
 
@@ -365,12 +379,13 @@ LayerPtrs layer_ptrs(const ah_stage* s, int layer) {
   p.g_ln1_g = gp(AH_P_LN1_G); p.g_ln1_b = gp(AH_P_LN1_B); p.g_wqkv = gp(AH_P_WQKV); p.g_bqkv = gp(AH_P_BQKV);
   p.g_wo = gp(AH_P_WO); p.g_bo = gp(AH_P_BO); p.g_ln2_g = gp(AH_P_LN2_G); p.g_ln2_b = gp(AH_P_LN2_B);
   p.g_w1 = gp(AH_P_W1); p.g_b1 = gp(AH_P_B1); p.g_w2 = gp(AH_P_W2); p.g_b2 = gp(AH_P_B2);
+  p.qn_g = pp(AH_P_QN_G); p.kn_g = pp(AH_P_KN_G); p.g_qn_g = gp(AH_P_QN_G); p.g_kn_g = gp(AH_P_KN_G);
   return p;
 }
 
 // pointers to one layer's activations: the input always lives in the slot; the
 // rest either in the slot (stored) or in the shared per-layer scratch (recompute)
-struct ActPtrs { char *x_in, *a, *qkv, *o, *lse, *x_mid, *c, *u, *g, *stats1, *stats2; };
+struct ActPtrs { char *x_in, *a, *qkv, *qk_raw, *o, *lse, *x_mid, *c, *u, *g, *stats1, *stats2; };
 
 ActPtrs act_ptrs(const ah_stage* s, int slot, int layer) {
   char* slot_base = (char*)s->bufs.activations + (size_t)slot * s->slot_bytes + (size_t)layer * s->per_layer_slot_bytes;
@@ -378,7 +393,7 @@ ActPtrs act_ptrs(const ah_stage* s, int slot, int layer) {
   const ActLayout& a = s->act;
   ActPtrs p;
   p.x_in = slot_base + a.x_in;
-  p.a = rest + a.a; p.qkv = rest + a.qkv; p.o = rest + a.o; p.lse = rest + a.lse; p.x_mid = rest + a.x_mid;
+  p.a = rest + a.a; p.qkv = rest + a.qkv; p.qk_raw = rest + a.qk_raw; p.o = rest + a.o; p.lse = rest + a.lse; p.x_mid = rest + a.x_mid;
   p.c = rest + a.c; p.u = rest + a.u; p.g = rest + a.g; p.stats1 = rest + a.stats1; p.stats2 = rest + a.stats2;
   return p;
 }
@@ -433,21 +448,26 @@ enum WgradWhich { WG_FC2, WG_FC1, WG_WO, WG_QKV };
 // what it does with them.  Undeferred: the shared workspace regions, written (acc = 0) and folded into the gradient
 // at once (finish).  Deferred: the layer's own regions, written by the first micro-batch of a group and added to by
 // the others, folded once when the group closes.
-struct VecPlan { float *n2, *n1, *b1, *bqkv; int acc; bool finish; int beta; };
+struct VecPlan { float *n2, *n1, *b1, *bqkv, *qk; int acc; bool finish; int beta; };
 
 VecPlan vec_plan(const ah_stage* s, int layer, bool deferred, int pos, bool closes, int beta_now, int beta_group) {
   char* wsb = (char*)s->bufs.workspace;
   if (!deferred)
     return {(float*)(wsb + s->ws.part_n2), (float*)(wsb + s->ws.part_n1), (float*)(wsb + s->ws.part_b1), (float*)(wsb + s->ws.part_bqkv),
-            0, true, beta_now};
+            (float*)(wsb + s->ws.part_qk), 0, true, beta_now};
   char* b = wsb + s->ws.vec_part + (size_t)layer * s->vpart.bytes;
   return {(float*)(b + s->vpart.n2), (float*)(b + s->vpart.n1), (float*)(b + s->vpart.b1), (float*)(b + s->vpart.bqkv),
-          pos > 0 ? 1 : 0, closes, beta_group};
+          (float*)(b + s->vpart.qk), pos > 0 ? 1 : 0, closes, beta_group};
 }
 
 // One layer's partial sums as entries of a list to be folded into its vector gradients, by the kernel that left them.
 void add_b1(const ah_stage* s, const LayerPtrs& p, const VecPlan& vp, FoldList& f) { f.add(vp.b1, s->T / 64, s->F, p.g_b1); }
 void add_bqkv(const ah_stage* s, const LayerPtrs& p, const VecPlan& vp, FoldList& f) { f.add(vp.bqkv, colsum_blocks(s->T), 3 * s->hl, p.g_bqkv); }
+void add_qk(const ah_stage* s, const LayerPtrs& p, const VecPlan& vp, FoldList& f) {
+  const int blocks = qk_norm_bwd_blocks(s->T, s->nh, s->d);
+  f.add(vp.qk, blocks, s->d, p.g_qn_g);
+  f.add(vp.qk + (size_t)blocks * s->d, blocks, s->d, p.g_kn_g);
+}
 void add_n2(const ah_stage* s, const LayerPtrs& p, const VecPlan& vp, FoldList& f) {
   if (s->llama) f.add(vp.n2, norm_bwd_blocks(s->T), s->h, p.g_ln2_g);
   else f.add3(vp.n2, norm_bwd_blocks(s->T), s->h, p.g_ln2_g, p.g_ln2_b, p.g_b2);
@@ -506,6 +526,9 @@ hipError_t launch_wgrads(ah_stage* s, WgradList& list, int together, hipStream_t
   return hipSuccess;
 }
 
+// angles of the rotary embedding, where there is one
+const float* rope_table(const ah_stage* s) { return s->llama ? (const float*)P(s->bufs.workspace, s->ws.rope) : nullptr; }
+
 // One layer forward.  y == nullptr: stop after the activations backward needs
 // (used when a layer is re-run inside backward).  x: the stage's input, of which the first norm leaves a copy in a.x_in;
 // nullptr where a.x_in holds the layer's input already.
@@ -527,11 +550,18 @@ hipError_t layer_forward(ah_stage* s, int layer, const ActPtrs& a, const void* x
     g.rope_cs = (const float*)P(s->bufs.workspace, s->ws.rope); g.rope_S = S; g.rope_d = s->d; g.rope_cols = 2 * hl;
     SiteTimer t(s, SITE_QKV_FWD, st);
     TRY(launch_gemm(GEMM_NN, EPI_ROPE, g, st));
+  } else if (s->qk_norm) {
+    // the heads before their norms are kept for backward: Q and K go to a place of their own, V where attention reads it
+    const char* bv = p.bqkv ? p.bqkv + (size_t)2 * hl * 2 : nullptr;
+    TRY(gemm(s, SITE_QKV_FWD, GEMM_NN, EPI_BF16, a.a, h, p.wqkv, 3 * hl, a.qk_raw, 2 * hl, T, 2 * hl, h, p.bqkv, nullptr, 0, nullptr, 0, st));
+    TRY(gemm(s, SITE_QKV_FWD, GEMM_NN, EPI_BF16, a.a, h, p.wqkv + (size_t)2 * hl * 2, 3 * hl, a.qkv + (size_t)2 * hl * 2, 3 * hl, T, hl, h, bv, nullptr, 0, nullptr, 0, st));
+    TIMED(SITE_QK_NORM_FWD, launch_qk_norm_fwd(a.qk_raw, 2 * hl, p.qn_g, p.kn_g, rope_table(s), a.qkv, 3 * hl, T, S, s->nh, s->d, s->eps, st));
   } else {
     TRY(gemm(s, SITE_QKV_FWD, GEMM_NN, EPI_BF16, a.a, h, p.wqkv, 3 * hl, a.qkv, 3 * hl, T, 3 * hl, h, p.bqkv, nullptr, 0, nullptr, 0, st));
     if (s->llama) TIMED(SITE_ROPE, launch_rope(a.qkv, (const float*)P(s->bufs.workspace, s->ws.rope), T, S, s->nh, s->d, 1.f, st));
   }
-  TIMED(SITE_ATTN_FWD, launch_attention_fwd(a.qkv, a.o, (float*)a.lse, B, S, s->nh, s->d, s->causal, st));
+  if (s->cfg.attn_window) TIMED(SITE_ATTN_FWD, launch_attention_window_fwd(a.qkv, a.o, (float*)a.lse, B, S, s->nh, s->d, s->cfg.attn_window, s->cfg.attn_sinks, st));
+  else TIMED(SITE_ATTN_FWD, launch_attention_fwd(a.qkv, a.o, (float*)a.lse, B, S, s->nh, s->d, s->causal, st));
   TRY(gemm(s, SITE_WO_FWD, GEMM_NN, resid, a.o, hl, p.wo, h, a.x_mid, h, T, h, hl, p.bo, a.x_in, h, nullptr, 0, st));
   TIMED(SITE_NORM_FWD, launch_norm_fwd(s->llama, a.x_mid, p.ln2_g, p.ln2_b, a.c, (float*)a.stats2, T, h, s->eps, st, r32));
   if (!s->llama) {
@@ -642,13 +672,18 @@ hipError_t layer_backward(ah_stage* s, int layer, const ActPtrs& a, const void* 
   TRY(gemm(s, SITE_WO_DGRAD, GEMM_NT, EPI_BF16, dmid, h, p.wo, h, dsm, hl, T, hl, h, nullptr, nullptr, 0, nullptr, 0, st, nullptr, 0, beside));  // do
   // attention (where dqkv shares its buffer with du: wait until the first MLP matrix's weight gradient has read it)
   if (du_reused) TRY(hipStreamWaitEvent(st, ev[2], 0));
-  TIMED(SITE_ATTN_BWD, launch_attention_bwd(a.qkv, a.o, (const float*)a.lse, dsm, dqkv, delta, B, S, s->nh, s->d, s->causal, st));
-  if (s->llama) TIMED(SITE_ROPE, launch_rope(dqkv, (const float*)P(s->bufs.workspace, s->ws.rope), T, S, s->nh, s->d, -1.f, st));
+  if (s->cfg.attn_window)
+    TIMED(SITE_ATTN_BWD, launch_attention_window_bwd(a.qkv, a.o, (const float*)a.lse, dsm, dqkv, delta, B, S, s->nh, s->d, s->cfg.attn_window, s->cfg.attn_sinks, st));
+  else TIMED(SITE_ATTN_BWD, launch_attention_bwd(a.qkv, a.o, (const float*)a.lse, dsm, dqkv, delta, B, S, s->nh, s->d, s->causal, st));
+  if (s->qk_norm)
+    TIMED(SITE_QK_NORM_BWD, launch_qk_norm_bwd(a.qk_raw, 2 * hl, p.qn_g, p.kn_g, rope_table(s), dqkv, 3 * hl, vp.qk, vp.acc, T, S, s->nh, s->d, s->eps, st));
+  else if (s->llama) TIMED(SITE_ROPE, launch_rope(dqkv, (const float*)P(s->bufs.workspace, s->ws.rope), T, S, s->nh, s->d, -1.f, st));
   TRY(stream_order(st, sd, ev[4]));
   // The column sums of dqkv: on one stream a small matrix's run beside the first norm's backward, which saves a launch; a large one is
   // read at once, while the caches hold it.  Stage, apart / together: smallest (0.4 MB) 320.9 / 311.2 us, 5-head (1.5 MB) 241.1 / 233.5,
   // 512-wide (3.1 MB) 451.2 / 439.5, 896-wide (6.2 MB) 488.3 / 482.8, BERT-Large (25 MB) 3391 / 3407, 1.3B (25 MB) 5924 / 5947.
   // (A trace times them by themselves.  The same bits either way.)
+  if (s->qk_norm) FOLD(add_qk);
   const ColsumJob sums = {dqkv, part_bqkv, 3 * hl, vp.acc};
   const bool with_norm = !s->llama && !beside && !s->tracing && (size_t)T * 3 * hl * 2 <= (size_t)12 << 20;
   if (!s->llama) {
@@ -690,11 +725,8 @@ hipError_t ensure_side(ah_stage* s) {
 
 hipError_t ensure_rope(ah_stage* s, hipStream_t st) {
   if (!s->llama || s->rope_ready) return hipSuccess;
-  const int S = s->cfg.seq_len, half = s->d / 2;
-  hipLaunchKernelGGL(rope_table_kernel, dim3((S * half + 255) / 256), dim3(256), 0, st, (float*)P(s->bufs.workspace, s->ws.rope), S,
-                     half, s->d, (double)s->rope_base);
   s->rope_ready = true;
-  return hipGetLastError();
+  return launch_rope_table((float*)P(s->bufs.workspace, s->ws.rope), s->cfg.seq_len, s->d, (double)s->rope_base, st);
 }
 
 hipError_t stage_forward(ah_stage* s, int slot, const void* x, void* y, hipStream_t st, hipEvent_t* ev) {
@@ -715,6 +747,7 @@ hipError_t finish_vectors(ah_stage* s, int layer, const VecPlan& vp, hipStream_t
   FoldList f = {};
   add_n2(s, p, vp, f);
   add_n1(s, p, vp, f);
+  if (s->qk_norm) add_qk(s, p, vp, f);
   if (!s->llama) {
     add_b1(s, p, vp, f);
     add_bqkv(s, p, vp, f);
@@ -838,10 +871,11 @@ float median(std::vector<float>& v) {
 
 extern "C" int ah_stage_query_sizes(const ah_stage_config_t* cfg, ah_stage_sizes_t* out) {
   if (!out) return set_error(AH_EINVAL, "ah_stage_query_sizes: out is NULL");
-  int rc = validate(cfg);
+  ah_stage_config_t full;
+  int rc = validate(cfg, &full);
   if (rc) return rc;
   ah_stage tmp;
-  plan(&tmp, cfg);
+  plan(&tmp, &full);
   out->param_elems = tmp.layer_elems * tmp.L;
   out->param_bytes = out->param_elems * 2;
   out->grad_bytes = out->param_elems * 4;
@@ -854,7 +888,8 @@ extern "C" int ah_stage_query_sizes(const ah_stage_config_t* cfg, ah_stage_sizes
 extern "C" int ah_stage_create(const ah_stage_config_t* cfg, const ah_stage_buffers_t* bufs, ah_stage_t** out) {
   if (!out) return set_error(AH_EINVAL, "ah_stage_create: out is NULL");
   *out = nullptr;
-  int rc = validate(cfg);
+  ah_stage_config_t full;
+  int rc = validate(cfg, &full);
   if (rc) return rc;
   if (!bufs || !bufs->params || !bufs->grads || !bufs->activations || !bufs->workspace)
     return set_error(AH_EINVAL, "ah_stage_create: all four buffers are required");
@@ -862,9 +897,9 @@ extern "C" int ah_stage_create(const ah_stage_config_t* cfg, const ah_stage_buff
     return set_error(AH_EINVAL, "ah_stage_create: buffers must be 256-byte aligned");
   ah_stage* s = new (std::nothrow) ah_stage();
   if (!s) return set_error(AH_ENOMEM, "ah_stage_create: out of host memory");
-  plan(s, cfg);
+  plan(s, &full);
   s->bufs = *bufs;
-  s->busy.assign(cfg->max_in_flight, 0);
+  s->busy.assign(full.max_in_flight, 0);
   s->overwrite_grads = true;
   s->overwrite_wgrads = true;
   s->force_immediate = false;
@@ -1065,9 +1100,16 @@ extern "C" int ah_stage_trace_end(ah_stage_t* st, ah_trace_entry_t* out, int cap
   // counts as 2x model flops), bytes moved once for the bandwidth-bound kernels.
   const double T = st->T, h = st->h, hl = st->hl, F = st->F, Fu = st->llama ? 2.0 * st->F : st->F;
   const double S = st->cfg.seq_len, B = st->cfg.microbatch_size;
-  const double attn = 4.0 * st->d * (st->causal ? S * (S + 1) / 2 : S * S) * st->nh * B;
+  double pairs = st->causal ? S * (S + 1) / 2 : S * S;   // (query, key) pairs that see each other
+  if (const double W = st->cfg.attn_window; W > 0 && W < S) {
+    const double n = std::min<double>(st->cfg.attn_sinks, S - W);   // a query far behind sees up to n of the first keys beside its window
+    pairs = W * (W + 1) / 2 + W * (S - W) + n * (n + 1) / 2 + n * (S - W - n);
+  }
+  const double attn = 4.0 * st->d * pairs * st->nh * B;
   double flops[SITE_COUNT] = {0}, bytes[SITE_COUNT] = {0};
-  flops[SITE_QKV_FWD] = flops[SITE_QKV_WGRAD] = flops[SITE_QKV_DGRAD] = 2 * T * h * 3 * hl;
+  // (with qk_norm the QKV product is two launches, counted at their mean)
+  flops[SITE_QKV_FWD] = (st->qk_norm ? 1 : 2) * T * h * 3 * hl;
+  flops[SITE_QKV_WGRAD] = flops[SITE_QKV_DGRAD] = 2 * T * h * 3 * hl;
   flops[SITE_WO_FWD] = flops[SITE_WO_WGRAD] = flops[SITE_WO_DGRAD] = 2 * T * hl * h;
   flops[SITE_FC1_FWD] = flops[SITE_FC1_WGRAD] = flops[SITE_FC1_DGRAD] = 2 * T * h * Fu;
   flops[SITE_FC2_FWD] = flops[SITE_FC2_WGRAD] = flops[SITE_FC2_DGRAD] = 2 * T * F * h;
@@ -1082,6 +1124,8 @@ extern "C" int ah_stage_trace_end(ah_stage_t* st, ah_trace_entry_t* out, int cap
   bytes[SITE_NORM_FWD] = (stream + 2) * T * h + 8 * T + 2 * T * h * st->kept_fwd / std::max(launches[SITE_NORM_FWD], 1L);
   bytes[SITE_NORM_BWD] = (stream + 6) * T * h + 8 * T + 2 * T * h * st->kept_bwd / std::max(launches[SITE_NORM_BWD], 1L);
   bytes[SITE_ROPE] = 2 * (2 * T * 2 * hl);
+  bytes[SITE_QK_NORM_FWD] = 2 * (2 * T * 2 * hl);
+  bytes[SITE_QK_NORM_BWD] = 3 * (2 * T * 2 * hl);
   int n = 0;
   for (int sidx = 0; sidx < SITE_COUNT && n < capacity; sidx++) {
     if (!launches[sidx]) continue;
