@@ -41,7 +41,8 @@ typedef struct {
 /* The step: with g' = factor * g (factor: below),
  *   m += (1 - beta1) (g' - m);   v += (1 - beta2) (g'^2 - v);
  *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
- * in fp32, the moments without fused multiply-adds (so that any IEEE machine gets the same bits).
+ * in fp32, the moments without fused multiply-adds (so that any IEEE machine gets the same bits).  bf16 parameters without a master copy are rounded
+ * to nearest after every step: one below half a unit in a parameter's last place is lost.
  *
  * 8-bit states.  32 consecutive elements share a scale 2^(s - 127), the top binade of the block: the least for which the block's
  * largest value is within 1.75 (m) or 1.875 (v) times it.  m: sign, 4 bits of exponent, 3 of mantissa (the bit pattern
@@ -55,7 +56,7 @@ typedef struct {
   uint32_t struct_size;   /* sizeof(ah_adamw_t), checked */
   int32_t param_type, grad_type;   /* ah_type_t; master copies go with bf16 parameters */
   int32_t state_bits;     /* 32 or 8 */
-  double lr, beta1, beta2, eps;    /* lr >= 0, betas in [0, 1), eps > 0 */
+  double lr, beta1, beta2, eps;    /* lr >= 0, betas in [0, 1), eps >= 1e-37 (its reciprocal is finite in fp32) */
   int64_t step;           /* 1, 2, ... */
   const float* lr_dev;    /* device, optional: read by the kernel in place of lr ... */
   const int32_t* step_dev;   /* ... and of step (at least 1): a captured step can be replayed with other values */
@@ -82,7 +83,8 @@ int ah_adamw_state_values(const ah_adamw_tensor_t* tensors, int n_tensors, void*
  * n_seq sequences; position i of one sees position j of it iff j <= i and (i - j < window or j < sinks).  Row t of q holds n_heads heads of head_dim
  * columns, of k and v n_kv_heads; query head h reads key and value head h / (n_heads / n_kv_heads).  Scores are scaled by
  * 1 / sqrt(head_dim), softmax and sums in fp32; probabilities (and their gradients) are rounded to bf16 for the second product, as in
- * ah_attention_fwd and _bwd.  A value that is not finite may reach the rows of queries within 64 positions of those that see it.
+ * ah_attention_fwd and _bwd.  A value that is not finite may reach rows within 192 positions of those that see its own
+ * (a block of 128 queries walks tiles of 64 keys).
  *
  * Sequences of one length: seq_len rows each, one behind the other (offsets NULL).  Packed: sequence b has the rows offsets[b] .. offsets[b + 1] - 1
  * (device, int32 [n_seq + 1], ascending, each length 0 .. seq_len); rows of no sequence are neither read nor written.  A sequence that would begin or

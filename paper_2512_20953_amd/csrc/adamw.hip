@@ -58,12 +58,16 @@ __device__ __forceinline__ int find_tensor(const Table& t, uint32_t block) {
 }
 
 // ---- N consecutive values of a tensor; what lies behind its end reads as 0
-template <class T, int N> struct Wide { typedef T type __attribute__((ext_vector_type(N))); };
+// (at: the same in memory, where more than 16 bytes need not be aligned to their size)
+template <class T, int N> struct Wide {
+  typedef T type __attribute__((ext_vector_type(N)));
+  typedef type at __attribute__((aligned(sizeof(T) * N < 16 ? sizeof(T) * N : 16)));
+};
 
 template <int N, class T>
 __device__ __forceinline__ typename Wide<T, N>::type load_n(const T* p, bool whole, int left) {
   typename Wide<T, N>::type r = {};
-  if (whole) return *(const typename Wide<T, N>::type*)p;
+  if (whole) return *(const typename Wide<T, N>::at*)p;
 #pragma unroll
   for (int j = 0; j < N; j++)
     if (j < left) r[j] = p[j];
@@ -72,7 +76,7 @@ __device__ __forceinline__ typename Wide<T, N>::type load_n(const T* p, bool who
 template <int N, class T>
 __device__ __forceinline__ void store_n(T* p, typename Wide<T, N>::type r, bool whole, int left) {
   if (whole) {
-    *(typename Wide<T, N>::type*)p = r;
+    *(typename Wide<T, N>::at*)p = r;
     return;
   }
 #pragma unroll
@@ -362,8 +366,8 @@ extern "C" int ah_adamw_step(const ah_adamw_t* c, const ah_adamw_tensor_t* x, in
   if ((c->param_type != AH_BF16 && c->param_type != AH_FP32) || (c->grad_type != AH_BF16 && c->grad_type != AH_FP32))
     return set_error(AH_EINVAL, "ah_adamw_step: types must be AH_BF16 or AH_FP32");
   if (c->state_bits != 32 && c->state_bits != 8) return set_error(AH_EUNSUPPORTED, "ah_adamw_step: state_bits %d: 32 or 8", c->state_bits);
-  if (!(c->lr >= 0) || !std::isfinite(c->lr) || !(c->beta1 >= 0 && c->beta1 < 1) || !(c->beta2 >= 0 && c->beta2 < 1) || !(c->eps > 0) || !std::isfinite(c->eps))
-    return set_error(AH_EINVAL, "ah_adamw_step: need finite lr >= 0, betas in [0, 1) and eps > 0");
+  if (!(c->lr >= 0) || !std::isfinite(c->lr) || !(c->beta1 >= 0 && c->beta1 < 1) || !(c->beta2 >= 0 && c->beta2 < 1) || !(c->eps >= 1e-37) || !std::isfinite(c->eps))
+    return set_error(AH_EINVAL, "ah_adamw_step: need finite lr >= 0, betas in [0, 1) and eps >= 1e-37");
   if (c->step < 1 && !c->step_dev) return set_error(AH_EINVAL, "ah_adamw_step: step must be >= 1");
   if (off(c->lr_dev, 4) || off(c->step_dev, 4) || off(c->grad_norm, 4)) return set_error(AH_EINVAL, "ah_adamw_step: misaligned device scalar");
   if (int rc = check_list("ah_adamw_step", x, n)) return rc;

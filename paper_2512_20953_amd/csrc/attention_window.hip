@@ -62,13 +62,16 @@ __device__ __forceinline__ void load_tile(const bf16* __restrict__ g, const uint
 
 // The key tiles that a block of queries walks: the first `sink` tiles, then those from tile `first` on.
 struct Tiles {
-  int sink, first, count;
-  __device__ __forceinline__ Tiles(const WinArgs& a, int q0, int qend) {   // queries q0 .. qend
+  int sink, first, count, sinks, len;
+  __device__ __forceinline__ Tiles(const WinArgs& a, int q0, int qend, int seq_len) : sinks(a.sinks), len(seq_len) {   // queries q0 .. qend
     first = max(0, q0 - a.W + 1) / 64;
     sink = min((a.sinks + 63) / 64, first);
     count = sink + qend / 64 - first + 1;
   }
   __device__ __forceinline__ int key(int t) const { return (t < sink ? t : first + t - sink) * 64; }
+  // Where the rows of tile t end.  Behind the first tokens none of their tiles' keys is seen, by any query of the block, and none is loaded: what is not
+  // finite there would reach all later positions as 0 * inf.
+  __device__ __forceinline__ int limit(int t) const { return t < sink ? min(sinks, len) : len; }
 };
 
 // What a wave's 32 queries from q0 on see of the keys k0 .. k0 + n - 1: nothing, all, or some
@@ -143,12 +146,12 @@ __global__ __launch_bounds__(256, 2) void win_fwd_kernel(WinArgs a) {
     offk[i] = tile_src_offset<D>(wave + 4 * i, lane, a.ld_k);
     offv[i] = tile_src_offset<D>(wave + 4 * i, lane, a.ld_v);
   }
-  const Tiles tiles(a, q0, min(q0 + 127, sq.len - 1));
+  const Tiles tiles(a, q0, min(q0 + 127, sq.len - 1), sq.len);
   auto load = [&](int t) {
     const int k0 = tiles.key(t);
     char* slot = ring + (t & 1) * STAGE;
-    load_tile<D>(kp + (size_t)k0 * a.ld_k, offk, a.ld_k, sq.len - k0, slot, wave, lane);
-    load_tile<D>(vp + (size_t)k0 * a.ld_v, offv, a.ld_v, sq.len - k0, slot + TILEB, wave, lane);
+    load_tile<D>(kp + (size_t)k0 * a.ld_k, offk, a.ld_k, tiles.limit(t) - k0, slot, wave, lane);
+    load_tile<D>(vp + (size_t)k0 * a.ld_v, offv, a.ld_v, tiles.limit(t) - k0, slot + TILEB, wave, lane);
   };
   load(0);
   AH_NEXT_TILE();
@@ -251,12 +254,12 @@ __global__ __launch_bounds__(256, 2) void win_dq_kernel(WinArgs a) {
     offk[i] = tile_src_offset<D>(wave + 4 * i, lane, a.ld_k);
     offv[i] = tile_src_offset<D>(wave + 4 * i, lane, a.ld_v);
   }
-  const Tiles tiles(a, q0, min(q0 + 127, sq.len - 1));
+  const Tiles tiles(a, q0, min(q0 + 127, sq.len - 1), sq.len);
   auto load = [&](int t) {
     const int k0 = tiles.key(t);
     char* slot = ring + (t & 1) * STAGE;
-    load_tile<D>(kp + (size_t)k0 * a.ld_k, offk, a.ld_k, sq.len - k0, slot, wave, lane);
-    load_tile<D>(vp + (size_t)k0 * a.ld_v, offv, a.ld_v, sq.len - k0, slot + TILEB, wave, lane);
+    load_tile<D>(kp + (size_t)k0 * a.ld_k, offk, a.ld_k, tiles.limit(t) - k0, slot, wave, lane);
+    load_tile<D>(vp + (size_t)k0 * a.ld_v, offv, a.ld_v, tiles.limit(t) - k0, slot + TILEB, wave, lane);
   };
   load(0);
   AH_NEXT_TILE();

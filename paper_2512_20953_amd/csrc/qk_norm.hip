@@ -17,8 +17,8 @@ using namespace ah;
 namespace {
 
 constexpr int NT = 256, NW = NT / 64;
-constexpr int kFwdPasses = 4, kBwdPasses = 2;   // heads of a lane in flight together
-constexpr int kBwdBlocks = 512;                 // rows of partial sums behind the gains' gradients
+constexpr int kFwdPasses = 2, kBwdPasses = 2;   // heads of a lane in flight together
+constexpr int kBwdBlocks = 768;                 // rows of partial sums behind the gains' gradients
 
 struct QkArgs {
   const bf16 *x, *dy, *gq, *gk;

@@ -141,18 +141,40 @@ def test_offsets_outside_the_buffers_are_cut():
 
 
 @pytest.mark.parametrize("bad", [float("inf"), float("nan"), -3.0e38])
-def test_what_nobody_sees_reaches_nobody(bad):
-    S, nh, d, W, sinks = 600, 2, 64, 60, 2
+@pytest.mark.parametrize("at,W,sinks,d", [(300, 60, 2, 64), (20, 60, 2, 128), (40, 1, 5, 64), (100, 130, 70, 128)])
+def test_what_nobody_sees_reaches_nobody(at, W, sinks, d, bad):
+    """A key and value that are not finite: queries at .. at + W - 1 see them, also where they share a tile with the first tokens, which all later ones see."""
+    S, nh = 900, 2
     x = _inputs(S, nh * d, nh * d, 0, 9)
     clean = _run(*x, 1, S, nh, nh, d, W, sinks)
     y = [t.clone() for t in x]
-    y[1][300], y[2][300] = bad, bad                    # a key and value in the middle: queries 300 .. 359 see it
+    y[1][at], y[2][at] = bad, bad
     o, lse, dq, dk, dv = _run(*y, 1, S, nh, nh, d, W, sinks)
-    near = slice(300 - 64, 360 + 64)
+    keep = torch.ones(S, dtype=torch.bool, device=DEV)
+    # a block of 128 queries from q0 on walks the whole tile of 64 keys that holds `at` while q0 < at + W + 63: up to query at + W + 189
+    keep[max(0, at - 192):at + W + 192] = False
+    assert keep.sum() > 200
     for t, c in ((o, clean[0]), (dq, clean[2])):
-        keep = torch.ones(S, dtype=torch.bool, device=DEV)
-        keep[near] = False
         assert torch.equal(t[keep], c[keep])
+    assert torch.equal(lse[:, :, keep], clean[1][:, :, keep])
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_a_bad_query_reaches_its_own_keys(bad):
+    """A query and output gradient that are not finite: keys at - W + 1 .. at and the first tokens see them."""
+    S, nh, d, W, sinks, at = 1000, 2, 64, 60, 2, 600
+    x = _inputs(S, nh * d, nh * d, 0, 9)
+    clean = _run(*x, 1, S, nh, nh, d, W, sinks)
+    y = [t.clone() for t in x]
+    y[0][at], y[3][at] = bad, bad
+    out = _run(*y, 1, S, nh, nh, d, W, sinks)
+    keep = torch.ones(S, dtype=torch.bool, device=DEV)
+    keep[at - W - 192:at + 192] = False
+    keep[:sinks + 192] = False
+    for k in (3, 4):
+        assert torch.equal(out[k][keep], clean[k][keep])
+    keep[:sinks + 192] = True
+    assert torch.equal(out[0][keep], clean[0][keep]) and torch.equal(out[2][keep], clean[2][keep])
 
 
 def test_the_same_bits_every_time_and_two_streams_at_once():

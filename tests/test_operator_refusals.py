@@ -95,7 +95,7 @@ def _tensor(**kw):
 
 @pytest.mark.parametrize("kw,status", [
     (dict(struct_size=8), EINVAL), (dict(param_type=2), EINVAL), (dict(grad_type=-1), EINVAL), (dict(state_bits=16), EUNSUPPORTED), (dict(lr=-1.0), EINVAL),
-    (dict(lr=float("nan")), EINVAL), (dict(beta1=1.0), EINVAL), (dict(beta2=-0.1), EINVAL), (dict(eps=0.0), EINVAL), (dict(step=0), EINVAL),
+    (dict(lr=float("nan")), EINVAL), (dict(beta1=1.0), EINVAL), (dict(beta2=-0.1), EINVAL), (dict(eps=0.0), EINVAL), (dict(eps=1e-38), EINVAL), (dict(step=0), EINVAL),
     (dict(lr_dev=258), EINVAL), (dict(step_dev=258), EINVAL), (dict(grad_norm=258), EINVAL)])
 def test_adamw_configurations(kw, status):
     assert B.lib.ah_adamw_step(C.byref(_adam(**kw)), _tensor(), 1, None) == status
