@@ -20,10 +20,13 @@ using namespace ah;
 
 namespace {
 
+// What stands behind this in a conditional is jumped over, not computed and selected (the masks: a fifth of a step's vector instructions, wanted in a fifth of the steps)
+#define AH_A_BRANCH() asm volatile("")
+
 struct WinArgs {
   const bf16 *q, *k, *v, *o, *d_o;
   bf16 *out, *dq, *dk, *dv;
-  float *lse, *delta, *part, *far_part;
+  float *lse, *delta, *nlse2, *part, *far_part;
   const int32_t* offsets;
   size_t ld_q, ld_k, ld_v, ld_o, ld_do, ld_dq, ld_dk, ld_dv;
   int64_t rows;
@@ -86,7 +89,7 @@ __device__ __forceinline__ Seen seen(const WinArgs& a, int q0, int k0, int n) {
 struct Mask {
   int lim, low, first;
   __device__ __forceinline__ Mask(const WinArgs& a, int q, int k0, int hf) : lim(q - k0 - 4 * hf), low(lim - a.W), first(a.sinks - k0 - 4 * hf) {}
-  __device__ __forceinline__ bool hides(int key) const { return key > lim || (key <= low && key >= first); }
+  __device__ __forceinline__ bool hides(int key) const { return (key > lim) | ((key <= low) & (key >= first)); }   // (no branches)
 };
 
 // rows of a result that lie before the sequence's end
@@ -170,6 +173,7 @@ __global__ __launch_bounds__(256, 2) void win_fwd_kernel(WinArgs a) {
         for (int ks = 0; ks < NK; ks++) s[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rowmajor<D>(cK, 32 * h + (lane & 31), ks, hf), qf[ks], s[h], 0, 0, 0);
       }
       if (what == SOME) {
+        AH_A_BRANCH();
         const Mask mask(a, q, k0, hf);
 #pragma unroll
         for (int h = 0; h < 2; h++)
@@ -246,7 +250,10 @@ __global__ __launch_bounds__(256, 2) void win_dq_kernel(WinArgs a) {
 #pragma unroll
     for (int r = 0; r < 16; r++) acc[dt][r] = 0.f;
   const float lse2 = a.lse[row] * LOG2E, delta = row_delta<D>(dof, a.o + token * a.ld_o + head * D, hf);
-  if (hf == 0 && q < sq.len) a.delta[row] = -delta;   // negated: what the dK/dV kernel starts dP from
+  if (hf == 0 && q < sq.len) {   // for the dK/dV kernel: what dP starts from, and what the exponent's argument ends with
+    a.delta[row] = -delta;
+    a.nlse2[row] = -lse2;
+  }
 
   uint32_t offk[ND], offv[ND];
 #pragma unroll
@@ -282,10 +289,10 @@ __global__ __launch_bounds__(256, 2) void win_dq_kernel(WinArgs a) {
 #pragma unroll
       for (int r = 0; r < 16; r++) s[r] = fexp2(__builtin_fmaf(s[r], a.sc2, -lse2));
       if (what == SOME) {
+        AH_A_BRANCH();
         const Mask mask(a, q, k0 + 32 * h, hf);
 #pragma unroll
-        for (int r = 0; r < 16; r++)
-          if (mask.hides(8 * (r >> 2) + (r & 3))) { s[r] = 0.f; dp[r] = 0.f; }
+        for (int r = 0; r < 16; r++) s[r] = mask.hides(8 * (r >> 2) + (r & 3)) ? 0.f : s[r];
       }
 #pragma unroll
       for (int r = 0; r < 16; r++) s[r] *= dp[r];
@@ -375,8 +382,8 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void win_dkv_kernel(WinArgs a
     fill ^= 1;
     load_tile<D>(a.q + (size_t)(sq.r0 + r0) * a.ld_q + head * D, offq, a.ld_q, left, slot, wave, lane);
     load_tile<D>(a.d_o + (size_t)(sq.r0 + r0) * a.ld_do + head * D, offo, a.ld_do, left, slot + TILEB, wave, lane);
-    // 64 log-sum-exps, 64 -deltas (waves 2 and 3 repeat them into spare bytes)
-    load4(((wave & 1) ? a.delta : a.lse) + ((size_t)b * a.nh + head) * a.S + r0, (uint32_t)min(lane, left - 1) * 4u, slot + 2 * TILEB + wave * 256);
+    // 64 -log-sum-exps (base 2), 64 -deltas (waves 2 and 3 repeat them into spare bytes)
+    load4(((wave & 1) ? a.delta : a.nlse2) + ((size_t)b * a.nh + head) * a.S + r0, (uint32_t)min(lane, left - 1) * 4u, slot + 2 * TILEB + wave * 256);
   };
   bf16x8 kf[NK], vf[NK];
   f32x16 dk[ND], dv[ND];
@@ -416,14 +423,15 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void win_dkv_kernel(WinArgs a
         dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rowmajor<D>(cO, t + (lane & 31), ks, hf), vf[ks], dp, 0, 0, 0);
       }
 #pragma unroll
-      for (int r = 0; r < 16; r++) s[r] = fexp2(__builtin_fmaf(s[r], a.sc2, -stat[t + 4 * hf + 8 * (r >> 2) + (r & 3)] * LOG2E));
+      for (int r = 0; r < 16; r++) s[r] = fexp2(__builtin_fmaf(s[r], a.sc2, stat[t + 4 * hf + 8 * (r >> 2) + (r & 3)]));
       if (!every) {
+        AH_A_BRANCH();
         // query qw0 + 4 hf + c sees the lane's key iff lo <= c <= hi
         const int lo = key - qw0 - 4 * hf, end = sq.len - 1 - qw0 - 4 * hf, hi = key < a.sinks ? end : min(end, lo + a.W - 1);
 #pragma unroll
         for (int r = 0; r < 16; r++) {
           const int c = 8 * (r >> 2) + (r & 3);
-          if (c < lo || c > hi) { s[r] = 0.f; dp[r] = 0.f; }
+          s[r] = (c < lo) | (c > hi) ? 0.f : s[r];
         }
       }
 #pragma unroll
@@ -576,14 +584,15 @@ hipError_t run_fwd(const WinArgs& a, int d, hipStream_t s) {
   return hipGetLastError();
 }
 
-size_t bwd_bytes(const ah_attention_window_t* c) { return delta_bytes(c) + near_bytes(c) + far_bytes(c); }
+size_t bwd_bytes(const ah_attention_window_t* c) { return 2 * delta_bytes(c) + near_bytes(c) + far_bytes(c); }
 
 hipError_t run_bwd(WinArgs a, const ah_attention_window_t* c, void* workspace, hipStream_t s) {
   a.delta = (float*)workspace;
   a.chunks = far_chunks(c);
   a.far_waves = far_waves(c);
   a.near = near_shares(c);
-  a.part = (float*)((char*)workspace + delta_bytes(c));
+  a.nlse2 = (float*)((char*)workspace + delta_bytes(c));
+  a.part = (float*)((char*)workspace + 2 * delta_bytes(c));
   a.far_part = (float*)((char*)a.part + near_bytes(c));
   const int key_blocks = (a.S + 127) / 128, sink_blocks = (a.sinks + 127) / 128;
   const dim3 gq((unsigned)(a.n_seq * a.nh * key_blocks)), gk((unsigned)(a.n_seq * a.nkv * (key_blocks * a.near + sink_blocks * a.chunks)));

@@ -42,10 +42,10 @@ def test_window_pointers():
 
 def test_window_workspace_holds_row_sums_and_the_shares_of_the_first_keys():
     n = lambda **kw: P.attention_window_bwd_workspace(**{**dict(n_seq=2, seq_len=100, nh=4, nh_kv=2, d=64, window=8, sinks=0), **kw})  # noqa: E731
-    sums = (2 * 4 * 100 * 4 + 255) // 256 * 256
+    sums = 2 * ((2 * 4 * 100 * 4 + 255) // 256 * 256)
     shares = n() - sums                                                    # a launch that small shares each key block's walk: [sequence, key head][share][100 keys]...
     assert shares > 0 and shares % (2 * 2 * 100 * 2 * 64 * 4) == 0
-    assert n(n_seq=300) == 300 * 4 * 100 * 4 // 256 * 256 + (0 if 300 * 4 * 100 * 4 % 256 == 0 else 256)   # ... one that fills the chip does not
+    assert n(n_seq=300) == 2 * 300 * 4 * 100 * 4   # ... one that fills the chip does not
     far = n(seq_len=4000, sinks=4) - n(seq_len=4000)
     assert far > 0 and far % (2 * 2 * 4 * 2 * 64 * 4) == 0                 # [sequence, key head][share][4 keys][dk, dv][64] fp32
     assert n(seq_len=4000, sinks=4, window=4000) == n(seq_len=4000, window=4000)   # nobody lies behind the window
