@@ -392,17 +392,20 @@ def _refuse(msg, *args):
     raise AhError(1, msg % args)
 
 
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else lambda: -1   # (-1 without a GPU, as a host tensor's)
+
+
 def _on_device(what, t):
     at = t.get_device()
-    if at < 0:
-        _refuse("%s is not in device memory", what)
-    if at != torch._C._cuda_getDevice():
-        _refuse("%s lies on device %d, which is not the current one", what, at)
+    if at < 0 or at != _current_device():
+        _refuse("%s is not in device memory" if at < 0 else "%s lies on device " + str(at) + ", which is not the current one", what)
 
 
 def _dense(what, t, dtype, n=None):
     """Address of a contiguous tensor of n elements."""
-    _on_device(what, t)
+    device = t.get_device()
+    if device < 0 or device != _current_device():
+        _on_device(what, t)
     if t.dtype is not dtype or not t.is_contiguous() or (n is not None and t.numel() != n):
         _refuse("%s: %s of shape %s (contiguous: %s), wanted a contiguous tensor of %s%s", what, t.dtype, tuple(t.shape), t.is_contiguous(), dtype,
                 "" if n is None else " with %d elements" % n)
@@ -411,7 +414,9 @@ def _dense(what, t, dtype, n=None):
 
 def _rows(what, t, rows, cols):
     """(address, columns from row to row) of a bf16 matrix whose rows are dense and 16-byte aligned, at any distance from each other."""
-    _on_device(what, t)
+    device = t.get_device()
+    if device < 0 or device != _current_device():
+        _on_device(what, t)
     shape, stride, at = t.shape, t.stride(), t.data_ptr()
     if t.dtype is not _BF16 or len(shape) != 2 or shape[1] != cols or shape[0] != rows:
         _refuse("%s: %s of shape %s, wanted bf16 [%d, %d]", what, t.dtype, tuple(shape), rows, cols)

@@ -18,10 +18,11 @@ using namespace ah;
 namespace {
 
 constexpr int NT = 256, kTensors = 48;
-constexpr int VEC = 4, kReps = 2, kChunk = NT * VEC * kReps;            // elements of a lane at once, times a lane, elements per block
-constexpr int VEC8 = 8, kReps8 = 1, kChunk8 = NT * VEC8 * kReps8;       // with states in 8 bits, of which four elements fill no load
+// Elements of a lane, and of a block.  One run of 16 bytes a lane for fp32 states (two take 651 instead of 623 us for 100 M parameters with a master copy and the norm, four
+// 658); eight for states in 8 bits, of which four fill no load.
+constexpr int VEC = 4, kChunk = NT * VEC, VEC8 = 8, kChunk8 = NT * VEC8;
 constexpr int kBlock = 32;                   // elements that share a scale
-constexpr uint64_t kMaxElements = 1ull << 34, kMaxBlocks = kMaxElements / 2048;   // of a tensor; of a launch (2^23: its threads are counted in 32 bits)
+constexpr uint64_t kMaxElements = 1ull << 33, kMaxBlocks = kMaxElements / kChunk;   // of a tensor; of a launch (2^23: its threads are counted in 32 bits)
 
 struct Entry {
   void* param;
@@ -132,101 +133,87 @@ __global__ __launch_bounds__(NT) void adamw_step_kernel(Table t, Hyper h) {
   }
   const int k = find_tensor(t, blockIdx.x);
   const Entry& e = t.e[k];
-  constexpr int V = BITS8 ? VEC8 : VEC, R = BITS8 ? kReps8 : kReps;
-  const uint64_t at = (uint64_t)(blockIdx.x - t.first[k]) * (NT * V * R);
-  const uint32_t left = (uint32_t)min(e.n - at, (uint64_t)(NT * V * R));   // elements of this chunk
+  constexpr int V = BITS8 ? VEC8 : VEC;
   typedef typename std::conditional<BITS8, uint8_t, float>::type S;
-  const G* g = (const G*)e.grad + at;
-  S *m = (S*)e.m + at, *v = (S*)e.v + at;
-  P* p = (P*)e.param + at;
-  float* w = MASTER ? e.master + at : nullptr;
+  // the lane's first element is the block's first, a scalar, and a 32-bit distance
+  const uint64_t base = (uint64_t)(blockIdx.x - t.first[k]) * (NT * V);
+  const uint32_t left = (uint32_t)min(e.n - base, (uint64_t)(NT * V)), i = threadIdx.x * V;
+  const int rest = i < left ? (int)(left - i) : 0;
+  const bool whole = h.aligned && rest >= V;
+  const G* g = (const G*)e.grad + base;
+  S *m = (S*)e.m + base, *v = (S*)e.v + base;
+  P* p = (P*)e.param + base;
+  float* w = MASTER ? e.master + base : nullptr;
   const float keep = 1.f - lr * e.wd;
-
-  typename Wide<G, V>::type tg[R];
-  typename Wide<S, V>::type tm[R], tv[R];
-  typename Wide<P, V>::type tp[R];
-  typename Wide<float, V>::type tw[R];
-  int sm[R], sv[R];
-#pragma unroll
-  for (int r = 0; r < R; r++) {
-    const uint32_t i = (r * NT + threadIdx.x) * V;
-    const int rest = i < left ? (int)(left - i) : 0;
-    const bool whole = h.aligned && rest >= V;
-    tg[r] = load_n<V, G>(g + i, whole, rest);
-    tm[r] = load_n<V, S>(m + i, whole, rest);
-    tv[r] = load_n<V, S>(v + i, whole, rest);
-    if constexpr (MASTER) tw[r] = load_n<V, float>(w + i, whole, rest);
-    else tp[r] = load_n<V, P>(p + i, whole, rest);
-    if constexpr (BITS8) {
-      sm[r] = rest ? e.ms[(at + i) / kBlock] : 0;
-      sv[r] = rest ? e.vs[(at + i) / kBlock] : 0;
-    }
+  const auto tg = load_n<V, G>(g + i, whole, rest);
+  const auto tm = load_n<V, S>(m + i, whole, rest), tv = load_n<V, S>(v + i, whole, rest);
+  typename Wide<P, V>::type tp;
+  typename Wide<float, V>::type tw;
+  if constexpr (MASTER) tw = load_n<V, float>(w + i, whole, rest);
+  else tp = load_n<V, P>(p + i, whole, rest);
+  int sm = 0, sv = 0;
+  if (BITS8 && rest) {
+    sm = e.ms[(base + i) / kBlock];
+    sv = e.vs[(base + i) / kBlock];
   }
+  float nm[V], nv[V];
+  typename Wide<float, V>::type now;
 #pragma unroll
-  for (int r = 0; r < R; r++) {
-    const uint32_t i = (r * NT + threadIdx.x) * V;
-    const int rest = i < left ? (int)(left - i) : 0;
-    const bool whole = h.aligned && rest >= V;
-    float nm[V], nv[V];
-    typename Wide<float, V>::type nw;
-#pragma unroll
-    for (int j = 0; j < V; j++) {
+  for (int j = 0; j < V; j++) {
 #pragma clang fp contract(off)
-      const float gr = (float)tg[r][j] * factor;
-      float om, ov;
-      if constexpr (BITS8) {
-        om = decode<15>(tm[r][j] & 127, sm[r]);
-        om = tm[r][j] & 128 ? -om : om;
-        ov = decode<31>(tv[r][j], sv[r]);
-      } else {
-        om = tm[r][j];
-        ov = tv[r][j];
-      }
-      nm[j] = om + h.c1 * (gr - om);
-      nv[j] = ov + h.c2 * (gr * gr - ov);
+    const float gr = (float)tg[j] * factor;
+    float om, ov;
+    if constexpr (BITS8) {
+      om = decode<15>(tm[j] & 127, sm);
+      om = tm[j] & 128 ? -om : om;
+      ov = decode<31>(tv[j], sv);
+    } else {
+      om = tm[j];
+      ov = tv[j];
     }
+    nm[j] = om + h.c1 * (gr - om);
+    nv[j] = ov + h.c2 * (gr * gr - ov);
+  }
+#pragma unroll
+  for (int j = 0; j < V; j++) {
+    const float denom = __builtin_fmaf(__builtin_amdgcn_sqrtf(nv[j]), root, h.eps);
+    now[j] = __builtin_fmaf(MASTER ? tw[j] : (float)tp[j], keep, -alpha * nm[j] * __builtin_amdgcn_rcpf(denom));
+  }
+  typename Wide<S, V>::type om, ov;
+  if constexpr (BITS8) {
+    uint32_t am = 0, av = 0;
 #pragma unroll
     for (int j = 0; j < V; j++) {
-      const float old = MASTER ? tw[r][j] : (float)tp[r][j];
-      const float denom = __builtin_fmaf(__builtin_amdgcn_sqrtf(nv[j]), root, h.eps);
-      nw[j] = __builtin_fmaf(old, keep, -alpha * nm[j] * __builtin_amdgcn_rcpf(denom));
+      if (j < rest) {
+        am = max(am, __float_as_uint(nm[j]) & 0x7fffffffu);
+        av = max(av, __float_as_uint(nv[j]) & 0x7fffffffu);
+      }
     }
-    typename Wide<S, V>::type om, ov;
-    if constexpr (BITS8) {
-      uint32_t am = 0, av = 0;
+    const int s1 = scale_of<15>(block_max(am)), s2 = scale_of<31>(block_max(av));
+    const uint32_t first = (e.number + (uint32_t)base + i) * kNumber + h.seed;
 #pragma unroll
-      for (int j = 0; j < V; j++) {
-        if (j < rest) {
-          am = max(am, __float_as_uint(nm[j]) & 0x7fffffffu);
-          av = max(av, __float_as_uint(nv[j]) & 0x7fffffffu);
-        }
-      }
-      const int s1 = scale_of<15>(block_max(am)), s2 = scale_of<31>(block_max(av));
-      const uint32_t first = (e.number + (uint32_t)at + i) * kNumber + h.seed;
-#pragma unroll
-      for (int j = 0; j < V; j++) {
-        const uint32_t bits = random_bits(first + j * kNumber);
-        const uint32_t cm = s1 == 255 ? 0x7f : encode<15>(fabsf(nm[j]), s1, bits & 0xffff);
-        const uint32_t cv = s2 == 255 ? 0xff : max(encode<31>(nv[j], s2, bits >> 16), nv[j] > 0.f ? 1u : 0u);
-        om[j] = (uint8_t)(cm | (__float_as_uint(nm[j]) >> 31 << 7));
-        ov[j] = (uint8_t)cv;
-      }
-      if (rest && (threadIdx.x & 3) == 0) {
-        e.ms[(at + i) / kBlock] = (uint8_t)s1;
-        e.vs[(at + i) / kBlock] = (uint8_t)s2;
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < V; j++) { om[j] = nm[j]; ov[j] = nv[j]; }
+    for (int j = 0; j < V; j++) {
+      const uint32_t bits = random_bits(first + j * kNumber);
+      const uint32_t cm = s1 == 255 ? 0x7f : encode<15>(fabsf(nm[j]), s1, bits & 0xffff);
+      const uint32_t cv = s2 == 255 ? 0xff : max(encode<31>(nv[j], s2, bits >> 16), nv[j] > 0.f ? 1u : 0u);
+      om[j] = (uint8_t)(cm | (__float_as_uint(nm[j]) >> 31 << 7));
+      ov[j] = (uint8_t)cv;
     }
-    store_n<V, S>(m + i, om, whole, rest);
-    store_n<V, S>(v + i, ov, whole, rest);
-    if constexpr (MASTER) store_n<V, float>(w + i, nw, whole, rest);
-    typename Wide<P, V>::type np;
+    if (rest && (threadIdx.x & 3) == 0) {
+      e.ms[(base + i) / kBlock] = (uint8_t)s1;
+      e.vs[(base + i) / kBlock] = (uint8_t)s2;
+    }
+  } else {
 #pragma unroll
-    for (int j = 0; j < V; j++) np[j] = (P)nw[j];
-    store_n<V, P>(p + i, np, whole, rest);
+    for (int j = 0; j < V; j++) { om[j] = nm[j]; ov[j] = nv[j]; }
   }
+  store_n<V, S>(m + i, om, whole, rest);
+  store_n<V, S>(v + i, ov, whole, rest);
+  if constexpr (MASTER) store_n<V, float>(w + i, now, whole, rest);
+  typename Wide<P, V>::type np;
+#pragma unroll
+  for (int j = 0; j < V; j++) np[j] = (P)now[j];
+  store_n<V, P>(p + i, np, whole, rest);
 }
 
 // ---- the norm of all gradients: a partial sum in fp64 for each of a fixed number of blocks, which a second launch adds up in order.  (Added up by the
@@ -353,7 +340,7 @@ bool vectors(const ah_adamw_tensor_t& x, const Widths& w, int n) {
 int check_list(const char* who, const ah_adamw_tensor_t* x, int n) {
   if (n < 0 || (n > 0 && !x)) return set_error(AH_EINVAL, "%s: bad tensor list", who);
   for (int i = 0; i < n; i++)
-    if (x[i].n > kMaxElements) return set_error(AH_EUNSUPPORTED, "%s: tensor %d has %llu elements, more than 2^34", who, i, (unsigned long long)x[i].n);
+    if (x[i].n > kMaxElements) return set_error(AH_EUNSUPPORTED, "%s: tensor %d has %llu elements, more than 2^33", who, i, (unsigned long long)x[i].n);
   return AH_OK;
 }
 
