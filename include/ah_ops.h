@@ -68,7 +68,7 @@ typedef struct {
 /* tensors: HOST array, read during the call. */
 int ah_adamw_step(const ah_adamw_t* cfg, const ah_adamw_tensor_t* tensors, int n_tensors, void* hip_stream);
 
-/* out[0] = the 2-norm of all the tensors' gradients together, out[1] = min(1, max_norm / out[0]) (1 where max_norm is 0: no limit;
+/* out[0] = the 2-norm of all the tensors' gradients together, out[1] = min(1, max_norm / out[0]) (1 where max_norm is 0: no limit, else at least 2^-126;
  * NaN where the norm is not finite).  Reads the tensors' grad and n only.  out: device, two floats.  Sums in fp64, in an order that depends on the sizes alone.
  * workspace: device, of the size that ah_grad_norm_workspace gives, 8-byte aligned. */
 int ah_grad_norm(const ah_adamw_tensor_t* tensors, int n_tensors, int grad_type, double max_norm, float* out, void* workspace, void* hip_stream);

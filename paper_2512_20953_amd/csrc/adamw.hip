@@ -10,6 +10,7 @@
 #include "common.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <type_traits>
@@ -413,7 +414,8 @@ extern "C" int ah_grad_norm(const ah_adamw_tensor_t* x, int n, int grad_type, do
   discard_stale_hip_error();
   if (!out || !workspace || off(out, 4) || off(workspace, 8)) return set_error(AH_EINVAL, "ah_grad_norm: out or workspace is NULL or misaligned");
   if (grad_type != AH_BF16 && grad_type != AH_FP32) return set_error(AH_EINVAL, "ah_grad_norm: grad_type must be AH_BF16 or AH_FP32");
-  if (!(max_norm >= 0) || !std::isfinite(max_norm)) return set_error(AH_EINVAL, "ah_grad_norm: max_norm must be finite and >= 0");
+  if (!(max_norm >= 0) || !std::isfinite(max_norm) || (max_norm > 0 && max_norm < FLT_MIN)) return set_error(AH_EINVAL, "ah_grad_norm: max_norm must be finite and 0 or at least 2^-126");
+  max_norm = std::min(max_norm, (double)FLT_MAX);   // (no finite norm is above it)
   if (int rc = check_list("ah_grad_norm", x, n)) return rc;
   const bool g32 = grad_type == AH_FP32;
   bool aligned = true;

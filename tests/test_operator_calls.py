@@ -1,0 +1,14 @@
+"""Calls at the edges of what the operators of include/ah_ops.h document, through the C ABI with made-up addresses (nothing is launched) and through the binding."""
+import ctypes as C
+
+import pytest
+
+from paper_2512_20953_amd import binding as B
+
+EINVAL = 1
+
+
+@pytest.mark.parametrize("max_norm", [1e-50, 1e-46, 1e-40])
+def test_a_limit_that_fp32_does_not_hold_is_refused(max_norm):
+    # (1e-50 rounds to 0, which would stand for no limit; subnormals lose digits of the factor)
+    assert B.lib.ah_grad_norm(None, 0, 1, max_norm, 256, 256, None) == EINVAL
