@@ -123,7 +123,7 @@ typedef struct {
   int32_t n_heads, n_kv_heads; /* >= 0, not both 0 */
   int32_t head_dim;            /* 64 or 128 */
   int32_t n_pos;               /* rows of cos_sin; without `positions` at least min(seq_len, rows) */
-  float eps;                   /* > 0 */
+  float eps;                   /* >= 2^-126 */
   int64_t ld_x, ld_y, ld_dx;   /* columns from row to row of x, of y (or dy) and of dx: multiples of 8, at least (n_heads + n_kv_heads) * head_dim; 0: just that */
   const void *gain_q, *gain_k; /* device; gain_k may be NULL where n_kv_heads is 0, gain_q likewise */
   const float* cos_sin;        /* device [n_pos][head_dim / 2][2] (ah_rope_table); NULL: no rotation */

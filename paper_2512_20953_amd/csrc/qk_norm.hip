@@ -12,6 +12,7 @@
 #include "kernels.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 
 using namespace ah;
@@ -226,7 +227,7 @@ int check(const char* who, const ah_qk_norm_rope_t* c) {
   if (c->rows < 0 || c->n_heads < 0 || c->n_kv_heads < 0 || c->n_heads > 65536 || c->n_kv_heads > 65536 || c->n_heads + c->n_kv_heads == 0)
     return set_error(AH_EINVAL, "%s: need rows >= 0 and 1 .. 65536 heads", who);
   if (c->rows > (1 << 25)) return set_error(AH_EUNSUPPORTED, "%s: more than 2^25 rows", who);
-  if (!(c->eps > 0) || !std::isfinite(c->eps)) return set_error(AH_EINVAL, "%s: eps must be finite and > 0", who);
+  if (!(c->eps >= FLT_MIN) || !std::isfinite(c->eps)) return set_error(AH_EINVAL, "%s: eps must be finite and at least 2^-126", who);
   if ((c->n_heads && !c->gain_q) || (c->n_kv_heads && !c->gain_k)) return set_error(AH_EINVAL, "%s: a gain is NULL", who);
   if (off16(c->gain_q) || off16(c->gain_k) || off16(c->cos_sin) || ((uintptr_t)c->positions & 3)) return set_error(AH_EINVAL, "%s: gains and cos_sin must be 16-byte aligned, positions 4-byte", who);
   const int64_t width = (int64_t)(c->n_heads + c->n_kv_heads) * c->head_dim;

@@ -8,6 +8,7 @@
 
 #include <algorithm>
 #include <array>
+#include <cfloat>
 #include <cmath>
 #include <cstddef>
 #include <cstdio>
@@ -95,6 +96,7 @@ int validate(const ah_stage_config_t* given, ah_stage_config_t* out) {
   const ah_stage_config_t* c = out;
   if (c->attn_window < 0 || c->attn_sinks < 0 || (c->attn_sinks > 0 && c->attn_window == 0)) return set_error(AH_EINVAL, "attn_window and attn_sinks must be >= 0, and attn_sinks needs a window");
   if (c->qk_norm != 0 && c->qk_norm != 1) return set_error(AH_EINVAL, "qk_norm must be 0 or 1");
+  if (c->qk_norm && c->norm_eps > 0 && c->norm_eps < FLT_MIN) return set_error(AH_EINVAL, "qk_norm needs a norm_eps of at least 2^-126");
   if (c->attn_window > 0 && c->arch == AH_ARCH_BERT) return set_error(AH_EUNSUPPORTED, "attn_window goes with causal attention");
   if (c->arch != AH_ARCH_GPT && c->arch != AH_ARCH_LLAMA && c->arch != AH_ARCH_BERT) return set_error(AH_EINVAL, "unknown arch %d", c->arch);
   if (c->n_layers < 1 || c->n_layers > 1024) return set_error(AH_EINVAL, "n_layers %d out of range [1, 1024]", c->n_layers);

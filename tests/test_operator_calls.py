@@ -12,3 +12,10 @@ EINVAL = 1
 def test_a_limit_that_fp32_does_not_hold_is_refused(max_norm):
     # (1e-50 rounds to 0, which would stand for no limit; subnormals lose digits of the factor)
     assert B.lib.ah_grad_norm(None, 0, 1, max_norm, 256, 256, None) == EINVAL
+
+
+@pytest.mark.parametrize("eps", [1e-45, 1e-39])
+def test_a_subnormal_epsilon_of_the_norms_is_refused(eps):
+    c = B._QkNormConfig(struct_size=C.sizeof(B._QkNormConfig), rows=10, seq_len=5, n_heads=4, n_kv_heads=2, head_dim=64, n_pos=5, eps=eps, gain_q=256, gain_k=256, cos_sin=256)
+    assert B.lib.ah_qk_norm_rope_fwd(C.byref(c), None, None, None) == EINVAL
+    assert b"eps" in B.lib.ah_last_error()
