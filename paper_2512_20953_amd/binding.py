@@ -427,6 +427,8 @@ def _rows(what, t, rows, cols):
 
 
 def _window_config(n_seq, seq_len, nh, nh_kv, d, window, sinks):
+    if not (0 <= window < 1 << 31 and 0 <= sinks < 1 << 31):    # (a field keeps the lowest 32 bits; the library refuses what is negative)
+        window, sinks = max(-1, min(window, (1 << 31) - 1)), max(-1, min(sinks, (1 << 31) - 1))
     return _WindowConfig(_WINDOW_SIZE, n_seq, seq_len, nh, nh_kv, d, window, sinks)
 
 

@@ -19,3 +19,12 @@ def test_a_subnormal_epsilon_of_the_norms_is_refused(eps):
     c = B._QkNormConfig(struct_size=C.sizeof(B._QkNormConfig), rows=10, seq_len=5, n_heads=4, n_kv_heads=2, head_dim=64, n_pos=5, eps=eps, gain_q=256, gain_k=256, cos_sin=256)
     assert B.lib.ah_qk_norm_rope_fwd(C.byref(c), None, None, None) == EINVAL
     assert b"eps" in B.lib.ah_last_error()
+
+
+def test_a_window_that_32_bits_do_not_hold_is_everything():
+    most = 2 ** 31 - 1
+    for window, sinks in ((2 ** 32 + 5, 0), (2 ** 40, 2 ** 33 + 1), (2 ** 31, 3)):
+        c = B._window_config(1, 100, 2, 2, 64, window, sinks)
+        assert c.window == most and c.sinks == min(sinks, most)
+    c = B._window_config(1, 100, 2, 2, 64, -2 ** 33 + 7, 0)
+    assert c.window < 1                                           # refused, not taken for 7
