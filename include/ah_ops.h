@@ -23,8 +23,8 @@ extern "C" {
 
 typedef enum { AH_BF16 = 0, AH_FP32 = 1 } ah_type_t;
 
-/* One tensor of a step.  Device pointers, each aligned to its element; n elements one behind the other.  Tensors of one call do
- * not overlap (each element would be stepped twice, in no order). */
+/* One tensor of a step.  Device pointers, each aligned to its element; n elements one behind the other.  What a call writes overlaps nothing else that
+ * it reads or writes (an element of a tensor given twice would be stepped twice, in no order); gradients may be shared. */
 typedef struct {
   void* param;          /* bf16 or fp32: ah_adamw_t.param_type */
   const void* grad;     /* bf16 or fp32: ah_adamw_t.grad_type */
@@ -102,7 +102,8 @@ typedef struct {
   int64_t ld_q, ld_k, ld_v, ld_o, ld_do, ld_dq, ld_dk, ld_dv;
 } ah_attention_window_t;
 
-/* o (bf16, rows of n_heads * head_dim) and lse (fp32 [n_seq][n_heads][seq_len], natural logarithm; entries behind a sequence's end are left as they are). */
+/* Results overlap neither each other nor what the call reads (columns of a packed matrix beside each other do not).
+ * o (bf16, rows of n_heads * head_dim) and lse (fp32 [n_seq][n_heads][seq_len], natural logarithm; entries behind a sequence's end are left as they are). */
 int ah_attention_window_fwd(const ah_attention_window_t* cfg, const void* q, const void* k, const void* v, void* o, float* lse, void* hip_stream);
 /* dq, dk, dv (bf16) from the forward's inputs and results and d_o.  No atomics: the same bits every time.  workspace: device, 256-byte aligned, of the size that
  * ah_attention_window_bwd_workspace gives (which looks at the sizes only). */

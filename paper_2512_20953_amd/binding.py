@@ -532,6 +532,18 @@ def qk_norm_rope_bwd(x, gain_q, gain_k, cos_sin, dy, dx, d_gain_q, d_gain_k, wor
     _check(lib.ah_qk_norm_rope_bwd(c, px, pdy, pdx, pgq, pgk, int(beta), work, _stream(stream)))
 
 
+def _apart(written, read):
+    """Whether no two of the (begin, end) spans in `written` overlap, nor one of them and one of `read`."""
+    last_written = last = 0                    # where those that begin before end
+    for begin, end, writes in sorted([(b, e, True) for b, e in written if b < e] + [(b, e, False) for b, e in read if b < e]):
+        if begin < (last if writes else last_written):
+            return False
+        last = max(last, end)
+        if writes:
+            last_written = max(last_written, end)
+    return True
+
+
 class AdamW:
     """AdamW over a list of tensors (ah_adamw_step): bf16 or fp32 parameters with fp32 or bf16 gradients.
 
@@ -540,7 +552,8 @@ class AdamW:
     the parameters' values; or a list of such tensors.
     weight_decay: one number, or one for each tensor.
     m, v (m_scale, v_scale): lists of state tensors to go on from; without them zeroed ones are made.
-    The object keeps the tensors that it was given, and its scratch memory serves one grad_norm at a time."""
+    Tensors that a step writes overlap no other.  The object keeps the tensors that it was given, and its scratch memory serves one grad_norm at a time.
+    It makes its own on the stream that is torch's current one at its construction: steps on other streams come behind that."""
 
     def __init__(self, params, grads, betas=(0.9, 0.95), eps=1e-8, weight_decay=0.0, state_bits=32, master=None, m=None, v=None,
                  m_scale=None, v_scale=None):
@@ -590,6 +603,9 @@ class AdamW:
             if master is True:
                 for a, b in zip(self.master, params):
                     a.copy_(b.reshape(-1))
+        spans = lambda tensors: [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in tensors]  # noqa: E731
+        if not _apart(spans([*params, *self.m, *self.v, *(self.m_scale or ()), *(self.v_scale or ()), *(self.master or ())]), spans(grads)):
+            _refuse("AdamW: parameters, states, copies and gradients overlap (gradients alone may)")
         self._list = (_AdamWTensor * n)()
         for k in range(n):
             e = self._list[k]
@@ -633,7 +649,7 @@ class AdamW:
         _check(lib.ah_adamw_step(c, self._list, len(self._list), _stream(stream)))
 
     def state_values(self, m_out, v_out, stream=None):
-        """What 8-bit states stand for, into two lists of bf16 tensors (which hold them exactly)."""
+        """What 8-bit states stand for, into two lists of bf16 tensors (which hold them exactly, and do not overlap)."""
         if self.m_scale is None:
             _refuse("AdamW.state_values: the states are in fp32 (m, v)")
         n, device = len(self._list), self._norm.get_device()

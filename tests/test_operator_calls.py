@@ -2,7 +2,9 @@
 import ctypes as C
 
 import pytest
+import torch
 
+import paper_2512_20953_amd as P
 from paper_2512_20953_amd import binding as B
 
 EINVAL = 1
@@ -28,3 +30,30 @@ def test_a_window_that_32_bits_do_not_hold_is_everything():
         assert c.window == most and c.sinks == min(sinks, most)
     c = B._window_config(1, 100, 2, 2, 64, -2 ** 33 + 7, 0)
     assert c.window < 1                                           # refused, not taken for 7
+
+
+@pytest.mark.parametrize("written,read,ok", [
+    ([(0, 8), (8, 16)], [(16, 32)], True),
+    ([(0, 8), (0, 8)], [], False),                     # the same tensor twice
+    ([(0, 64), (8, 16)], [], False),                   # one inside another
+    ([(0, 8)], [(16, 32), (16, 32), (20, 24)], True),  # gradients may be shared
+    ([(24, 28)], [(0, 32)], False), ([(0, 32)], [(24, 28)], False), ([(30, 40)], [(0, 32), (8, 12)], False), ([(32, 40)], [(0, 32), (8, 12)], True),
+    ([(5, 5), (0, 8)], [(0, 0)], True),                # nothing overlaps nothing
+])
+def test_tensors_that_overlap(written, read, ok):
+    assert B._apart(written, read) == ok
+
+
+@pytest.mark.gpu
+def test_adamw_refuses_tensors_that_overlap():
+    n = 256
+    f = lambda: torch.zeros(n, device="cuda")          # noqa: E731
+    p, q, g = f(), f(), f()
+    P.AdamW([p, q], [g, g])                            # the same gradient for both
+    for params, grads, kw in (([p, p], [g, g], {}), ([p, p[8:]], [g, g[8:]], {}), ([p], [p], {}), ([p, q], [g, g], dict(m=[q, f()])),
+                              ([p], [g], dict(m=[p])), ([p], [g], dict(m=[g])), ([p, q], [g, g], dict(v=[q, f()]))):
+        with pytest.raises(P.AhError, match="overlap"):
+            P.AdamW(params, grads, **kw)
+    m = f()
+    with pytest.raises(P.AhError, match="overlap"):
+        P.AdamW([p], [g], m=[m], v=[m])
