@@ -121,6 +121,8 @@ int validate(const ah_stage_config_t* given, ah_stage_config_t* out) {
   if (hl > 65536 || F > 262144) return set_error(AH_EUNSUPPORTED, "local widths too large");
   if (c->attn_window > 0 && (long)c->microbatch_size * (hl / c->head_dim) * (c->seq_len / 128 + 8L * ((std::min(c->attn_sinks, c->seq_len) + 127) / 128)) > (1L << 23))
     return set_error(AH_EUNSUPPORTED, "microbatch_size * heads * seq_len too large for attn_window");
+  // A window of the whole sequence is causal attention, whose own kernels, without runtime masks, are faster (backward, 2 x 16 x 2048 x 128: 137 us, 168 with the window's)
+  if (c->attn_window >= c->seq_len) out->attn_window = out->attn_sinks = 0;
   return AH_OK;
 }
 

@@ -57,3 +57,23 @@ def test_adamw_refuses_tensors_that_overlap():
     m = f()
     with pytest.raises(P.AhError, match="overlap"):
         P.AdamW([p], [g], m=[m], v=[m])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("window,sinks", [(256, 0), (256, 3), (1000, 300)])
+def test_a_stage_with_a_window_of_its_whole_sequence_has_causal_attention(window, sinks):
+    results = []
+    for kw in ({}, dict(attn_window=window, attn_sinks=sinks)):
+        cfg = B.StageConfig.make(arch="llama", n_layers=1, hidden=256, n_heads=4, head_dim=64, ffn=512, seq=256, mb=2, qk_norm=1, **kw)
+        st = P.Stage(cfg)
+        g = torch.Generator().manual_seed(3)
+        st.params.copy_((0.04 * torch.randn(st.params.shape, generator=g)).bfloat16())
+        x, dy = (torch.randn(512, 256, generator=g).bfloat16().cuda() for _ in range(2))
+        y, dx = torch.empty_like(x), torch.empty_like(x)
+        st.forward(0, x, y)
+        st.zero_grads()
+        st.backward(0, dy, dx)
+        torch.cuda.synchronize()
+        results.append((y.cpu(), dx.cpu(), st.grads.cpu().clone()))
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
