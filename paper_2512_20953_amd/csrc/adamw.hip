@@ -1,6 +1,7 @@
 // Optimizer step over many tensors in few launches (declared in include/ah_ops.h): AdamW with moments in fp32 or in 8 bits, and the
 // norm of all gradients.  With fp32 states bound by HBM: every value is read and written once (100 M parameters with a master copy: 503 us, 6.0 TB/s; the norm of their
-// fp32 gradients 118).  With 8-bit states bound by vector instructions, 88 an element (202 M: 516 us, 4.8 TB/s, 451 of them at one instruction a SIMD in 4 clocks).
+// fp32 gradients 118).  With 8-bit states 80 vector instructions an element (202 M: 516 us, 4.8 TB/s; with 88 it took as
+// long, so that these do not bound it alone).
 //
 // A launch takes up to kTensors tensors, whose descriptors travel in the kernel's arguments (no copy to the device, nothing
 // that a captured graph could find changed); a block takes one chunk of one tensor and finds it by counting the tensors that
@@ -94,11 +95,15 @@ template <int BINS>
 __device__ __forceinline__ float decode(uint32_t code, int scale) {
   return __builtin_amdgcn_ldexpf(__uint_as_float(code << 20), scale - BINS);
 }
+// a code of 7 bits and a sign: as the shift of the signed byte, of which the sign and the 7 bits stay
+__device__ __forceinline__ float decode_signed(uint32_t code, int scale) {
+  return __builtin_amdgcn_ldexpf(__uint_as_float((uint32_t)((int32_t)(code << 24) >> 4) & 0x87f00000u), scale - 15);
+}
 // |x| to a code; rnd: 16 random bits
 template <int BINS>
 __device__ __forceinline__ uint32_t encode(float ax, int scale, uint32_t rnd) {
   const uint32_t u = __float_as_uint(__builtin_amdgcn_ldexpf(ax, BINS - scale));
-  return min((u + (rnd << 4)) >> 20, BINS == 15 ? 0x7eu : 0xffu);
+  return (u + (rnd << 4)) >> 20;
 }
 // scale byte of a block whose largest magnitude has these bits; a block that is not finite gets 255
 template <int BINS>
@@ -166,8 +171,7 @@ __global__ __launch_bounds__(NT) void adamw_step_kernel(Table t, Hyper h) {
     const float gr = (float)tg[j] * factor;
     float om, ov;
     if constexpr (BITS8) {
-      om = decode<15>(tm[j] & 127, sm);
-      om = tm[j] & 128 ? -om : om;
+      om = decode_signed(tm[j], sm);
       ov = decode<31>(tv[j], sv);
     } else {
       om = tm[j];
@@ -183,23 +187,29 @@ __global__ __launch_bounds__(NT) void adamw_step_kernel(Table t, Hyper h) {
   }
   typename Wide<S, V>::type om, ov;
   if constexpr (BITS8) {
-    uint32_t am = 0, av = 0;
+    uint32_t am = 0, av = 0;   // (what lies behind the tensor's end is 0 here too)
 #pragma unroll
     for (int j = 0; j < V; j++) {
-      if (j < rest) {
-        am = max(am, __float_as_uint(nm[j]) & 0x7fffffffu);
-        av = max(av, __float_as_uint(nv[j]) & 0x7fffffffu);
-      }
+      am = max(am, __float_as_uint(nm[j]) & 0x7fffffffu);
+      av = max(av, __float_as_uint(nv[j]) & 0x7fffffffu);
     }
     const int s1 = scale_of<15>(block_max(am)), s2 = scale_of<31>(block_max(av));
     const uint32_t first = (e.number + (uint32_t)base + i) * kNumber + h.seed;
 #pragma unroll
     for (int j = 0; j < V; j++) {
       const uint32_t bits = random_bits(first + j * kNumber);
-      const uint32_t cm = s1 == 255 ? 0x7f : encode<15>(fabsf(nm[j]), s1, bits & 0xffff);
-      const uint32_t cv = s2 == 255 ? 0xff : max(encode<31>(nv[j], s2, bits >> 16), nv[j] > 0.f ? 1u : 0u);
-      om[j] = (uint8_t)(cm | (__float_as_uint(nm[j]) >> 31 << 7));
-      ov[j] = (uint8_t)cv;
+      const uint32_t cm = min(encode<15>(fabsf(nm[j]), s1, bits & 0xffff), 0x7eu);
+      const uint32_t cv = encode<31>(nv[j], s2, bits >> 16), least = min(__float_as_uint(nv[j]), 1u);   // a v > 0 stays above 0
+      om[j] = (uint8_t)(cm | (__float_as_uint(nm[j]) >> 24 & 0x80));
+      ov[j] = (uint8_t)min(max(cv, least), 0xffu);
+    }
+    if (max(s1, s2) == 255) {   // a block that is not finite
+      asm volatile("");          // (a branch, no selects)
+#pragma unroll
+      for (int j = 0; j < V; j++) {
+        if (s1 == 255) om[j] |= 0x7f;
+        if (s2 == 255) ov[j] = 0xff;
+      }
     }
     if (rest && (threadIdx.x & 3) == 0) {
       e.ms[(base + i) / kBlock] = (uint8_t)s1;
@@ -287,8 +297,7 @@ __global__ __launch_bounds__(NT) void state_values_kernel(Table t, int aligned) 
   typename Wide<bf16, kValues>::type om, ov;
 #pragma unroll
   for (int j = 0; j < kValues; j++) {
-    const float x = decode<15>(cm[j] & 127, sm);
-    om[j] = (bf16)(cm[j] & 128 ? -x : x);
+    om[j] = (bf16)decode_signed(cm[j], sm);
     ov[j] = (bf16)decode<31>(cv[j], sv);
   }
   store_n<kValues, bf16>((bf16*)e.param + at, om, whole, rest);    // (the table's places for what a step writes)
