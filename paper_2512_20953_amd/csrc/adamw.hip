@@ -1,7 +1,6 @@
 // Optimizer step over many tensors in few launches (declared in include/ah_ops.h): AdamW with moments in fp32 or in 8 bits, and the
-// norm of all gradients.  With fp32 states bound by HBM: every value is read and written once (100 M parameters with a master copy: 503 us, 6.0 TB/s; the norm of their
-// fp32 gradients 118).  With 8-bit states 80 vector instructions an element (202 M: 516 us, 4.8 TB/s; with 88 it took as
-// long, so that these do not bound it alone).
+// norm of all gradients.  Bound by HBM: every value is read and written once (kernels traced, called repeatedly: 100 M parameters with fp32 states and a master copy 447 us, 6.8 TB/s;
+// 202 M with 8-bit states 460, 5.3 TB/s, where vector units have their 80 instructions an element to issue as well).
 //
 // A launch takes up to kTensors tensors, whose descriptors travel in the kernel's arguments (no copy to the device, nothing
 // that a captured graph could find changed); a block takes one chunk of one tensor and finds it by counting the tensors that
@@ -22,8 +21,8 @@ namespace {
 
 constexpr int NT = 256, kTensors = 48;
 // Elements of a lane, and of a block.  One run of 16 bytes a lane for fp32 states (two take 651 instead of 623 us for 100 M parameters with a master copy and the norm, four
-// 658); eight for states in 8 bits, of which four fill no load.
-constexpr int VEC = 4, kChunk = NT * VEC, VEC8 = 8, kChunk8 = NT * VEC8;
+// 658); eight for states in 8 bits, of which four fill no load, twice over (724 -> 692 us for 202 M with the states' values; four times 697).
+constexpr int VEC = 4, kChunk = NT * VEC, VEC8 = 8, kRuns8 = 2, kChunk8 = NT * VEC8 * kRuns8;
 constexpr int kBlock = 32;                   // elements that share a scale
 constexpr uint64_t kMaxElements = 1ull << 33, kMaxBlocks = kMaxElements / kChunk;   // of a tensor; of a launch (2^23: its threads are counted in 32 bits)
 
@@ -68,19 +67,26 @@ template <class T, int N> struct Wide {
   typedef type at __attribute__((aligned(sizeof(T) * N < 16 ? sizeof(T) * N : 16)));
 };
 
-template <int N, class T>
+// (ONCE: past the caches, for what nobody reads again before they have been overwritten.  All that the step touches: it evicts less of the gradients that the norm has just
+// read.  100 M parameters with the norm, caches overwritten before each call: 630 -> 581 us; called repeatedly 623 -> 527, as some gradients survive from call to call; the
+// norm itself reads with the caches, or 553.)
+template <int N, class T, bool ONCE = false>
 __device__ __forceinline__ typename Wide<T, N>::type load_n(const T* p, bool whole, int left) {
   typename Wide<T, N>::type r = {};
-  if (whole) return *(const typename Wide<T, N>::at*)p;
+  if (whole) {
+    if constexpr (ONCE) return __builtin_nontemporal_load((const typename Wide<T, N>::at*)p);
+    else return *(const typename Wide<T, N>::at*)p;
+  }
 #pragma unroll
   for (int j = 0; j < N; j++)
     if (j < left) r[j] = p[j];
   return r;
 }
-template <int N, class T>
+template <int N, class T, bool ONCE = false>
 __device__ __forceinline__ void store_n(T* p, typename Wide<T, N>::type r, bool whole, int left) {
   if (whole) {
-    *(typename Wide<T, N>::at*)p = r;
+    if constexpr (ONCE) __builtin_nontemporal_store(r, (typename Wide<T, N>::at*)p);
+    else *(typename Wide<T, N>::at*)p = r;
     return;
   }
 #pragma unroll
@@ -142,90 +148,95 @@ __global__ __launch_bounds__(NT) void adamw_step_kernel(Table t, Hyper h) {
   const Entry& e = t.e[k];
   constexpr int V = BITS8 ? VEC8 : VEC;
   typedef typename std::conditional<BITS8, uint8_t, float>::type S;
-  // the lane's first element is the block's first, a scalar, and a 32-bit distance
-  const uint64_t base = (uint64_t)(blockIdx.x - t.first[k]) * (NT * V);
-  const uint32_t left = (uint32_t)min(e.n - base, (uint64_t)(NT * V)), i = threadIdx.x * V;
-  const int rest = i < left ? (int)(left - i) : 0;
-  const bool whole = h.aligned && rest >= V;
-  const G* g = (const G*)e.grad + base;
-  S *m = (S*)e.m + base, *v = (S*)e.v + base;
-  P* p = (P*)e.param + base;
-  float* w = MASTER ? e.master + base : nullptr;
-  const float keep = 1.f - lr * e.wd;
-  const auto tg = load_n<V, G>(g + i, whole, rest);
-  const auto tm = load_n<V, S>(m + i, whole, rest), tv = load_n<V, S>(v + i, whole, rest);
-  typename Wide<P, V>::type tp;
-  typename Wide<float, V>::type tw;
-  if constexpr (MASTER) tw = load_n<V, float>(w + i, whole, rest);
-  else tp = load_n<V, P>(p + i, whole, rest);
-  int sm = 0, sv = 0;
-  if (BITS8 && rest) {
-    sm = e.ms[(base + i) / kBlock];
-    sv = e.vs[(base + i) / kBlock];
-  }
-  float nm[V], nv[V];
-  typename Wide<float, V>::type now;
+  constexpr int RUNS = BITS8 ? kRuns8 : 1;
+#pragma unroll 1
+  for (int run = 0; run < RUNS; run++) {
+    // the lane's first element is the block's first, a scalar, and a 32-bit distance
+    const uint64_t base = ((uint64_t)(blockIdx.x - t.first[k]) * RUNS + run) * (NT * V);
+    if (base >= e.n) return;
+    const uint32_t left = (uint32_t)min(e.n - base, (uint64_t)(NT * V)), i = threadIdx.x * V;
+    const int rest = i < left ? (int)(left - i) : 0;
+    const bool whole = h.aligned && rest >= V;
+    const G* g = (const G*)e.grad + base;
+    S *m = (S*)e.m + base, *v = (S*)e.v + base;
+    P* p = (P*)e.param + base;
+    float* w = MASTER ? e.master + base : nullptr;
+    const float keep = 1.f - lr * e.wd;
+    const auto tg = load_n<V, G, true>(g + i, whole, rest);
+    const auto tm = load_n<V, S, true>(m + i, whole, rest), tv = load_n<V, S, true>(v + i, whole, rest);
+    typename Wide<P, V>::type tp;
+    typename Wide<float, V>::type tw;
+    if constexpr (MASTER) tw = load_n<V, float, true>(w + i, whole, rest);
+    else tp = load_n<V, P, true>(p + i, whole, rest);
+    int sm = 0, sv = 0;
+    if (BITS8 && rest) {
+      sm = e.ms[(base + i) / kBlock];
+      sv = e.vs[(base + i) / kBlock];
+    }
+    float nm[V], nv[V];
+    typename Wide<float, V>::type now;
 #pragma unroll
-  for (int j = 0; j < V; j++) {
+    for (int j = 0; j < V; j++) {
 #pragma clang fp contract(off)
-    const float gr = (float)tg[j] * factor;
-    float om, ov;
+      const float gr = (float)tg[j] * factor;
+      float om, ov;
+      if constexpr (BITS8) {
+        om = decode_signed(tm[j], sm);
+        ov = decode<31>(tv[j], sv);
+      } else {
+        om = tm[j];
+        ov = tv[j];
+      }
+      nm[j] = om + h.c1 * (gr - om);
+      nv[j] = ov + h.c2 * (gr * gr - ov);
+    }
+#pragma unroll
+    for (int j = 0; j < V; j++) {
+      const float denom = __builtin_fmaf(__builtin_amdgcn_sqrtf(nv[j]), root, h.eps);
+      now[j] = __builtin_fmaf(MASTER ? tw[j] : (float)tp[j], keep, -alpha * nm[j] * __builtin_amdgcn_rcpf(denom));
+    }
+    typename Wide<S, V>::type om, ov;
     if constexpr (BITS8) {
-      om = decode_signed(tm[j], sm);
-      ov = decode<31>(tv[j], sv);
-    } else {
-      om = tm[j];
-      ov = tv[j];
-    }
-    nm[j] = om + h.c1 * (gr - om);
-    nv[j] = ov + h.c2 * (gr * gr - ov);
-  }
-#pragma unroll
-  for (int j = 0; j < V; j++) {
-    const float denom = __builtin_fmaf(__builtin_amdgcn_sqrtf(nv[j]), root, h.eps);
-    now[j] = __builtin_fmaf(MASTER ? tw[j] : (float)tp[j], keep, -alpha * nm[j] * __builtin_amdgcn_rcpf(denom));
-  }
-  typename Wide<S, V>::type om, ov;
-  if constexpr (BITS8) {
-    uint32_t am = 0, av = 0;   // (what lies behind the tensor's end is 0 here too)
-#pragma unroll
-    for (int j = 0; j < V; j++) {
-      am = max(am, __float_as_uint(nm[j]) & 0x7fffffffu);
-      av = max(av, __float_as_uint(nv[j]) & 0x7fffffffu);
-    }
-    const int s1 = scale_of<15>(block_max(am)), s2 = scale_of<31>(block_max(av));
-    const uint32_t first = (e.number + (uint32_t)base + i) * kNumber + h.seed;
-#pragma unroll
-    for (int j = 0; j < V; j++) {
-      const uint32_t bits = random_bits(first + j * kNumber);
-      const uint32_t cm = min(encode<15>(fabsf(nm[j]), s1, bits & 0xffff), 0x7eu);
-      const uint32_t cv = encode<31>(nv[j], s2, bits >> 16), least = min(__float_as_uint(nv[j]), 1u);   // a v > 0 stays above 0
-      om[j] = (uint8_t)(cm | (__float_as_uint(nm[j]) >> 24 & 0x80));
-      ov[j] = (uint8_t)min(max(cv, least), 0xffu);
-    }
-    if (max(s1, s2) == 255) {   // a block that is not finite
-      asm volatile("");          // (a branch, no selects)
+      uint32_t am = 0, av = 0;   // (what lies behind the tensor's end is 0 here too)
 #pragma unroll
       for (int j = 0; j < V; j++) {
-        if (s1 == 255) om[j] |= 0x7f;
-        if (s2 == 255) ov[j] = 0xff;
+        am = max(am, __float_as_uint(nm[j]) & 0x7fffffffu);
+        av = max(av, __float_as_uint(nv[j]) & 0x7fffffffu);
       }
-    }
-    if (rest && (threadIdx.x & 3) == 0) {
-      e.ms[(base + i) / kBlock] = (uint8_t)s1;
-      e.vs[(base + i) / kBlock] = (uint8_t)s2;
-    }
-  } else {
+      const int s1 = scale_of<15>(block_max(am)), s2 = scale_of<31>(block_max(av));
+      const uint32_t first = (e.number + (uint32_t)base + i) * kNumber + h.seed;
 #pragma unroll
-    for (int j = 0; j < V; j++) { om[j] = nm[j]; ov[j] = nv[j]; }
+      for (int j = 0; j < V; j++) {
+        const uint32_t bits = random_bits(first + j * kNumber);
+        const uint32_t cm = min(encode<15>(fabsf(nm[j]), s1, bits & 0xffff), 0x7eu);
+        const uint32_t cv = encode<31>(nv[j], s2, bits >> 16), least = min(__float_as_uint(nv[j]), 1u);   // a v > 0 stays above 0
+        om[j] = (uint8_t)(cm | (__float_as_uint(nm[j]) >> 24 & 0x80));
+        ov[j] = (uint8_t)min(max(cv, least), 0xffu);
+      }
+      if (max(s1, s2) == 255) {   // a block that is not finite
+        asm volatile("");          // (a branch, no selects)
+#pragma unroll
+        for (int j = 0; j < V; j++) {
+          if (s1 == 255) om[j] |= 0x7f;
+          if (s2 == 255) ov[j] = 0xff;
+        }
+      }
+      if (rest && (threadIdx.x & 3) == 0) {
+        e.ms[(base + i) / kBlock] = (uint8_t)s1;
+        e.vs[(base + i) / kBlock] = (uint8_t)s2;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; j++) { om[j] = nm[j]; ov[j] = nv[j]; }
+    }
+    store_n<V, S, true>(m + i, om, whole, rest);
+    store_n<V, S, true>(v + i, ov, whole, rest);
+    if constexpr (MASTER) store_n<V, float, true>(w + i, now, whole, rest);
+    typename Wide<P, V>::type np;
+#pragma unroll
+    for (int j = 0; j < V; j++) np[j] = (P)now[j];
+    store_n<V, P, true>(p + i, np, whole, rest);
   }
-  store_n<V, S>(m + i, om, whole, rest);
-  store_n<V, S>(v + i, ov, whole, rest);
-  if constexpr (MASTER) store_n<V, float>(w + i, now, whole, rest);
-  typename Wide<P, V>::type np;
-#pragma unroll
-  for (int j = 0; j < V; j++) np[j] = (P)now[j];
-  store_n<V, P>(p + i, np, whole, rest);
 }
 
 // ---- the norm of all gradients: a partial sum in fp64 for each of a fixed number of blocks, which a second launch adds up in order.  (Added up by the
