@@ -77,3 +77,23 @@ def test_a_stage_with_a_window_of_its_whole_sequence_has_causal_attention(window
         results.append((y.cpu(), dx.cpu(), st.grads.cpu().clone()))
     for a, b in zip(*results):
         assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n_seq,S,W,d", [(7, 1, 123, 64), (3, 1, 4, 128), (2, 200, 1, 64), (1, 130, 1, 128)])
+def test_a_query_that_sees_itself_alone_has_no_gradient(n_seq, S, W, d):
+    """P = 1, o = v, so that dS = dO v - sum(o dO) is 0: what is left is the rounding of two fp32 sums of d products, each at most d 2^-24 of the sum of their
+    magnitudes; P is 1 within 2^-10 (the exponent's argument, below 2^7 in magnitude, is formed from three roundings), dS is rounded by 2^-8 more, and a key has 3 queries: 2 covers both factors."""
+    nh, nk, T = 9, 3, n_seq * S
+    g = torch.Generator().manual_seed(S + d)
+    q, k, v, do = (torch.randn(T, n * d, generator=g).bfloat16().cuda() for n in (nh, nk, nk, nh))
+    o, lse = torch.empty_like(q), torch.empty(n_seq, nh, S, device="cuda")
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    work = torch.empty(P.attention_window_bwd_workspace(n_seq, S, nh, nk, d, W), dtype=torch.uint8, device="cuda")
+    P.attention_window_fwd(q, k, v, o, lse, n_seq, S, nh, nk, d, W)
+    P.attention_window_bwd(q, k, v, o, lse, do, dq, dk, dv, work, n_seq, S, nh, nk, d, W)
+    heads = lambda t, n: t.double().cpu().reshape(T, n, d)                    # noqa: E731
+    assert torch.equal(heads(o, nh), heads(v, nk).repeat_interleave(nh // nk, 1))
+    room = 2 * 2 * d * 2.0 ** -24 * (heads(o, nh) * heads(do, nh)).abs().sum(-1, keepdim=True) / d ** 0.5
+    assert (heads(dq, nh).abs() <= room * heads(k, nk).repeat_interleave(nh // nk, 1).abs()).all()
+    assert (heads(dk, nk).abs() <= (room * heads(q, nh).abs()).reshape(T, nk, nh // nk, d).sum(2)).all()
