@@ -49,8 +49,10 @@ typedef struct {
  * of e4m3); v: 5 bits of exponent, 3 of mantissa; both with gradual underflow below their last binade.  The step itself uses the
  * unrounded moments.  They are rounded to a neighbouring code at random, with the probability that keeps their expectation (a
  * step changes v by at most 1 - beta2 of itself, less than half the distance of two codes: rounded to nearest it would never
- * move); the random bits are a function of `seed` and the element's number alone (tensors are numbered one behind the other,
- * each from a multiple of 64 on; the bits repeat after 2^32 elements).  A v > 0 never becomes 0 (m / sqrt(v) would have no
+ * move); the random bits are a function of `seed` plus the step's number (modulo 2^32) and of the element's number alone (tensors are numbered
+ * one behind the other, each from a multiple of 64 on; the bits repeat after 2^32 elements).  They have to differ from step to step: where an element is
+ * rounded by the same ones every time, its moments stand still.  A captured step therefore needs `step_dev` (and its owner counts that up
+ * between replays); without it the call is refused.  A v > 0 never becomes 0 (m / sqrt(v) would have no
  * bound).  A block whose moment is infinite or NaN stays so, as a single 32-bit state would.  Zero bytes stand for zeros. */
 typedef struct {
   uint32_t struct_size;   /* sizeof(ah_adamw_t), checked */
@@ -61,7 +63,7 @@ typedef struct {
   const float* lr_dev;    /* device, optional: read by the kernel in place of lr ... */
   const int32_t* step_dev;   /* ... and of step (at least 1): a captured step can be replayed with other values */
   const float* grad_norm; /* device, optional: the two values that ah_grad_norm left.  The second is the factor above; NaN leaves everything as it was. */
-  uint32_t seed;          /* of the random rounding: another one for every step */
+  uint32_t seed;          /* of the random rounding: the step's number is added to it, so one value serves all steps */
   uint32_t reserved;      /* 0 */
 } ah_adamw_t;
 

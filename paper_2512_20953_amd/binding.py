@@ -628,10 +628,12 @@ class AdamW:
         _check(lib.ah_grad_norm(self._list, len(self._list), self._cfg.grad_type, float(max_norm), self._norm.data_ptr(), self._norm_work.data_ptr(), _stream(stream)))
         return self._norm
 
-    def step(self, lr, step, grad_norm=None, seed=0, stream=None):
+    def step(self, lr, step, grad_norm=None, seed=None, stream=None):
         """One step, number `step` (from 1 on).  lr: a number, or an fp32 tensor of one element on the device; step: likewise, int32 (a captured
-        step reads them anew when it is replayed).  grad_norm: what grad_norm() gave: gradients are multiplied by its factor, and where that is NaN
-        nothing changes.  seed: of the rounding of 8-bit states, another one for every step."""
+        step reads them anew when it is replayed; one with 8-bit states needs the step's number there).  grad_norm: what grad_norm() gave: gradients are
+        multiplied by its factor, and where that is NaN nothing changes.  seed: of the random rounding of 8-bit states, which has to differ from step to step.
+        None: it goes by the step's number.  A number beside a `step` on the device: by their sum.  A number beside a number: by that seed alone, and
+        the caller gives another one for every step."""
         c = self._cfg
         _on_device("AdamW: parameters", self._norm)
         c.lr_dev = c.step_dev = c.grad_norm = None
@@ -645,7 +647,8 @@ class AdamW:
             c.step = step
         if grad_norm is not None:
             c.grad_norm = _dense("AdamW.step: grad_norm", grad_norm, _F32, 2)
-        c.seed = seed & 0xFFFFFFFF
+        # (the library adds the step's number)
+        c.seed = 0 if seed is None else (seed if c.step_dev else seed - step) & 0xFFFFFFFF
         _check(lib.ah_adamw_step(c, self._list, len(self._list), _stream(stream)))
 
     def state_values(self, m_out, v_out, stream=None):

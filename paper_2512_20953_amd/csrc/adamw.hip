@@ -49,7 +49,7 @@ struct Hyper {
   int64_t step;
   const float *lr_dev, *grad_norm;
   const int32_t* step_dev;
-  uint32_t seed;
+  uint32_t seed;              // (without step_dev the step's number is in it already)
   int aligned;                // every pointer of the launch allows vector access
 };
 
@@ -138,8 +138,11 @@ __global__ __launch_bounds__(NT) void adamw_step_kernel(Table t, Hyper h) {
     if (factor != factor) return;
   }
   float lr = h.lr, alpha = h.alpha, root = h.root;
+  uint32_t seed = h.seed;
   if (h.lr_dev || h.step_dev) {
-    const double step = h.step_dev ? (double)max(*h.step_dev, 1) : (double)h.step;
+    const int64_t number = h.step_dev ? (int64_t)max(*h.step_dev, 1) : h.step;
+    const double step = (double)number;
+    if (h.step_dev) seed += (uint32_t)number;   // a replay rounds by other bits than the one before
     if (h.lr_dev) lr = *h.lr_dev;
     alpha = (float)((double)lr / -expm1(step * h.log_b1));
     root = (float)(1.0 / sqrt(-expm1(step * h.log_b2)));
@@ -204,7 +207,7 @@ __global__ __launch_bounds__(NT) void adamw_step_kernel(Table t, Hyper h) {
         av = max(av, __float_as_uint(nv[j]) & 0x7fffffffu);
       }
       const int s1 = scale_of<15>(block_max(am)), s2 = scale_of<31>(block_max(av));
-      const uint32_t first = (e.number + (uint32_t)base + i) * kNumber + h.seed;
+      const uint32_t first = (e.number + (uint32_t)base + i) * kNumber + seed;
 #pragma unroll
       for (int j = 0; j < V; j++) {
         const uint32_t bits = random_bits(first + j * kNumber);
@@ -359,6 +362,17 @@ bool vectors(const ah_adamw_tensor_t& x, const Widths& w, int n) {
   return !(bad(x.grad, w.g) || bad(x.param, w.p) || bad(x.m, w.s) || bad(x.v, w.s) || bad(x.master, 4));
 }
 
+// Whether the stream is being captured (the legacy default stream cannot be, nor be asked while another is)
+bool captures(hipStream_t s) {
+  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+  if (!s) return false;
+  if (hipStreamIsCapturing(s, &status) != hipSuccess) {
+    (void)hipGetLastError();
+    return false;
+  }
+  return status != hipStreamCaptureStatusNone;
+}
+
 int check_list(const char* who, const ah_adamw_tensor_t* x, int n) {
   if (n < 0 || (n > 0 && !x)) return set_error(AH_EINVAL, "%s: bad tensor list", who);
   for (int i = 0; i < n; i++)
@@ -395,6 +409,8 @@ extern "C" int ah_adamw_step(const ah_adamw_t* c, const ah_adamw_tensor_t* x, in
   }
   if (master && p32) return set_error(AH_EINVAL, "ah_adamw_step: master copies go with bf16 parameters");
   if (!any) return AH_OK;
+  if (bits8 && !c->step_dev && captures((hipStream_t)stream))
+    return set_error(AH_EINVAL, "ah_adamw_step: a captured step with 8-bit states needs step_dev: its replays would round by the same random bits every time");
   Hyper h = {};
   h.c1 = (float)(1 - c->beta1); h.c2 = (float)(1 - c->beta2); h.eps = (float)c->eps; h.lr = (float)c->lr;
   h.log_b1 = std::log(c->beta1); h.log_b2 = std::log(c->beta2);
@@ -403,7 +419,8 @@ extern "C" int ah_adamw_step(const ah_adamw_t* c, const ah_adamw_tensor_t* x, in
     h.alpha = (float)(c->lr / -std::expm1((double)c->step * h.log_b1));
     h.root = (float)(1.0 / std::sqrt(-std::expm1((double)c->step * h.log_b2)));
   }
-  h.lr_dev = c->lr_dev; h.step_dev = c->step_dev; h.grad_norm = c->grad_norm; h.seed = c->seed; h.aligned = aligned;
+  h.lr_dev = c->lr_dev; h.step_dev = c->step_dev; h.grad_norm = c->grad_norm; h.aligned = aligned;
+  h.seed = c->seed + (c->step_dev ? 0u : (uint32_t)c->step);
   const hipError_t e = by_tables(x, n, bits8 ? kChunk8 : kChunk, nullptr, nullptr, [&](const Table& t, uint32_t blocks) {
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(NT), 0, (hipStream_t)stream, t, h); };
     auto by_state = [&](auto p, auto g, auto has_master) {
