@@ -147,6 +147,7 @@ __global__ __launch_bounds__(NT) void adamw_step_kernel(Table t, Hyper h) {
     alpha = (float)((double)lr / -expm1(step * h.log_b1));
     root = (float)(1.0 / sqrt(-expm1(step * h.log_b2)));
   }
+  const float root_low = root * 0x1p-16f;
   const int k = find_tensor(t, blockIdx.x);
   const Entry& e = t.e[k];
   constexpr int V = BITS8 ? VEC8 : VEC;
@@ -195,7 +196,9 @@ __global__ __launch_bounds__(NT) void adamw_step_kernel(Table t, Hyper h) {
     }
 #pragma unroll
     for (int j = 0; j < V; j++) {
-      const float denom = __builtin_fmaf(__builtin_amdgcn_sqrtf(nv[j]), root, h.eps);
+      // (the root instruction takes a subnormal for 0, which with a tiny eps would leave nothing to divide by: those are scaled up for it)
+      const bool low = nv[j] < FLT_MIN;
+      const float denom = __builtin_fmaf(__builtin_amdgcn_sqrtf(nv[j] * (low ? 0x1p32f : 1.f)), low ? root_low : root, h.eps);
       now[j] = __builtin_fmaf(MASTER ? tw[j] : (float)tp[j], keep, -alpha * nm[j] * __builtin_amdgcn_rcpf(denom));
     }
     typename Wide<S, V>::type om, ov;
