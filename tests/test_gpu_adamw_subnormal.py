@@ -31,7 +31,7 @@ def test_states_in_32_bits(eps, dtype):
         _check(p, m, v, step, eps)
 
 
-@pytest.mark.parametrize("eps", [1e-37, 1e-30])
+@pytest.mark.parametrize("eps", [1e-37, 1e-30, 8e-12, 8.2e-12, 1e-8])   # (from 8.13e-12 on subnormals are below half a unit of it)
 def test_states_in_8_bits(eps):
     n = 640
     grad = torch.full((n,), 1e-19, device=DEV)
