@@ -18,6 +18,11 @@ PARAM_INDEX = {"ln1_g": 0, "ln1_b": 1, "wqkv": 2, "bqkv": 3, "wo": 4, "bo": 5,
 PARAM_ALIASES = {"wgu": "w1", "wd": "w2"}
 
 
+def _clamped(n):
+    """A number for an int32 field, which would keep the lowest 32 bits of a larger one: a window, say, above that stands for all positions, what is negative is refused."""
+    return max(-1, min(n, (1 << 31) - 1))
+
+
 class AhError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__("ah status %d: %s" % (status, msg))
@@ -38,7 +43,7 @@ class StageConfig(C.Structure):
              attn_window=0, attn_sinks=0, qk_norm=0):
         return cls(C.sizeof(cls), _ARCH[arch], n_layers, hidden, n_heads, head_dim,
                    ffn, tp, tp_rank, seq, mb, n_mb, max_in_flight, recompute, wgrad_group, norm_eps, rope_base, residual_fp32,
-                   attn_window, attn_sinks, qk_norm)
+                   _clamped(attn_window), _clamped(attn_sinks), qk_norm)
 
 
 class _Sizes(C.Structure):
@@ -427,8 +432,8 @@ def _rows(what, t, rows, cols):
 
 
 def _window_config(n_seq, seq_len, nh, nh_kv, d, window, sinks):
-    if not (0 <= window < 1 << 31 and 0 <= sinks < 1 << 31):    # (a field keeps the lowest 32 bits; the library refuses what is negative)
-        window, sinks = max(-1, min(window, (1 << 31) - 1)), max(-1, min(sinks, (1 << 31) - 1))
+    if not (0 <= window < 1 << 31 and 0 <= sinks < 1 << 31):
+        window, sinks = _clamped(window), _clamped(sinks)
     return _WindowConfig(_WINDOW_SIZE, n_seq, seq_len, nh, nh_kv, d, window, sinks)
 
 
