@@ -432,9 +432,10 @@ def _rows(what, t, rows, cols):
 
 
 def _window_config(n_seq, seq_len, nh, nh_kv, d, window, sinks):
-    if not (0 <= window < 1 << 31 and 0 <= sinks < 1 << 31):
-        window, sinks = _clamped(window), _clamped(sinks)
-    return _WindowConfig(_WINDOW_SIZE, n_seq, seq_len, nh, nh_kv, d, window, sinks)
+    sizes = n_seq, seq_len, nh, nh_kv, d, window, sinks
+    if (n_seq | seq_len | nh | nh_kv | d | window | sinks) >> 31:    # one of them does not fit
+        sizes = map(_clamped, sizes)
+    return _WindowConfig(_WINDOW_SIZE, *sizes)
 
 
 def _window_args(c, q, k, v, o, lse, offsets):
@@ -505,6 +506,8 @@ def _qk_args(x, other, gain_q, gain_k, cos_sin, seq_len, nh, nh_kv, d, eps, posi
             _refuse("cos_sin is %s, wanted [n_pos, %d, 2]", tuple(cos_sin.shape), d // 2)
         if positions is not None:
             pos = _dense("positions", positions, _I32, T)
+    if (seq_len | nh | nh_kv | d) >> 31:
+        seq_len, nh, nh_kv, d = map(_clamped, (seq_len, nh, nh_kv, d))
     return _QkNormConfig(_QK_SIZE, T, seq_len, nh, nh_kv, d, n_pos, eps, ld_x, ld_o, 0, pq, pk, table, pos), px, po
 
 
@@ -519,7 +522,7 @@ def qk_norm_rope_fwd(x, gain_q, gain_k, cos_sin, y, seq_len, nh, nh_kv, d, eps=1
 def qk_norm_rope_bwd_workspace(rows, nh, nh_kv, d):
     """Bytes of scratch memory that qk_norm_rope_bwd takes."""
     n = C.c_uint64()
-    _check(lib.ah_qk_norm_rope_bwd_workspace(_QkNormConfig(_QK_SIZE, rows, 0, nh, nh_kv, d), n))
+    _check(lib.ah_qk_norm_rope_bwd_workspace(_QkNormConfig(_QK_SIZE, *map(_clamped, (rows, 0, nh, nh_kv, d))), n))
     return n.value
 
 

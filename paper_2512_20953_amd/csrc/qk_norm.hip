@@ -19,7 +19,7 @@ using namespace ah;
 
 namespace {
 
-constexpr int NT = 256, NW = NT / 64;
+constexpr int NT = 256, NW = NT / 64, kMaxRows = 1 << 25;
 // Heads of a lane in flight together (at those sizes 1, 2, 4: 30.4, 28.6, 29.9 us; backward 1, 2, 3: 66 to 69, 59, 68), and the rows of partial sums behind the
 // gains' gradients: three blocks a CU, as many as 160 registers allow (512, 768, 1024: 61, 59, 65 us)
 constexpr int kFwdPasses = 2, kBwdPasses = 2;
@@ -226,7 +226,7 @@ int check(const char* who, const ah_qk_norm_rope_t* c) {
   if (c->head_dim != 64 && c->head_dim != 128) return set_error(AH_EUNSUPPORTED, "%s: head_dim %d: only 64 and 128 are supported", who, c->head_dim);
   if (c->rows < 0 || c->n_heads < 0 || c->n_kv_heads < 0 || c->n_heads > 65536 || c->n_kv_heads > 65536 || c->n_heads + c->n_kv_heads == 0)
     return set_error(AH_EINVAL, "%s: need rows >= 0 and 1 .. 65536 heads", who);
-  if (c->rows > (1 << 25)) return set_error(AH_EUNSUPPORTED, "%s: more than 2^25 rows", who);
+  if (c->rows > kMaxRows) return set_error(AH_EUNSUPPORTED, "%s: more than 2^25 rows", who);
   if (!(c->eps >= FLT_MIN) || !std::isfinite(c->eps)) return set_error(AH_EINVAL, "%s: eps must be finite and at least 2^-126", who);
   if ((c->n_heads && !c->gain_q) || (c->n_kv_heads && !c->gain_k)) return set_error(AH_EINVAL, "%s: a gain is NULL", who);
   if (off16(c->gain_q) || off16(c->gain_k) || off16(c->cos_sin) || ((uintptr_t)c->positions & 3)) return set_error(AH_EINVAL, "%s: gains and cos_sin must be 16-byte aligned, positions 4-byte", who);
@@ -335,6 +335,7 @@ extern "C" int ah_qk_norm_rope_bwd_workspace(const ah_qk_norm_rope_t* c, uint64_
   if (!c || c->struct_size != sizeof(ah_qk_norm_rope_t) || (c->head_dim != 64 && c->head_dim != 128) || c->rows < 0 || c->n_heads < 0 || c->n_kv_heads < 0 ||
       c->n_heads > 65536 || c->n_kv_heads > 65536)
     return set_error(AH_EINVAL, "ah_qk_norm_rope_bwd_workspace: bad configuration");
+  if (c->rows > kMaxRows) return set_error(AH_EUNSUPPORTED, "ah_qk_norm_rope_bwd_workspace: more than 2^25 rows");
   *bytes = (uint64_t)bwd_blocks(c) * 2 * c->head_dim * sizeof(float);
   return AH_OK;
 }

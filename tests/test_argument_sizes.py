@@ -20,3 +20,31 @@ def test_a_stage_window_below_zero_is_refused():
     for kw in (dict(attn_window=-2 ** 33 + 7), dict(attn_window=7, attn_sinks=-2 ** 33 + 7)):
         with pytest.raises(P.AhError):
             B.query_sizes(_stage(**kw))
+
+
+@pytest.mark.parametrize("kw", [dict(n_seq=2 ** 32 + 1), dict(seq_len=2 ** 32 + 64), dict(nh=2 ** 32 + 4, nh_kv=2 ** 32 + 4), dict(d=2 ** 32 + 64), dict(seq_len=-2 ** 32 + 64)])
+def test_windowed_attention_refuses_sizes_that_its_fields_do_not_hold(kw):
+    with pytest.raises(P.AhError):
+        P.attention_window_bwd_workspace(**{**dict(n_seq=1, seq_len=64, nh=4, nh_kv=4, d=64, window=8, sinks=2), **kw})
+
+
+@pytest.mark.parametrize("kw", [dict(rows=2 ** 32 + 5), dict(rows=-2 ** 32 + 5), dict(nh=2 ** 32 + 5), dict(nh_kv=2 ** 32 + 5), dict(d=2 ** 32 + 64)])
+def test_norms_refuse_sizes_that_their_fields_do_not_hold(kw):
+    with pytest.raises(P.AhError):
+        P.qk_norm_rope_bwd_workspace(**{**dict(rows=5, nh=2, nh_kv=2, d=64), **kw})
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("seq_len", [2 ** 31, 2 ** 32, 2 ** 32 + 5, 2 ** 63])
+def test_a_sequence_longer_than_all_rows_has_their_positions(seq_len):
+    import torch
+    T, d = 20, 64
+    g = torch.Generator().manual_seed(1)
+    x = torch.randn(T, 2 * d, generator=g).bfloat16().cuda()
+    gain = torch.ones(d, dtype=torch.bfloat16, device="cuda")
+    table = torch.empty(T, d // 2, 2, device="cuda")
+    P.rope_table(table, d)
+    y, want = torch.empty_like(x), torch.empty_like(x)
+    P.qk_norm_rope_fwd(x, gain, gain, table, want, T, 1, 1, d)
+    P.qk_norm_rope_fwd(x, gain, gain, table, y, seq_len, 1, 1, d)
+    assert torch.equal(y, want)
