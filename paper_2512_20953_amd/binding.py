@@ -529,6 +529,8 @@ def qk_norm_rope_bwd_workspace(rows, nh, nh_kv, d):
 def qk_norm_rope_bwd(x, gain_q, gain_k, cos_sin, dy, dx, d_gain_q, d_gain_k, workspace, seq_len, nh, nh_kv, d, eps=1e-6, positions=None, beta=0,
                      stream=None):
     """dx from x and dy (dx may be either), and d_gain = beta * d_gain + the gain's gradient (fp32 [d]).  workspace: uint8, qk_norm_rope_bwd_workspace(...) bytes."""
+    if beta not in (0, 1):
+        _refuse("qk_norm_rope_bwd: beta %s: 0 or 1", beta)
     c, px, pdy = _qk_args(x, dy, gain_q, gain_k, cos_sin, seq_len, nh, nh_kv, d, eps, positions)
     pdx, c.ld_dx = _rows("dx", dx, c.rows, (nh + nh_kv) * d)
     pgq = _dense("d_gain_q", d_gain_q, _F32, d) if nh else None

@@ -48,3 +48,17 @@ def test_a_sequence_longer_than_all_rows_has_their_positions(seq_len):
     P.qk_norm_rope_fwd(x, gain, gain, table, want, T, 1, 1, d)
     P.qk_norm_rope_fwd(x, gain, gain, table, y, seq_len, 1, 1, d)
     assert torch.equal(y, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("beta", [0.5, 0.99, -0.5, 2, 2 ** 32, float("nan")])
+def test_norms_add_to_their_gains_gradients_or_not(beta):
+    import torch
+    T, d = 4, 64
+    x = torch.ones(T, 2 * d, dtype=torch.bfloat16, device="cuda")
+    gain = torch.ones(d, dtype=torch.bfloat16, device="cuda")
+    dx, dg = torch.full_like(x, 7), torch.full((2, d), 3.0, device="cuda")
+    work = torch.empty(P.qk_norm_rope_bwd_workspace(T, 1, 1, d), dtype=torch.uint8, device="cuda")
+    with pytest.raises(P.AhError):
+        P.qk_norm_rope_bwd(x, gain, gain, None, x, dx, dg[0], dg[1], work, T, 1, 1, d, beta=beta)
+    assert (dx == 7).all() and (dg == 3).all()
