@@ -133,9 +133,9 @@ typedef struct {
   const int32_t* positions;    /* device [rows], optional; a row whose position is outside [0, n_pos) comes out as NaN */
 } ah_qk_norm_rope_t;
 
-/* y may be x (each element is read before it is written). */
+/* y may be x with the same row stride (each element is read before it is written); else it overlaps nothing that the call reads. */
 int ah_qk_norm_rope_fwd(const ah_qk_norm_rope_t* cfg, const void* x, void* y, void* hip_stream);
-/* dx (bf16) from x and dy; dx may be dy or x.  d_gain_q, d_gain_k (fp32 [head_dim]) = beta * themselves + the gains' gradients, beta in {0, 1}: sums in
+/* dx (bf16) from x and dy; dx may be dy or x with the same row stride.  d_gain_q, d_gain_k (fp32 [head_dim]) = beta * themselves + the gains' gradients, beta in {0, 1}: sums in
  * an order that depends on the sizes alone.  Either may be NULL where there are no such heads.  workspace: device, 16-byte aligned, of the size that
  * ah_qk_norm_rope_bwd_workspace gives. */
 int ah_qk_norm_rope_bwd(const ah_qk_norm_rope_t* cfg, const void* x, const void* dy, void* dx, float* d_gain_q, float* d_gain_k, int beta,

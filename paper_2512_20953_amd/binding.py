@@ -513,7 +513,7 @@ def _qk_args(x, other, gain_q, gain_k, cos_sin, seq_len, nh, nh_kv, d, eps, posi
 
 def qk_norm_rope_fwd(x, gain_q, gain_k, cos_sin, y, seq_len, nh, nh_kv, d, eps=1e-6, positions=None, stream=None):
     """RMS norm of every head with its gain, then the rotation (ah_qk_norm_rope_fwd).  x, y: [T, (nh + nh_kv) * d], query heads then key heads, rows at
-    any distance (the first columns of a packed projection); y may be x.  cos_sin: see rope_table; None: no rotation.  positions: int32 [T], without them
+    any distance (the first columns of a packed projection); y may be x, its rows as far apart.  cos_sin: see rope_table; None: no rotation.  positions: int32 [T], without them
     row t has position t % seq_len."""
     c, px, py = _qk_args(x, y, gain_q, gain_k, cos_sin, seq_len, nh, nh_kv, d, eps, positions)
     _check(lib.ah_qk_norm_rope_fwd(c, px, py, _stream(stream)))
@@ -528,7 +528,7 @@ def qk_norm_rope_bwd_workspace(rows, nh, nh_kv, d):
 
 def qk_norm_rope_bwd(x, gain_q, gain_k, cos_sin, dy, dx, d_gain_q, d_gain_k, workspace, seq_len, nh, nh_kv, d, eps=1e-6, positions=None, beta=0,
                      stream=None):
-    """dx from x and dy (dx may be either), and d_gain = beta * d_gain + the gain's gradient (fp32 [d]).  workspace: uint8, qk_norm_rope_bwd_workspace(...) bytes."""
+    """dx from x and dy (dx may be either, row for row), and d_gain = beta * d_gain + the gain's gradient (fp32 [d]).  workspace: uint8, qk_norm_rope_bwd_workspace(...) bytes."""
     if beta not in (0, 1):
         _refuse("qk_norm_rope_bwd: beta %s: 0 or 1", beta)
     c, px, pdy = _qk_args(x, dy, gain_q, gain_k, cos_sin, seq_len, nh, nh_kv, d, eps, positions)

@@ -241,6 +241,9 @@ int check(const char* who, const ah_qk_norm_rope_t* c) {
   return AH_OK;
 }
 
+// Results in the place of what a call reads: row for row only
+bool shifted(const void* in, size_t ld_in, const QkArgs& a) { return a.out == in && a.T > 1 && ld_in != a.ld_out; }
+
 QkArgs args(const ah_qk_norm_rope_t* c, const void* x, const void* dy, void* out, int64_t ld_out, float* part) {
   const size_t width = (size_t)(c->n_heads + c->n_kv_heads) * c->head_dim;
   QkArgs a = {};
@@ -327,6 +330,7 @@ extern "C" int ah_qk_norm_rope_fwd(const ah_qk_norm_rope_t* c, const void* x, vo
   if (c->rows == 0) return AH_OK;
   if (!x || !y || off16(x) || off16(y)) return set_error(AH_EINVAL, "ah_qk_norm_rope_fwd: x or y is NULL or not 16-byte aligned");
   const QkArgs a = args(c, x, nullptr, y, c->ld_y, nullptr);
+  if (shifted(x, a.ld_x, a)) return set_error(AH_EINVAL, "ah_qk_norm_rope_fwd: y in the place of x needs x's row stride");
   return hip_status(run_fwd(a, c->head_dim, (hipStream_t)stream), "ah_qk_norm_rope_fwd");
 }
 
@@ -351,6 +355,7 @@ extern "C" int ah_qk_norm_rope_bwd(const ah_qk_norm_rope_t* c, const void* x, co
   const int blocks = bwd_blocks(c), d = c->head_dim;
   float* part = (float*)workspace;
   const QkArgs a = args(c, x, dy, dx, c->ld_dx, part);
+  if (shifted(x, a.ld_x, a) || shifted(dy, a.ld_y, a)) return set_error(AH_EINVAL, "ah_qk_norm_rope_bwd: dx in the place of x or dy needs its row stride");
   hipError_t e = run_bwd(a, d, blocks, (hipStream_t)stream);   // (no rows: writes zeros)
   if (e == hipSuccess) {
     FoldList f = {};

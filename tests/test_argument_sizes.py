@@ -62,3 +62,13 @@ def test_norms_add_to_their_gains_gradients_or_not(beta):
     with pytest.raises(P.AhError):
         P.qk_norm_rope_bwd(x, gain, gain, None, x, dx, dg[0], dg[1], work, T, 1, 1, d, beta=beta)
     assert (dx == 7).all() and (dg == 3).all()
+
+
+def test_norms_in_place_go_row_for_row():
+    """Rows written at another distance than they are read would overwrite rows that are still to be read (made-up addresses: a call that is not refused reaches no device here)."""
+    c = dict(struct_size=B._QK_SIZE, rows=10, seq_len=5, n_heads=4, n_kv_heads=2, head_dim=64, n_pos=5, eps=1e-6, gain_q=256, gain_k=256)
+    fwd = lambda **kw: B.lib.ah_qk_norm_rope_fwd(B._QkNormConfig(**c, **kw), 256, 256, None)  # noqa: E731
+    bwd = lambda x, dy, dx, **kw: B.lib.ah_qk_norm_rope_bwd(B._QkNormConfig(**c, **kw), x, dy, dx, 256, 256, 0, 256, None)  # noqa: E731
+    assert fwd(ld_x=392) == fwd(ld_y=392) == fwd(ld_x=392, ld_y=400) == 1
+    assert bwd(256, 512, 256, ld_x=392) == bwd(256, 512, 256, ld_dx=392) == bwd(512, 256, 256, ld_y=392) == bwd(512, 256, 256, ld_dx=392) == 1
+    assert b"stride" in B.lib.ah_last_error()
