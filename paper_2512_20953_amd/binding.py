@@ -612,7 +612,7 @@ class AdamW:
             self.master = state("master", None if master is True else master, _F32, 1)
             if master is True:
                 for a, b in zip(self.master, params):
-                    a.copy_(b.reshape(-1))
+                    a.copy_(b.detach().reshape(-1))    # (the copies are no part of a graph of b's)
         spans = lambda tensors: [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in tensors]  # noqa: E731
         if not _apart(spans([*params, *self.m, *self.v, *(self.m_scale or ()), *(self.v_scale or ()), *(self.master or ())]), spans(grads)):
             _refuse("AdamW: parameters, states, copies and gradients overlap (gradients alone may)")
