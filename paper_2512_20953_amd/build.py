@@ -17,7 +17,8 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-tar
 # maximum (a third of the vector instructions behind the row maximum otherwise); infinities (the mask) stay honoured.
 # And its kernels of more than 256 registers compute on their score tiles between matrix products: results of those
 # products go to the ordinary registers, not to the accumulation registers from which every element would have to be
-# copied (backward at 1 x 16 x 2048 x 128: 99 -> 91 us).  attention_window.hip: the same maxima (a query sees itself); its dK/dV kernel of
+# copied (backward at 1 x 16 x 2048 x 128: 99 -> 91 us).  attention_window.hip: the same maxima (a query sees itself; a
+# NaN in the inputs passes them by and shows through the exponentials); its dK/dV kernel of
 # 128-wide heads is better off with the sums of dK and dV in the accumulation registers (4096 x 32 x 128, window 1024: 313 -> 299 us).
 EXTRA = {"attention.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form=1"], "attention_window.hip": ["-fno-honor-nans"]}
 
