@@ -576,6 +576,8 @@ class AdamW:
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
         if len(decay) != n:
             _refuse("AdamW: %d weight decays for %d parameters", len(decay), n)
+        if state_bits == 8 and ((m is None) != (m_scale is None) or (v is None) != (v_scale is None)):
+            _refuse("AdamW: states in 8 bits are nothing without their scales: m goes with m_scale, v with v_scale")
         p_type, g_type = params[0].dtype, grads[0].dtype
         if p_type not in (_BF16, _F32) or g_type not in (_BF16, _F32):
             _refuse("AdamW: parameters of %s and gradients of %s, wanted bf16 or fp32", p_type, g_type)

@@ -19,3 +19,12 @@ def test_parameters_that_need_gradients(bits):
     assert torch.equal(p.detach(), q) and torch.equal(a.master[0], b.master[0])
     p.float().sum().backward()
     assert (p.grad == 1).all()
+
+
+def test_states_in_8_bits_come_with_their_scales():
+    n, f = 96, lambda k: [torch.ones(k, dtype=torch.uint8, device="cuda")]      # noqa: E731
+    p, g = [torch.zeros(n, device="cuda")], [torch.ones(n, device="cuda")]
+    for kw in (dict(m=f(n)), dict(v=f(n)), dict(m=f(n), v=f(n)), dict(m=f(n), v=f(n), m_scale=f(3)), dict(m_scale=f(3)), dict(v_scale=f(3))):
+        with pytest.raises(P.AhError, match="scales"):
+            P.AdamW(p, g, state_bits=8, **kw)
+    P.AdamW(p, g, state_bits=8, m=f(n), v=f(n), m_scale=f(3), v_scale=f(3))
