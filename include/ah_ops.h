@@ -48,8 +48,8 @@ typedef struct {
  * largest value is within 1.75 (m) or 1.875 (v) times it.  m: sign, 4 bits of exponent, 3 of mantissa (the bit pattern
  * of e4m3); v: 5 bits of exponent, 3 of mantissa; both with gradual underflow below their last binade.  The step itself uses the
  * unrounded moments.  They are rounded to a neighbouring code at random, with the probability that keeps their expectation (a
- * step changes v by at most 1 - beta2 of itself, less than half the distance of two codes: rounded to nearest it would never
- * move); the random bits are a function of `seed` plus the step's number (modulo 2^32) and of the element's number alone (tensors are numbered
+ * step takes at most 1 - beta2 of v away, and the middle between a code and the one below it is 1/32 to 1/18 of the code away: rounded to nearest, v would never
+ * shrink where 1 - beta2 is below 1/32, 0.99 or 0.999, and stop at some of its codes at 0.95); the random bits are a function of `seed` plus the step's number (modulo 2^32) and of the element's number alone (tensors are numbered
  * one behind the other, each from a multiple of 64 on; the bits repeat after 2^32 elements).  They have to differ from step to step: where an element is
  * rounded by the same ones every time, its moments stand still.  A captured step therefore needs `step_dev` (and its owner counts that up
  * between replays); without it the call is refused.  A v > 0 never becomes 0 (m / sqrt(v) would have no
@@ -85,8 +85,9 @@ int ah_adamw_state_values(const ah_adamw_tensor_t* tensors, int n_tensors, void*
  * n_seq sequences; position i of one sees position j of it iff j <= i and (i - j < window or j < sinks).  Row t of q holds n_heads heads of head_dim
  * columns, of k and v n_kv_heads; query head h reads key and value head h / (n_heads / n_kv_heads).  Scores are scaled by
  * 1 / sqrt(head_dim), softmax and sums in fp32; probabilities (and their gradients) are rounded to bf16 for the second product, as in
- * ah_attention_fwd and _bwd.  A value that is not finite may reach rows within 192 positions of those that see its own
- * (a block of 128 queries walks tiles of 64 keys).
+ * ah_attention_fwd and _bwd.  A NaN shows in all rows that see it (a score of -infinity counts as nothing); what is not finite may reach rows within 192 positions of
+ * those too (a block of 128 queries walks tiles of 64 keys).  Sizes: seq_len at most 2^24, n_heads 4096, and n_seq * n_heads * (ceil(seq_len / 128) +
+ * 8 ceil(sinks / 128)) at most 2^23, packed sequences counted at seq_len each: so is the memory of lse and of the workspace.
  *
  * Sequences of one length: seq_len rows each, one behind the other (offsets NULL).  Packed: sequence b has the rows offsets[b] .. offsets[b + 1] - 1
  * (device, int32 [n_seq + 1], ascending, each length 0 .. seq_len); rows of no sequence are neither read nor written.  A sequence that would begin or
@@ -118,7 +119,8 @@ int ah_attention_window_bwd_workspace(const ah_attention_window_t* cfg, uint64_t
  * Row t of x holds n_heads query heads and behind them n_kv_heads key heads of head_dim columns each (the first columns of a packed
  * projection [Q | K | V]).  Each head by itself: n = x / sqrt(mean(x^2) + eps) * gain (gain_q or gain_k, bf16 [head_dim]); then
  * columns i and i + head_dim / 2 turn by the angle of the row's position p: y_i = n_i c - n_{i + d/2} s,
- * y_{i + d/2} = n_{i + d/2} c + n_i s with (c, s) = cos_sin[p][i].  In fp32, rounded once. */
+ * y_{i + d/2} = n_{i + d/2} c + n_i s with (c, s) = cos_sin[p][i].  In fp32, rounded once (a head whose sum of squares is above fp32's range, elements of 1e18 and
+ * more, comes out as zeros). */
 typedef struct {
   uint32_t struct_size;        /* sizeof(ah_qk_norm_rope_t), checked */
   int32_t rows;                /* T >= 0 */
@@ -130,7 +132,7 @@ typedef struct {
   int64_t ld_x, ld_y, ld_dx;   /* columns from row to row of x, of y (or dy) and of dx: multiples of 8, at least (n_heads + n_kv_heads) * head_dim; 0: just that */
   const void *gain_q, *gain_k; /* device; gain_k may be NULL where n_kv_heads is 0, gain_q likewise */
   const float* cos_sin;        /* device [n_pos][head_dim / 2][2] (ah_rope_table); NULL: no rotation */
-  const int32_t* positions;    /* device [rows], optional; a row whose position is outside [0, n_pos) comes out as NaN */
+  const int32_t* positions;    /* device [rows], optional; a row whose position is outside [0, n_pos) comes out as NaN (and, backward, the gains' gradients) */
 } ah_qk_norm_rope_t;
 
 /* y may be x with the same row stride (each element is read before it is written); else it overlaps nothing that the call reads. */

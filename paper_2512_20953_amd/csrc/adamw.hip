@@ -123,7 +123,8 @@ __device__ __forceinline__ uint32_t block_max(uint32_t x) {
   x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, true));           // lanes 1 0 3 2
   return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, true));        // lanes 2 3 0 1
 }
-// 32 bits from the product of an element's number with an odd constant plus the seed
+// 32 bits from the product of an element's number with an odd constant plus the seed (the constant: the prime 2654435761 of Knuth's multiplicative hashing; the shifts and
+// multipliers behind it: C. Wellons, "Prospecting for Hash Functions", 2018)
 constexpr uint32_t kNumber = 0x9E3779B1u;
 __device__ __forceinline__ uint32_t random_bits(uint32_t x) {
   x ^= x >> 16; x *= 0x7feb352du; x ^= x >> 15; x *= 0x846ca68bu;

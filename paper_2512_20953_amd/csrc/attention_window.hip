@@ -5,6 +5,9 @@
 // those with the first tokens, so the work grows with seq_len * (window + sinks).  Lengths are any: the rows of a tile that
 // lie behind the sequence's end are loaded as copies of its last row and masked.
 //
+// Probabilities and dS are rounded to bf16 (2^-8 at most of each), the type that the matrix instruction takes: an error of 1.9e-3 to 2.4e-3 of a result's norm, against 1.6e-3 with both in
+// fp32, which is that of rounding the result itself; products in more bits would be another instruction at a fraction of the rate.
+//
 // Backward: a block per 128 queries for dQ (it leaves -delta behind), then a block per 128 keys and key head for dK, dV, which walks the query
 // heads that share the key head one after the other: no atomics.  The keys that all later positions see have seq_len queries instead
 // of window + 128: what lies behind their window is shared by further blocks, whose sums meet in a third kernel.
@@ -117,9 +120,9 @@ __device__ __forceinline__ void store_rows_to(const F& val, char* strip, bf16* _
 }
 
 // =========================================================================== forward
-// One pass with a running maximum and sum.  Bound by the CU's LDS path: a wave needs all of a K and V tile as fragments, 160 KB a tile and block of
-// 128-wide heads with the tile's arrival, 114 of the 170 us that 1 x 8192 x 32 heads in groups of four x 128 take (window 1024, 4 first tokens; 85 B/clk, 2.4 GHz).  Two blocks a
-// CU; with 64 queries a wave half the LDS reads, but one wave a SIMD: 252 us.
+// One pass with a running maximum and sum.  1 x 8192 x 32 heads in groups of four x 128, window 1024, 4 first tokens: 168 us.  No unit is full: of a launch's cycles by counters (traced, 182 us
+// at 2.05 GHz) the CU's LDS path has 55 % (a wave needs all of a K and V tile as fragments, 128 KB a tile and block at 128 B/clk, and the tile's 32 KB arrive at 1.7 times that price), the matrix
+// units 37, the vector units 35; two waves a SIMD do not hide them behind one another.  With 64 queries a wave half the LDS reads, but one wave a SIMD: 252 us.
 template <int D>
 __global__ __launch_bounds__(256, 2) void win_fwd_kernel(WinArgs a) {
   constexpr int TILEB = 64 * 2 * D, STAGE = 2 * TILEB, NK = D / 16, ND = D / 32;
@@ -225,8 +228,8 @@ __global__ __launch_bounds__(256, 2) void win_fwd_kernel(WinArgs a) {
 }
 
 // =========================================================================== backward: dQ
-// P from the kept log-sum-exps, dS = P (dO V^T - delta), dQ = scale dS K.  1 x 4096 x 32 x 128, window 1024, 4 first tokens: 120 us traced, matrix units busy a third of it; the fragments
-// of K (both ways round) and V are 224 KB a tile and block with the tile's arrival: 74 us of LDS path.
+// P from the kept log-sum-exps, dS = P (dO V^T - delta), dQ = scale dS K.  1 x 4096 x 32 x 128, window 1024, 4 first tokens: 118 us traced, of whose cycles the matrix
+// units have 36 %, the LDS path about half (the fragments of K, both ways round, and V: 192 KB a tile and block beside the tile's arrival), the vector units 23.
 template <int D>
 __global__ __launch_bounds__(256, 2) void win_dq_kernel(WinArgs a) {
   constexpr int TILEB = 64 * 2 * D, STAGE = 2 * TILEB, NK = D / 16, ND = D / 32;
