@@ -1,7 +1,8 @@
 /*
  * ah_ops.h — operators that a stage of a newer decoder trains with, one call each (C ABI, part of libahstage.so): attention
- * over a sliding window with visible first tokens, norms of the query and key heads with the position rotation, and the
- * optimizer step over a stage's tensors.
+ * over a sliding window with visible first tokens, norms of the query and key heads with the position rotation, the
+ * optimizer steps over a stage's tensors (AdamW, and Muon for its matrices), and what stands before the first stage and behind the last one: the
+ * embedding of the tokens, the norm in front of the head, the loss of the logits.
  *
  * The rules of ah_stage.h hold: plain C, every function returns an ah_status_t and leaves a message for ah_last_error(), device
  * memory is the caller's, work is only enqueued on `hip_stream` (a hipStream_t cast to void*; NULL = the default stream) and
@@ -145,6 +146,109 @@ int ah_qk_norm_rope_bwd(const ah_qk_norm_rope_t* cfg, const void* x, const void*
 int ah_qk_norm_rope_bwd_workspace(const ah_qk_norm_rope_t* cfg, uint64_t* bytes);
 /* cos_sin[p][i] = (cos, sin)(p base^(-2 i / head_dim)) for p < n_pos, in fp64 rounded to fp32 (the table of the LLaMA-style stage). */
 int ah_rope_table(float* cos_sin, int n_pos, int head_dim, double base, void* hip_stream);
+
+/* ---- the optimizer step of matrices by their momentum's orthogonal factor (Muon) ----
+ *
+ * For each matrix of its own, with g' = factor * g (as in ah_adamw_step),
+ *   m += (1 - momentum) (g' - m);   u = nesterov ? m + (1 - momentum) (g' - m) : m
+ *   X = u / (|u| + eps), |u| the root of the sum of squares, X transposed where there are more rows than columns;
+ *   ns_steps times: A = X X^T; X = a X + (b A + c A A) X, (a, b, c) = (3.4445, -4.7750, 2.0315), which brings the singular values of 1 / 500 and more to 0.68 .. 1.21;
+ *   p = p (1 - lr weight_decay) - lr scale X.
+ * Momentum, norm, update in fp32 (the sum of squares in fp64).  X is kept between the products in 22 bits (two fp16 numbers); the products' operands are fp16
+ * (11 bits; X, A and b A + c A A are at most 3 in magnitude whatever u is), their sums fp32.  bf16 parameters without a master copy are rounded to nearest after every step. */
+typedef struct {
+  void* param;          /* [rows, cols], bf16 or fp32: ah_muon_t.param_type */
+  const void* grad;     /* bf16 or fp32: ah_muon_t.grad_type */
+  float* momentum;      /* read and written */
+  float* master;        /* bf16 parameters kept in fp32, or NULL: all matrices of a call alike */
+  int64_t rows, cols;   /* 0 is allowed; at most 32768, the larger one 131072 */
+  int64_t ld_param, ld_grad, ld_momentum, ld_master;   /* elements from row to row (a block of a wider matrix's columns, for one), at least cols; 0: cols */
+  float weight_decay;   /* decoupled */
+  float scale;          /* of the update; 0.2 sqrt(max(rows, cols)) makes its elements as large as AdamW's */
+} ah_muon_matrix_t;
+
+typedef struct {
+  uint32_t struct_size;   /* sizeof(ah_muon_t), checked */
+  int32_t param_type, grad_type;   /* ah_type_t; master copies go with bf16 parameters */
+  int32_t nesterov, ns_steps;      /* 0 or 1; 1 .. 32 */
+  uint32_t reserved;      /* 0 */
+  double lr, momentum, eps;        /* lr >= 0, momentum in [0, 1), eps >= 1e-37 */
+  const float* lr_dev;    /* device, optional: read by the kernel in place of lr */
+  const float* grad_norm; /* device, optional: the two values that ah_grad_norm left.  The second is the factor above; NaN leaves everything as it was. */
+} ah_muon_t;
+
+/* matrices: HOST array, read during the call.  What a call writes overlaps nothing else that it reads or writes (columns of a wider matrix beside each other do not).
+ * A matrix whose momentum is or becomes infinite or NaN is NaN behind the step; the others are not touched by it.  workspace: device, 256-byte aligned, of the size that
+ * ah_muon_workspace gives for these matrices (which looks at rows and cols only): the largest group of matrices that are worked on together. */
+int ah_muon_step(const ah_muon_t* cfg, const ah_muon_matrix_t* matrices, int n_matrices, void* workspace, void* hip_stream);
+int ah_muon_workspace(const ah_muon_matrix_t* matrices, int n_matrices, uint64_t* bytes);
+
+/* ---- embedding: what the first stage's rows are made from ----
+ *
+ * y_t = scale * table[token_t] + pos_table[position_t] in fp32, rounded once.  A token of -1 is none (padding): its row of the table counts as zeros, and it has no
+ * gradient.  Any other outside [0, vocab), or a position outside [0, n_pos), makes its row NaN (backward: such a token has no gradient). */
+typedef struct {
+  uint32_t struct_size;       /* sizeof(ah_embedding_t), checked */
+  int32_t rows;               /* T, 0 .. 2^25 */
+  int32_t vocab;              /* rows of the table, 1 .. 2^30 */
+  int32_t width;              /* 1 .. 65536 */
+  int32_t table_type, act_type;   /* ah_type_t of table and pos_table, and of y or dy */
+  int32_t token_bits;         /* 32 or 64: signed numbers of as many bits */
+  float scale;                /* finite */
+  int64_t ld_table, ld_act, ld_pos;   /* elements from row to row of table (backward: of d_table), y or dy, pos_table; at least width; 0: width */
+  const void* pos_table;      /* device [n_pos, width], optional */
+  int32_t n_pos, seq_len;     /* position of row t: t % seq_len, or ... */
+  const int32_t* positions;   /* ... device [rows], optional */
+} ah_embedding_t;
+
+/* Results overlap nothing that a call reads. */
+int ah_embedding_fwd(const ah_embedding_t* cfg, const void* table, const void* tokens, void* y, void* hip_stream);
+/* d_table (fp32 [vocab, width]) = beta * d_table + scale * the sum of dy_t over the rows t with that token; beta in {0, 1}; 0 writes all rows, 1 reads and writes only
+ * those whose token occurs.  Sums in fp32, in an order that depends on the tokens alone (no atomics).  The gradient of pos_table is that of a table of n_pos rows
+ * with the positions as tokens and a scale of 1.  workspace: device, 256-byte aligned, of the size that ah_embedding_bwd_workspace gives (which looks at rows, vocab and width). */
+int ah_embedding_bwd(const ah_embedding_t* cfg, const void* tokens, const void* dy, float* d_table, int beta, void* workspace, void* hip_stream);
+int ah_embedding_bwd_workspace(const ah_embedding_t* cfg, uint64_t* bytes);
+
+/* ---- layer norm: what stands in front of the head ----
+ *
+ * n = (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps) of each row (rms: without the mean), y = n * gain + bias, in fp32, rounded once. */
+typedef struct {
+  uint32_t struct_size;       /* sizeof(ah_layer_norm_t), checked */
+  int32_t rows;               /* T, 0 .. 2^25 */
+  int32_t width;              /* 1 .. 16384 */
+  int32_t rms;                /* 0 or 1 */
+  int32_t act_type, param_type;   /* ah_type_t of x, y, dy, dx; of gain and bias */
+  float eps;                  /* >= 2^-126 */
+  uint32_t reserved;          /* 0 */
+  int64_t ld_x, ld_y, ld_dx;  /* elements from row to row of x, of y (or dy) and of dx; at least width; 0: width */
+  const void *gain, *bias;    /* device [width]; NULL: ones, zeros */
+} ah_layer_norm_t;
+
+/* y may be x with the same row stride; else it overlaps nothing that the call reads. */
+int ah_layer_norm_fwd(const ah_layer_norm_t* cfg, const void* x, void* y, void* hip_stream);
+/* dx from x and dy (statistics are computed again); dx may be x or dy with the same row stride.  d_gain, d_bias (fp32 [width], either may be NULL) = beta * themselves + the
+ * gradients, beta in {0, 1}: sums in an order that depends on the sizes alone.  workspace: device, 16-byte aligned, of the size that ah_layer_norm_bwd_workspace gives. */
+int ah_layer_norm_bwd(const ah_layer_norm_t* cfg, const void* x, const void* dy, void* dx, float* d_gain, float* d_bias, int beta, void* workspace, void* hip_stream);
+int ah_layer_norm_bwd_workspace(const ah_layer_norm_t* cfg, uint64_t* bytes);
+
+/* ---- loss of the logits, with its gradient ----
+ *
+ * With lse = log(sum over j of exp(z_j)) of row t and its target i: loss_t = lse - z_i; d_logits_tj = s (exp(z_j - lse) - [j = i]) with s = scale (or *scale_dev), in fp32, rounded once.
+ * A target of -1 is none: loss and gradient 0.  Any other outside [0, vocab) makes both NaN, and so does a row whose logits are all -infinity, or of which one is
+ * +infinity or NaN; a logit of -infinity beside finite ones has the probability 0. */
+typedef struct {
+  uint32_t struct_size;       /* sizeof(ah_cross_entropy_t), checked */
+  int32_t rows;               /* T, 0 .. 2^25 */
+  int32_t vocab;              /* columns, 1 .. 2^24 */
+  int32_t act_type;           /* ah_type_t of logits and d_logits */
+  int32_t target_bits;        /* 32 or 64: signed numbers of as many bits */
+  float scale;                /* of the gradient: 1 / (number of targets), for one; finite */
+  const float* scale_dev;     /* device, optional: read by the kernel in place of scale */
+  int64_t ld_logits, ld_grad; /* elements from row to row, at least vocab; 0: vocab */
+} ah_cross_entropy_t;
+
+/* loss: fp32 [rows].  d_logits: NULL (the loss alone), logits themselves with the same row stride, or a buffer that overlaps nothing that the call reads. */
+int ah_cross_entropy(const ah_cross_entropy_t* cfg, const void* logits, const void* targets, float* loss, void* d_logits, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -7,7 +7,8 @@ _LAZY = ("AH_ARCH_GPT", "AH_ARCH_LLAMA", "AH_ARCH_BERT", "PARAM_INDEX", "AhError
          "attention_fwd", "attention_bwd_static", "ATTENTION_STATIC_MAX_ROWS", "gemm_nn", "gemm_nn_swiglu", "gemm_nt", "gemm_plan", "gemm_tn", "gemm_tn_segmented", "lib", "library_path", "query_sizes", "cost_layers_time",
          "cost_pipeline_time", "cost_iteration_time", "cost_idle_fractions", "cost_partition_layers", "AdamW",
          "attention_window_fwd", "attention_window_bwd", "attention_window_bwd_workspace", "qk_norm_rope_fwd", "qk_norm_rope_bwd",
-         "qk_norm_rope_bwd_workspace", "rope_table")
+         "qk_norm_rope_bwd_workspace", "rope_table", "Muon", "grad_norm", "grad_norm_workspace", "embedding_fwd", "embedding_bwd", "embedding_bwd_workspace",
+         "layer_norm_fwd", "layer_norm_bwd", "layer_norm_bwd_workspace", "cross_entropy")
 
 
 def __getattr__(name):

@@ -91,6 +91,32 @@ class _QkNormConfig(C.Structure):
                 ("gain_q", C.c_void_p), ("gain_k", C.c_void_p), ("cos_sin", C.c_void_p), ("positions", C.c_void_p)]
 
 
+class _MuonMatrix(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("param", "grad", "momentum", "master")] + [
+                (n, C.c_int64) for n in ("rows", "cols", "ld_param", "ld_grad", "ld_momentum", "ld_master")] + [("weight_decay", C.c_float), ("scale", C.c_float)]
+
+
+class _MuonConfig(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("param_type", C.c_int32), ("grad_type", C.c_int32), ("nesterov", C.c_int32), ("ns_steps", C.c_int32),
+                ("reserved", C.c_uint32), ("lr", C.c_double), ("momentum", C.c_double), ("eps", C.c_double), ("lr_dev", C.c_void_p), ("grad_norm", C.c_void_p)]
+
+
+class _EmbeddingConfig(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("rows", C.c_int32), ("vocab", C.c_int32), ("width", C.c_int32), ("table_type", C.c_int32), ("act_type", C.c_int32),
+                ("token_bits", C.c_int32), ("scale", C.c_float), ("ld_table", C.c_int64), ("ld_act", C.c_int64), ("ld_pos", C.c_int64),
+                ("pos_table", C.c_void_p), ("n_pos", C.c_int32), ("seq_len", C.c_int32), ("positions", C.c_void_p)]
+
+
+class _LayerNormConfig(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("rows", C.c_int32), ("width", C.c_int32), ("rms", C.c_int32), ("act_type", C.c_int32), ("param_type", C.c_int32),
+                ("eps", C.c_float), ("reserved", C.c_uint32), ("ld_x", C.c_int64), ("ld_y", C.c_int64), ("ld_dx", C.c_int64), ("gain", C.c_void_p), ("bias", C.c_void_p)]
+
+
+class _CrossEntropyConfig(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("rows", C.c_int32), ("vocab", C.c_int32), ("act_type", C.c_int32), ("target_bits", C.c_int32), ("scale", C.c_float),
+                ("scale_dev", C.c_void_p), ("ld_logits", C.c_int64), ("ld_grad", C.c_int64)]
+
+
 def library_path():
     return os.path.join(HERE, "libahstage.so")
 
@@ -148,6 +174,16 @@ def _load():
     L.ah_qk_norm_rope_bwd.argtypes = [qc, vp, vp, vp, vp, vp, i, vp, vp]
     L.ah_qk_norm_rope_bwd_workspace.argtypes = [qc, C.POINTER(C.c_uint64)]
     L.ah_rope_table.argtypes = [vp, i, i, C.c_double, vp]
+    mc, mm, ec, lc = C.POINTER(_MuonConfig), C.POINTER(_MuonMatrix), C.POINTER(_EmbeddingConfig), C.POINTER(_LayerNormConfig)
+    L.ah_muon_step.argtypes = [mc, mm, i, vp, vp]
+    L.ah_muon_workspace.argtypes = [mm, i, C.POINTER(C.c_uint64)]
+    L.ah_embedding_fwd.argtypes = [ec, vp, vp, vp, vp]
+    L.ah_embedding_bwd.argtypes = [ec, vp, vp, vp, i, vp, vp]
+    L.ah_embedding_bwd_workspace.argtypes = [ec, C.POINTER(C.c_uint64)]
+    L.ah_layer_norm_fwd.argtypes = [lc, vp, vp, vp]
+    L.ah_layer_norm_bwd.argtypes = [lc, vp, vp, vp, vp, vp, i, vp, vp]
+    L.ah_layer_norm_bwd_workspace.argtypes = [lc, C.POINTER(C.c_uint64)]
+    L.ah_cross_entropy.argtypes = [C.POINTER(_CrossEntropyConfig), vp, vp, vp, vp, vp]
     L.ah_adamw_state_values.argtypes = [tp, i, C.POINTER(vp), C.POINTER(vp), vp]
     return L
 
@@ -251,19 +287,31 @@ class Stage:
         _check(lib.ah_stage_backward_streams(self._h, C.byref(n)))
         return n.value
 
-    def adamw(self, weight_decay=0.1, **options):
+    def adamw(self, weight_decay=0.1, matrices=True, **options):
         """An AdamW over the stage's parameters and gradients (state_bits, master, betas, eps as there); weight_decay acts on the matrices, not on
-        biases, gains and offsets.  Its step goes behind the last backward (or flush_grads) of an iteration, on the same stream."""
+        biases, gains and offsets.  matrices False: over those alone, beside muon().  Its step goes behind the last backward (or flush_grads) of an iteration, on the same stream."""
         params, grads, decay = [], [], []
         for layer in range(self.cfg.n_layers):
             for which in PARAM_INDEX.values():
                 off, r, c = C.c_uint64(), C.c_int32(), C.c_int32()
-                if lib.ah_stage_param_layout(self._h, layer, which, C.byref(off), C.byref(r), C.byref(c)) == 0:    # (not every architecture has each)
+                if lib.ah_stage_param_layout(self._h, layer, which, C.byref(off), C.byref(r), C.byref(c)) == 0 and (matrices or r.value == 1):    # (not every architecture has each)
                     at = slice(off.value, off.value + r.value * c.value)
                     params.append(self.params[at])
                     grads.append(self.grads[at])
                     decay.append(weight_decay if r.value > 1 else 0.0)
         return AdamW(params, grads, weight_decay=decay, **options)
+
+    def muon(self, weight_decay=0.1, **options):
+        """A Muon over the stage's matrices (momentum, nesterov, scale, ns_steps, eps, master as there): the query, key and value blocks of their projection
+        are matrices of their own, and so are the gate and up blocks of a LLaMA-style MLP.  adamw(matrices=False) steps the other tensors."""
+        params, grads = [], []
+        for layer in range(self.cfg.n_layers):
+            for name in ("wqkv", "wo", "w1", "w2"):
+                blocks = 3 if name == "wqkv" else 2 if name == "w1" and self.cfg.arch == AH_ARCH_LLAMA else 1
+                p = self.param_view(layer, name)
+                params += p.split(p.shape[1] // blocks, dim=1)
+                grads += self.grad_view(layer, name).split(p.shape[1] // blocks, dim=1)
+        return Muon(params, grads, weight_decay=weight_decay, **options)
 
     def grads_ptr(self):
         p, n = C.c_void_p(), C.c_uint64()
@@ -677,3 +725,272 @@ class AdamW:
                 _refuse("AdamW.state_values: outputs are contiguous bf16 tensors on the parameters' device")
         at = [t.data_ptr() for t in both]
         _check(lib.ah_adamw_state_values(self._list, n, (C.c_void_p * n)(*at[:n]), (C.c_void_p * n)(*at[n:]), _stream(stream)))
+
+
+def grad_norm_workspace(n):
+    """Bytes of scratch memory that grad_norm takes for n tensors."""
+    need = C.c_uint64()
+    _check(lib.ah_grad_norm_workspace(_clamped(n), need))
+    return need.value
+
+
+def grad_norm(grads, out, workspace, max_norm=0.0, stream=None):
+    """out (fp32 [2]) = [norm of all the gradients together, factor that brings it down to max_norm], for the steps of several optimizers (ah_grad_norm).  grads: a list of
+    contiguous tensors, all bf16 or all fp32; max_norm 0: no limit.  workspace: uint8, grad_norm_workspace(len(grads)) bytes."""
+    n = len(grads)
+    if n == 0 or grads[0].dtype not in (_BF16, _F32):
+        _refuse("grad_norm: wanted a list of bf16 or fp32 tensors")
+    kind, each = grads[0].dtype, (_AdamWTensor * n)()
+    for k in range(n):
+        each[k].grad, each[k].n = _dense("grad_norm: gradient", grads[k], kind), grads[k].numel()
+    work, need = _dense("workspace", workspace, _U8), grad_norm_workspace(n)
+    if workspace.numel() < need:
+        _refuse("grad_norm: the workspace holds %d bytes, too few", workspace.numel())
+    _check(lib.ah_grad_norm(each, n, int(kind is _F32), float(max_norm), _dense("grad_norm: out", out, _F32, 2), work, _stream(stream)))
+
+
+def _matrix(what, t, dtype, shape):
+    """(address, elements from row to row) of a matrix whose rows are dense, at any distance from each other."""
+    _on_device(what, t)
+    stride = t.stride()
+    if t.dtype is not dtype or t.dim() != 2 or (shape is not None and t.shape != shape):
+        _refuse("%s: %s of shape %s, wanted a matrix of %s%s", what, t.dtype, tuple(t.shape), dtype, "" if shape is None else " and shape %s" % (tuple(shape),))
+    rows, cols = t.shape
+    ld = stride[0] if rows > 1 else max(cols, 1)
+    if (cols > 1 and stride[1] != 1) or ld < cols:
+        _refuse("%s: rows must be dense and apart (strides %s)", what, stride)
+    return t.data_ptr(), ld
+
+
+def _matrices_apart(written, read):
+    """Whether no two of the matrices (begin, rows, bytes of a row, bytes from row to row) in `written` overlap, nor one of them and one of `read`.  Those that lie in each
+    other's span are apart if their rows are as far apart and their columns beside each other."""
+    spans = sorted([(b, b + (r - 1) * ld + w, w, ld, True) for b, r, w, ld in written if r and w] + [(b, b + (r - 1) * ld + w, w, ld, False) for b, r, w, ld in read if r and w])
+    open_ = []
+    for b, e, w, ld, writes in spans:
+        open_ = [x for x in open_ if x[1] > b]
+        for b0, _, w0, ld0, writes0 in open_:
+            if (writes or writes0) and not (ld == ld0 and w0 <= (b - b0) % ld and (b - b0) % ld + w <= ld):
+                return False
+        open_.append((b, e, w, ld, writes))
+    return True
+
+
+class Muon:
+    """One optimizer step over matrices whose update is their momentum, orthogonalised (ah_muon_step): bf16 or fp32 parameters with fp32 or bf16 gradients, fp32 momentum.
+    Matrices may be blocks of columns of wider ones.
+
+    weight_decay: one number, or one for each matrix.
+    scale: of the update, likewise; None: 0.2 sqrt(max(rows, cols)), which makes its elements as large as AdamW's (its lr and decay then fit).
+    master: True keeps bf16 parameters in fp32 too (the step updates those and rounds them into the parameters), starting from the parameters' values; or a list of such matrices.
+    m: a list of momenta to go on from; without it zeroed ones are made.
+    Matrices that a step writes overlap no other.  The object keeps the tensors that it was given, and its scratch memory serves one step at a time.
+    It makes its own on the stream that is torch's current one at its construction: steps on other streams come behind that."""
+
+    def __init__(self, params, grads, momentum=0.95, nesterov=True, weight_decay=0.0, scale=None, ns_steps=5, eps=1e-7, master=None, m=None):
+        params, grads = list(params), list(grads)
+        n = len(params)
+        if n == 0 or len(grads) != n:
+            _refuse("Muon: %d parameters and %d gradients", n, len(grads))
+        p_type, g_type = params[0].dtype, grads[0].dtype
+        if p_type not in (_BF16, _F32) or g_type not in (_BF16, _F32):
+            _refuse("Muon: parameters of %s and gradients of %s, wanted bf16 or fp32", p_type, g_type)
+        each = lambda what, v: list(v) if isinstance(v, (list, tuple)) else [v] * n    # noqa: E731
+        decay, scales = each("weight_decay", weight_decay), each("scale", scale)
+        if len(decay) != n or len(scales) != n:
+            _refuse("Muon: %d weight decays and %d scales for %d parameters", len(decay), len(scales), n)
+        self._device = params[0].device
+        shapes = [p.shape for p in params]
+        for k in range(n):
+            if len(shapes[k]) != 2:
+                _refuse("Muon: parameter %d has the shape %s, wanted a matrix", k, tuple(shapes[k]))
+        if m is None:
+            m = [torch.zeros(s, dtype=_F32, device=self._device) for s in shapes]
+        if master is True:
+            if p_type != _BF16:
+                _refuse("Muon: master copies go with bf16 parameters")
+            master = [p.detach().float().contiguous() for p in params]
+        self.params, self.grads, self.m, self.master = params, grads, list(m), None if master is None or master is False else list(master)
+        if len(self.m) != n or (self.master is not None and len(self.master) != n):
+            _refuse("Muon: momenta or master copies are not as many as parameters")
+        self._list = (_MuonMatrix * n)()
+        written, read = [], []
+        for k in range(n):
+            e, rows, cols = self._list[k], *shapes[k]
+            e.rows, e.cols = rows, cols
+            e.param, e.ld_param = _matrix("Muon: parameter %d" % k, params[k], p_type, None)
+            e.grad, e.ld_grad = _matrix("Muon: gradient %d" % k, grads[k], g_type, shapes[k])
+            e.momentum, e.ld_momentum = _matrix("Muon: momentum %d" % k, self.m[k], _F32, shapes[k])
+            p_size, g_size = params[k].element_size(), grads[k].element_size()
+            written += [(e.param, rows, cols * p_size, e.ld_param * p_size), (e.momentum, rows, cols * 4, e.ld_momentum * 4)]
+            read.append((e.grad, rows, cols * g_size, e.ld_grad * g_size))
+            if self.master is not None:
+                e.master, e.ld_master = _matrix("Muon: master copy %d" % k, self.master[k], _F32, shapes[k])
+                written.append((e.master, rows, cols * 4, e.ld_master * 4))
+            e.weight_decay = float(decay[k])
+            e.scale = 0.2 * max(rows, cols) ** 0.5 if scales[k] is None else float(scales[k])
+        if not _matrices_apart(written, read):
+            _refuse("Muon: parameters, momenta, copies and gradients overlap (gradients alone may)")
+        self._cfg = _MuonConfig(struct_size=C.sizeof(_MuonConfig), param_type=int(p_type == _F32), grad_type=int(g_type == _F32), nesterov=int(bool(nesterov)),
+                                ns_steps=_clamped(ns_steps), momentum=float(momentum), eps=float(eps))
+        need = C.c_uint64()
+        _check(lib.ah_muon_workspace(self._list, n, need))
+        self._work = torch.empty(need.value, dtype=_U8, device=self._device)
+
+    def step(self, lr, grad_norm=None, stream=None):
+        """One step.  lr: a number, or an fp32 tensor of one element on the device (a captured step reads it anew when it is replayed).  grad_norm: what grad_norm()
+        or AdamW.grad_norm() gave: gradients are multiplied by its factor, and where that is NaN nothing changes."""
+        c = self._cfg
+        _on_device("Muon: parameters", self._work)
+        c.lr_dev = c.grad_norm = None
+        if isinstance(lr, torch.Tensor):
+            c.lr, c.lr_dev = 0.0, _dense("Muon.step: lr", lr, _F32, 1)
+        else:
+            c.lr = lr
+        if grad_norm is not None:
+            c.grad_norm = _dense("Muon.step: grad_norm", grad_norm, _F32, 2)
+        _check(lib.ah_muon_step(c, self._list, len(self._list), self._work.data_ptr(), _stream(stream)))
+
+
+# ---- in front of the first stage and behind the last one
+_EMBED_SIZE, _NORM_SIZE, _LOSS_SIZE = C.sizeof(_EmbeddingConfig), C.sizeof(_LayerNormConfig), C.sizeof(_CrossEntropyConfig)
+_TYPES = {_BF16: 0, _F32: 1}
+
+
+def _fits(*sizes):
+    for n in sizes:
+        if n >> 31:
+            _refuse("a size of %d: more than 2^31 - 1", n)
+
+
+def _any_rows(what, t, rows, cols, dtype=None):
+    """(address, elements from row to row, ah_type_t) of a bf16 or fp32 matrix (or one of `dtype`) whose rows are dense, at any distance from each other."""
+    device = t.get_device()
+    if device < 0 or device != _current_device():
+        _on_device(what, t)
+    shape, stride, kind = t.shape, t.stride(), t.dtype
+    if kind not in _TYPES or (dtype is not None and kind is not dtype) or len(shape) != 2 or shape[0] != rows or shape[1] != cols:
+        _refuse("%s: %s of shape %s, wanted %s [%d, %d]", what, kind, tuple(shape), "bf16 or fp32" if dtype is None else dtype, rows, cols)
+    ld = stride[0] if rows > 1 else cols
+    if (cols > 1 and stride[1] != 1) or ld < cols:
+        _refuse("%s: rows must be dense and apart (strides %s)", what, stride)
+    return t.data_ptr(), ld, _TYPES[kind]
+
+
+def _indices(what, t, n):
+    """(address, bits) of n int32 or int64 numbers."""
+    if t.dtype is _I32:
+        return _dense(what, t, _I32, n), 32
+    return _dense(what, t, torch.int64, n), 64
+
+
+def embedding_fwd(table, tokens, y, scale=1.0, pos_table=None, positions=None, seq_len=0, stream=None):
+    """y[t] = scale * table[tokens[t]] + pos_table[position of t] (ah_embedding_fwd).  table: [vocab, width], y: [T, width], bf16 or fp32 each, rows at any distance; tokens: int32 or
+    int64 [T], -1: none.  pos_table: like table, [n_pos, width]; positions: int32 [T], without them row t has position t % seq_len."""
+    if table.dim() != 2:
+        _refuse("embedding_fwd: table of shape %s, wanted [vocab, width]", tuple(table.shape))
+    (vocab, width), T = table.shape, tokens.numel()
+    _fits(vocab, width, T)
+    pt, ld_t, kind = _any_rows("table", table, vocab, width)
+    py, ld_y, act = _any_rows("y", y, T, width)
+    at, bits = _indices("tokens", tokens, T)
+    c = _EmbeddingConfig(_EMBED_SIZE, T, vocab, width, kind, act, bits, scale, ld_t, ld_y)
+    if pos_table is not None:
+        n_pos = pos_table.shape[0]
+        _fits(n_pos)
+        c.pos_table, c.ld_pos, _ = _any_rows("pos_table", pos_table, n_pos, width, table.dtype)
+        c.n_pos, c.seq_len = n_pos, _clamped(seq_len)
+        if positions is not None:
+            c.positions = _dense("positions", positions, _I32, T)
+    _check(lib.ah_embedding_fwd(c, pt, at, py, _stream(stream)))
+
+
+def embedding_bwd_workspace(rows, vocab, width):
+    """Bytes of scratch memory that embedding_bwd takes."""
+    n = C.c_uint64()
+    _check(lib.ah_embedding_bwd_workspace(_EmbeddingConfig(_EMBED_SIZE, *map(_clamped, (rows, vocab, width))), n))
+    return n.value
+
+
+def embedding_bwd(tokens, dy, d_table, workspace, scale=1.0, beta=0, stream=None):
+    """d_table (fp32 [vocab, width]) = beta * d_table + scale * the sums of dy's rows by token (ah_embedding_bwd).  beta 0 writes all rows, 1 reads and writes those whose
+    token occurs.  workspace: uint8, embedding_bwd_workspace(T, vocab, width) bytes."""
+    if beta not in (0, 1):
+        _refuse("embedding_bwd: beta %s: 0 or 1", beta)
+    if d_table.dim() != 2:
+        _refuse("embedding_bwd: d_table of shape %s, wanted [vocab, width]", tuple(d_table.shape))
+    (vocab, width), T = d_table.shape, tokens.numel()
+    _fits(vocab, width, T)
+    pd, ld_d, _ = _any_rows("d_table", d_table, vocab, width, _F32)
+    py, ld_y, act = _any_rows("dy", dy, T, width)
+    at, bits = _indices("tokens", tokens, T)
+    c = _EmbeddingConfig(_EMBED_SIZE, T, vocab, width, 0, act, bits, scale, ld_d, ld_y)
+    work, need = _dense("workspace", workspace, _U8), C.c_uint64()
+    _check(lib.ah_embedding_bwd_workspace(c, need))
+    if workspace.numel() < need.value:
+        _refuse("embedding_bwd: the workspace holds %d bytes, too few", workspace.numel())
+    _check(lib.ah_embedding_bwd(c, at, py, pd, int(beta), work, _stream(stream)))
+
+
+def _norm_args(x, gain, bias, other, eps, rms):
+    if x.dim() != 2:
+        _refuse("layer_norm: x of shape %s, wanted [T, width]", tuple(x.shape))
+    T, width = x.shape
+    _fits(T, width)
+    px, ld_x, act = _any_rows("x", x, T, width)
+    po, ld_o, _ = _any_rows("y or dy", other, T, width, x.dtype)
+    kind = (gain if gain is not None else bias).dtype if gain is not None or bias is not None else _BF16
+    if kind not in _TYPES:
+        _refuse("layer_norm: gain or bias of %s, wanted bf16 or fp32", kind)
+    pg = _dense("gain", gain, kind, width) if gain is not None else None
+    pb = _dense("bias", bias, kind, width) if bias is not None else None
+    return _LayerNormConfig(_NORM_SIZE, T, width, int(bool(rms)), act, _TYPES[kind], eps, 0, ld_x, ld_o, 0, pg, pb), px, po
+
+
+def layer_norm_fwd(x, gain, bias, y, eps=1e-5, rms=False, stream=None):
+    """The norm of every row of x [T, width] with gain and bias ([width], bf16 or fp32; None: ones, zeros), rms: without the mean (ah_layer_norm_fwd).  x, y: bf16 or fp32,
+    rows at any distance; y may be x, row for row."""
+    c, px, py = _norm_args(x, gain, bias, y, eps, rms)
+    _check(lib.ah_layer_norm_fwd(c, px, py, _stream(stream)))
+
+
+def layer_norm_bwd_workspace(rows, width):
+    """Bytes of scratch memory that layer_norm_bwd takes."""
+    n = C.c_uint64()
+    _check(lib.ah_layer_norm_bwd_workspace(_LayerNormConfig(_NORM_SIZE, *map(_clamped, (rows, width))), n))
+    return n.value
+
+
+def layer_norm_bwd(x, gain, dy, dx, d_gain, d_bias, workspace, eps=1e-5, rms=False, beta=0, stream=None):
+    """dx from x and dy (dx may be either, row for row); d_gain, d_bias (fp32 [width]; None: not wanted) = beta * themselves + the gradients (ah_layer_norm_bwd).
+    workspace: uint8, layer_norm_bwd_workspace(T, width) bytes."""
+    if beta not in (0, 1):
+        _refuse("layer_norm_bwd: beta %s: 0 or 1", beta)
+    c, px, pdy = _norm_args(x, gain, None, dy, eps, rms)
+    width = c.width
+    pdx, c.ld_dx, _ = _any_rows("dx", dx, c.rows, width, x.dtype)
+    pg = _dense("d_gain", d_gain, _F32, width) if d_gain is not None else None
+    pb = _dense("d_bias", d_bias, _F32, width) if d_bias is not None else None
+    work, need = _dense("workspace", workspace, _U8), C.c_uint64()
+    _check(lib.ah_layer_norm_bwd_workspace(c, need))
+    if workspace.numel() < need.value:
+        _refuse("layer_norm_bwd: the workspace holds %d bytes, too few", workspace.numel())
+    _check(lib.ah_layer_norm_bwd(c, px, pdy, pdx, pg, pb, int(beta), work, _stream(stream)))
+
+
+def cross_entropy(logits, targets, loss, d_logits=None, scale=1.0, stream=None):
+    """loss[t] = -log softmax(logits[t])[targets[t]] (fp32 [T]) and, in the same pass, d_logits = scale * its gradient (ah_cross_entropy).  logits, d_logits: [T, vocab], both bf16
+    or both fp32, rows at any distance; d_logits may be logits, row for row.  targets: int32 or int64 [T], -1: none (loss and gradient 0).  scale: a number, or an fp32
+    tensor of one element on the device."""
+    if logits.dim() != 2:
+        _refuse("cross_entropy: logits of shape %s, wanted [T, vocab]", tuple(logits.shape))
+    T, V = logits.shape
+    _fits(T, V)
+    pz, ld_z, act = _any_rows("logits", logits, T, V)
+    at, bits = _indices("targets", targets, T)
+    on_device = isinstance(scale, torch.Tensor)
+    c = _CrossEntropyConfig(_LOSS_SIZE, T, V, act, bits, 0.0 if on_device else scale, _dense("scale", scale, _F32, 1) if on_device else None, ld_z, 0)
+    pd = None
+    if d_logits is not None:
+        pd, c.ld_grad, _ = _any_rows("d_logits", d_logits, T, V, logits.dtype)
+    _check(lib.ah_cross_entropy(c, pz, at, _dense("loss", loss, _F32, T), pd, _stream(stream)))

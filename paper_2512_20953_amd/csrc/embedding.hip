@@ -1,0 +1,395 @@
+// Embedding of tokens and its gradient (declared in include/ah_ops.h).  Bound by HBM: forward reads a row of the table for each token and
+// writes one, backward reads the rows' gradients and writes (or adds to) the rows of the table that occur.
+//
+// Backward: the tokens' numbers are sorted by token, stably (digits of 8 bits from the lowest on), so that the rows that a row of the table
+// is the sum of lie behind each other.  The sorted list is cut into chunks; a block adds up a chunk, writes each sum that begins and ends in it, and leaves the
+// sums that reach over its ends, at most one on either side, as partial sums, which a second kernel adds up in the chunks' order.  So the work of a
+// block does not depend on how often a token occurs, and no row is written by two blocks.
+#include "ah_ops.h"
+#include "capi_util.h"
+#include "wide.h"
+
+#include <algorithm>
+#include <cmath>
+
+using namespace ah;
+
+namespace {
+
+constexpr int NT = 256, NW = NT / 64, kMaxRows = 1 << 25, kMaxVocab = 1 << 30, kMaxWidth = 65536;
+constexpr int kMaxChunks = 2048, kMinChunk = 32;
+constexpr int kItems = 16, kSortBlock = NT * kItems;   // numbers that a block of the sort takes
+
+struct FwdArgs {
+  const void *table, *tokens, *pos_table;
+  const int32_t* positions;
+  void* y;
+  size_t ld_table, ld_y, ld_pos;
+  int T, vocab, width, n_pos, S, bits;
+  float scale;
+};
+
+// 2^LANES lanes to a row, V elements each and time
+template <class TT, class AT, int V>
+__global__ __launch_bounds__(NT) void embedding_fwd_kernel(FwdArgs a, int lanes_log2) {
+  const int lanes = 1 << lanes_log2, lane = threadIdx.x & (lanes - 1), rows = NT >> lanes_log2;
+  for (int64_t t = (int64_t)blockIdx.x * rows + (threadIdx.x >> lanes_log2); t < a.T; t += (int64_t)gridDim.x * rows) {
+    const int64_t token = load_index(a.tokens, t, a.bits);
+    const int pos = a.pos_table ? (a.positions ? a.positions[t] : (int)(t % a.S)) : 0;
+    const bool none = token == -1, bad = (!none && (uint64_t)token >= (uint64_t)a.vocab) || (a.pos_table && (unsigned)pos >= (unsigned)a.n_pos);
+    const TT* row = (const TT*)a.table + (size_t)(none || bad ? 0 : token) * a.ld_table;
+    const TT* prow = (const TT*)a.pos_table + (size_t)(bad ? 0 : pos) * a.ld_pos;
+    AT* y = (AT*)a.y + (size_t)t * a.ld_y;
+    for (int c = lane * V; c < a.width; c += lanes * V) {
+      wide_t<AT, V> out;
+      if (bad) {
+#pragma unroll
+        for (int j = 0; j < V; j++) out[j] = (AT)__builtin_nanf("");
+      } else {
+        float v[V];
+        if (none) {
+#pragma unroll
+          for (int j = 0; j < V; j++) v[j] = 0.f;
+        } else {
+          const wide_t<TT, V> r = load_wide<V>(row + c);
+#pragma unroll
+          for (int j = 0; j < V; j++) v[j] = (float)r[j] * a.scale;
+        }
+        if (a.pos_table) {
+          const wide_t<TT, V> r = load_wide<V>(prow + c);
+#pragma unroll
+          for (int j = 0; j < V; j++) v[j] += (float)r[j];
+        }
+#pragma unroll
+        for (int j = 0; j < V; j++) out[j] = (AT)v[j];
+      }
+      store_wide<V>(y + c, out);
+    }
+  }
+}
+
+// ---- the tokens' numbers sorted by token, those of no row behind the others (their key: vocab)
+__device__ __forceinline__ uint32_t key_of(const void* tokens, size_t t, int bits, int vocab) {
+  const int64_t k = load_index(tokens, t, bits);
+  return (uint64_t)k < (uint64_t)vocab ? (uint32_t)k : (uint32_t)vocab;
+}
+
+struct SortArgs {
+  const void* tokens;           // the first digit's keys come from here, with the numbers 0 .. T - 1
+  const uint32_t *key_in, *at_in;
+  uint32_t *key_out, *at_out;
+  uint32_t* count;              // [256][blocks]
+  int T, vocab, bits, shift, blocks;
+};
+
+__global__ __launch_bounds__(NT) void digit_count_kernel(SortArgs a) {
+  __shared__ uint32_t n[256];
+  n[threadIdx.x] = 0;
+  __syncthreads();
+  const int first = blockIdx.x * kSortBlock;
+  for (int i = threadIdx.x; i < kSortBlock && first + i < a.T; i += NT) {
+    const uint32_t k = a.tokens ? key_of(a.tokens, first + i, a.bits, a.vocab) : a.key_in[first + i];
+    atomicAdd(&n[(k >> a.shift) & 255], 1u);
+  }
+  __syncthreads();
+  a.count[threadIdx.x * a.blocks + blockIdx.x] = n[threadIdx.x];
+}
+
+// count[i] = the sum of those before it: one block
+__global__ __launch_bounds__(1024) void digit_scan_kernel(uint32_t* count, int n) {
+  __shared__ uint32_t wave_sum[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t before = 0;
+  for (int first = 0; first < n; first += 1024) {
+    const int i = first + threadIdx.x;
+    const uint32_t v = i < n ? count[i] : 0;
+    uint32_t s = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t u = __shfl_up(s, o, 64);
+      if (lane >= o) s += u;
+    }
+    if (lane == 63) wave_sum[wave] = s;
+    __syncthreads();
+    uint32_t base = before, total = before;
+    for (int w = 0; w < 16; w++) {
+      if (w < wave) base += wave_sum[w];
+      total += wave_sum[w];
+    }
+    if (i < n) count[i] = base + s - v;
+    before = total;
+    __syncthreads();
+  }
+}
+
+// A wave takes 64 numbers after the other; among those, a lane's place is behind the lanes before it with the same digit.
+__global__ __launch_bounds__(NT) void digit_place_kernel(SortArgs a) {
+  __shared__ uint32_t place[NW][256];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int first = blockIdx.x * kSortBlock + wave * (kSortBlock / NW);
+  for (int i = threadIdx.x; i < NW * 256; i += NT) place[0][i] = 0;
+  __syncthreads();
+  uint32_t key[kItems], at[kItems];
+#pragma unroll
+  for (int i = 0; i < kItems; i++) {
+    const int t = first + i * 64 + lane;
+    if (t < a.T) {
+      key[i] = a.tokens ? key_of(a.tokens, t, a.bits, a.vocab) : a.key_in[t];
+      at[i] = a.tokens ? t : a.at_in[t];
+      atomicAdd(&place[wave][(key[i] >> a.shift) & 255], 1u);
+    }
+  }
+  __syncthreads();
+  uint32_t base = a.count[threadIdx.x * a.blocks + blockIdx.x];
+#pragma unroll
+  for (int w = 0; w < NW; w++) {
+    const uint32_t n = place[w][threadIdx.x];
+    place[w][threadIdx.x] = base;
+    base += n;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kItems; i++) {
+    const bool on = first + i * 64 + lane < a.T;
+    const uint32_t d = on ? (key[i] >> a.shift) & 255 : 256;
+    uint64_t same = ~0ull;          // lanes with this lane's digit
+#pragma unroll
+    for (int b = 0; b < 9; b++) {
+      const uint64_t m = __ballot((d >> b) & 1);
+      same &= (d >> b) & 1 ? m : ~m;
+    }
+    const int behind = __popcll(same & ((1ull << lane) - 1));
+    if (on) {                       // (the wave's own counters: its accesses follow each other as they are written)
+      volatile uint32_t* mine = &place[wave][d];
+      const uint32_t to = *mine + behind;
+      if (behind == 0) *mine = to + __popcll(same);
+      a.key_out[to] = key[i];
+      a.at_out[to] = at[i];
+    }
+  }
+}
+
+struct BwdArgs {
+  const uint32_t *key, *at;     // sorted
+  const void* dy;
+  float *d, *part;              // part[chunk][2][width]: of the sum that began before the chunk, of that which goes on behind it
+  size_t ld_d, ld_dy;
+  int T, vocab, width, chunk, beta;
+  float scale;
+};
+
+// rows of the table set to zeros
+__global__ __launch_bounds__(NT) void fill_rows_kernel(float* d, size_t ld, int rows, int width, int lanes_log2, int vec) {
+  const int lanes = 1 << lanes_log2, lane = threadIdx.x & (lanes - 1), per = NT >> lanes_log2;
+  for (int64_t r = (int64_t)blockIdx.x * per + (threadIdx.x >> lanes_log2); r < rows; r += (int64_t)gridDim.x * per) {
+    float* p = d + (size_t)r * ld;
+    if (vec) for (int c = lane * 4; c < width; c += lanes * 4) *(f32x4*)(p + c) = f32x4{0.f, 0.f, 0.f, 0.f};
+    else for (int c = lane; c < width; c += lanes) p[c] = 0.f;
+  }
+}
+
+template <int V>
+__device__ __forceinline__ void put(const BwdArgs& a, uint32_t row, int c, const float (&s)[V]) {
+  float* p = a.d + (size_t)row * a.ld_d + c;
+  wide_t<float, V> v;
+#pragma unroll
+  for (int j = 0; j < V; j++) v[j] = s[j] * a.scale;
+  if (a.beta) v += load_wide<V>((const float*)p);
+  store_wide<V>(p, v);
+}
+
+// A block adds up V columns a lane of one chunk.  The list is the same for all lanes: keys and numbers are scalars.
+template <class AT, int V>
+__global__ __launch_bounds__(NT) void embedding_bwd_kernel(BwdArgs a) {
+  constexpr int AHEAD = 8;       // rows in flight
+  const int c = (blockIdx.y * NT + threadIdx.x) * V;
+  const int first = blockIdx.x * a.chunk, end = min(first + a.chunk, a.T);
+  if (c >= a.width) return;
+  const AT* dy = (const AT*)a.dy + c;
+  float s[V];
+#pragma unroll
+  for (int j = 0; j < V; j++) s[j] = 0.f;
+  bool began = first == 0 || a.key[first - 1] != a.key[first];      // whether the present sum began in this chunk
+  for (int i = first; i < end; i += AHEAD) {
+    wide_t<AT, V> r[AHEAD];
+    uint32_t key[AHEAD + 1];
+#pragma unroll
+    for (int k = 0; k < AHEAD; k++) {
+      const int e = min(i + k, a.T - 1);
+      key[k] = a.key[e];
+      if (key[k] < (uint32_t)a.vocab) r[k] = load_wide<V>(dy + (size_t)a.at[e] * a.ld_dy);
+    }
+    key[AHEAD] = a.key[min(i + AHEAD, a.T - 1)];
+#pragma unroll
+    for (int k = 0; k < AHEAD; k++) {
+      if (i + k >= end || key[k] >= (uint32_t)a.vocab) return;       // (tokens of no row: behind all others)
+#pragma unroll
+      for (int j = 0; j < V; j++) s[j] += (float)r[k][j];
+      const bool last = i + k + 1 == a.T || key[k + 1] != key[k], cut = i + k + 1 == end;
+      if (last || cut) {
+        if (last && began) {
+          put<V>(a, key[k], c, s);
+        } else {
+          float* p = a.part + ((size_t)blockIdx.x * 2 + (began ? 1 : 0)) * a.width + c;
+          wide_t<float, V> v;
+#pragma unroll
+          for (int j = 0; j < V; j++) v[j] = s[j];
+          store_wide<V>(p, v);
+        }
+#pragma unroll
+        for (int j = 0; j < V; j++) s[j] = 0.f;
+        began = true;
+      }
+    }
+  }
+}
+
+// The chunk in which a sum begins that goes on behind it adds up what the following ones left of it.
+template <int V>
+__global__ __launch_bounds__(NT) void embedding_join_kernel(BwdArgs a, int chunks) {
+  const int first = blockIdx.x * a.chunk, end = first + a.chunk;
+  if (end >= a.T) return;
+  const uint32_t k = a.key[end - 1];
+  if (k >= (uint32_t)a.vocab || a.key[end] != k) return;
+  if (a.key[first] == k && first > 0 && a.key[first - 1] == k) return;      // it began earlier
+  const int c = (blockIdx.y * NT + threadIdx.x) * V;
+  if (c >= a.width) return;
+  const float* p = a.part + (size_t)blockIdx.x * 2 * a.width + c;
+  wide_t<float, V> s = load_wide<V>(p + a.width);
+  for (int b = blockIdx.x + 1; b < chunks && a.key[(size_t)b * a.chunk] == k; b++) s += load_wide<V>(p + (size_t)(b - blockIdx.x) * 2 * a.width);
+  float v[V];
+#pragma unroll
+  for (int j = 0; j < V; j++) v[j] = s[j];
+  put<V>(a, k, c, v);
+}
+
+int sort_blocks(int T) { return (T + kSortBlock - 1) / kSortBlock; }
+int chunk_of(int T) { return std::max(kMinChunk, (T + kMaxChunks - 1) / kMaxChunks); }
+uint64_t up256(uint64_t n) { return (n + 255) / 256 * 256; }
+
+// Places in the workspace
+struct Places { uint64_t key[2], at[2], count, part, bytes; };
+Places places(const ah_embedding_t* c) {
+  Places p;
+  uint64_t at = 0;
+  auto take = [&](uint64_t bytes) { const uint64_t r = at; at += up256(bytes); return r; };
+  const uint64_t T = std::max(c->rows, 1);
+  for (int i = 0; i < 2; i++) { p.key[i] = take(4 * T); p.at[i] = take(4 * T); }
+  p.count = take(4ull * 256 * sort_blocks((int)T));
+  const uint64_t chunk = chunk_of((int)T), chunks = (T + chunk - 1) / chunk;
+  p.part = take(4ull * chunks * 2 * c->width);
+  p.bytes = at;
+  return p;
+}
+
+int log2_lanes(int width, int v) {   // lanes to a row: as many as have elements to take, at most a block
+  int l = 0;
+  while (l < 8 && (1 << l) * v < width) l++;
+  return l;
+}
+
+int check_sizes(const char* who, const ah_embedding_t* c) {
+  if (!c) return set_error(AH_EINVAL, "%s: config is NULL", who);
+  if (c->struct_size != sizeof(ah_embedding_t)) return set_error(AH_EINVAL, "%s: struct_size %u != %zu", who, c->struct_size, sizeof(ah_embedding_t));
+  if (c->rows < 0 || c->vocab < 1 || c->width < 1) return set_error(AH_EINVAL, "%s: need rows >= 0, vocab >= 1 and width >= 1", who);
+  if (c->rows > kMaxRows || c->vocab > kMaxVocab || c->width > kMaxWidth)
+    return set_error(AH_EUNSUPPORTED, "%s: more than 2^25 rows, a vocabulary of 2^30 or a width of 65536", who);
+  return AH_OK;
+}
+
+int check(const char* who, const ah_embedding_t* c) {
+  if (int rc = check_sizes(who, c)) return rc;
+  if ((c->table_type != AH_BF16 && c->table_type != AH_FP32) || (c->act_type != AH_BF16 && c->act_type != AH_FP32))
+    return set_error(AH_EINVAL, "%s: types must be AH_BF16 or AH_FP32", who);
+  if (c->token_bits != 32 && c->token_bits != 64) return set_error(AH_EINVAL, "%s: token_bits %d: 32 or 64", who, c->token_bits);
+  if (!std::isfinite(c->scale)) return set_error(AH_EINVAL, "%s: scale is not finite", who);
+  for (int64_t ld : {c->ld_table, c->ld_act, c->ld_pos})
+    if (ld != 0 && (ld < c->width || ld > (1ll << 31))) return set_error(AH_EINVAL, "%s: a row stride must be at least the width, %d, and at most 2^31", who, c->width);
+  return AH_OK;
+}
+
+}  // namespace
+
+extern "C" int ah_embedding_fwd(const ah_embedding_t* c, const void* table, const void* tokens, void* y, void* stream) {
+  discard_stale_hip_error();
+  if (int rc = check("ah_embedding_fwd", c)) return rc;
+  const int tb = c->table_type == AH_FP32 ? 4 : 2, ab = c->act_type == AH_FP32 ? 4 : 2;
+  if (c->pos_table) {
+    if (c->n_pos < 1) return set_error(AH_EINVAL, "ah_embedding_fwd: n_pos must be >= 1");
+    if (!c->positions && (c->seq_len < 1 || std::min(c->seq_len, std::max(c->rows, 1)) > c->n_pos))
+      return set_error(AH_EINVAL, "ah_embedding_fwd: seq_len %d needs as many rows of pos_table (n_pos %d)", c->seq_len, c->n_pos);
+    if (!aligned_to(c->pos_table, tb) || !aligned_to(c->positions, 4)) return set_error(AH_EINVAL, "ah_embedding_fwd: pos_table or positions is misaligned");
+  }
+  if (c->rows == 0) return AH_OK;
+  if (!table || !tokens || !y || !aligned_to(table, tb) || !aligned_to(tokens, c->token_bits / 8) || !aligned_to(y, ab))
+    return set_error(AH_EINVAL, "ah_embedding_fwd: table, tokens or y is NULL or misaligned");
+  FwdArgs a = {};
+  a.table = table; a.tokens = tokens; a.pos_table = c->pos_table; a.positions = c->positions; a.y = y;
+  a.ld_table = c->ld_table ? c->ld_table : c->width; a.ld_y = c->ld_act ? c->ld_act : c->width; a.ld_pos = c->ld_pos ? c->ld_pos : c->width;
+  a.T = c->rows; a.vocab = c->vocab; a.width = c->width; a.n_pos = c->n_pos; a.S = c->seq_len; a.bits = c->token_bits; a.scale = c->scale;
+  const bool wide = c->width % 8 == 0 && rows16(table, a.ld_table, tb) && rows16(y, a.ld_y, ab) && (!a.pos_table || rows16(a.pos_table, a.ld_pos, tb));
+  const int l = log2_lanes(c->width, wide ? 8 : 1), per = NT >> l;
+  const int blocks = std::min((c->rows + per - 1) / per, 1 << 22);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(NT), 0, (hipStream_t)stream, a, l); };
+  auto by_act = [&](auto t) {
+    typedef decltype(t) TT;
+    if (ab == 4) { if (wide) go(embedding_fwd_kernel<TT, float, 8>); else go(embedding_fwd_kernel<TT, float, 1>); }
+    else { if (wide) go(embedding_fwd_kernel<TT, bf16, 8>); else go(embedding_fwd_kernel<TT, bf16, 1>); }
+  };
+  if (tb == 4) by_act(float());
+  else by_act(bf16());
+  return hip_status(hipGetLastError(), "ah_embedding_fwd");
+}
+
+extern "C" int ah_embedding_bwd_workspace(const ah_embedding_t* c, uint64_t* bytes) {
+  if (!bytes) return set_error(AH_EINVAL, "ah_embedding_bwd_workspace: bytes is NULL");
+  if (int rc = check_sizes("ah_embedding_bwd_workspace", c)) return rc;
+  *bytes = places(c).bytes;
+  return AH_OK;
+}
+
+extern "C" int ah_embedding_bwd(const ah_embedding_t* c, const void* tokens, const void* dy, float* d_table, int beta, void* workspace, void* stream) {
+  discard_stale_hip_error();
+  if (int rc = check("ah_embedding_bwd", c)) return rc;
+  if (beta != 0 && beta != 1) return set_error(AH_EINVAL, "ah_embedding_bwd: beta must be 0 or 1");
+  const int ab = c->act_type == AH_FP32 ? 4 : 2;
+  if (!d_table || !workspace || !aligned_to(d_table, 4) || !aligned_to(workspace, 256)) return set_error(AH_EINVAL, "ah_embedding_bwd: d_table or the workspace is NULL or misaligned");
+  if (c->rows && (!tokens || !dy || !aligned_to(tokens, c->token_bits / 8) || !aligned_to(dy, ab))) return set_error(AH_EINVAL, "ah_embedding_bwd: tokens or dy is NULL or misaligned");
+  const hipStream_t s = (hipStream_t)stream;
+  const int T = c->rows;
+  BwdArgs a = {};
+  a.dy = dy; a.d = d_table; a.ld_d = c->ld_table ? c->ld_table : c->width; a.ld_dy = c->ld_act ? c->ld_act : c->width;
+  a.T = T; a.vocab = c->vocab; a.width = c->width; a.chunk = chunk_of(T); a.beta = beta; a.scale = c->scale;
+  if (!beta) {
+    const int vec = c->width % 4 == 0 && rows16(d_table, a.ld_d, 4), l = log2_lanes(c->width, vec ? 4 : 1), per = NT >> l;
+    hipLaunchKernelGGL(fill_rows_kernel, dim3(std::min<int64_t>(((int64_t)c->vocab + per - 1) / per, 1 << 22)), dim3(NT), 0, s, d_table, a.ld_d, c->vocab, c->width, l, vec);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return hip_status(e, "ah_embedding_bwd");
+  }
+  if (T == 0) return AH_OK;
+  const Places p = places(c);
+  char* w = (char*)workspace;
+  a.part = (float*)(w + p.part);
+  SortArgs q = {};
+  q.T = T; q.vocab = c->vocab; q.bits = c->token_bits; q.blocks = sort_blocks(T); q.count = (uint32_t*)(w + p.count);
+  q.tokens = tokens;
+  int to = 0;
+  for (q.shift = 0; q.shift < 32 && (q.shift == 0 || (c->vocab >> q.shift) != 0); q.shift += 8, to ^= 1) {   // (the largest key is vocab)
+    q.key_out = (uint32_t*)(w + p.key[to]); q.at_out = (uint32_t*)(w + p.at[to]);
+    hipLaunchKernelGGL(digit_count_kernel, dim3(q.blocks), dim3(NT), 0, s, q);
+    hipLaunchKernelGGL(digit_scan_kernel, dim3(1), dim3(1024), 0, s, q.count, 256 * q.blocks);
+    hipLaunchKernelGGL(digit_place_kernel, dim3(q.blocks), dim3(NT), 0, s, q);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return hip_status(e, "ah_embedding_bwd");
+    q.tokens = nullptr;
+    q.key_in = q.key_out; q.at_in = q.at_out;
+  }
+  a.key = q.key_in; a.at = q.at_in;
+  const bool wide = c->width % 8 == 0 && rows16(dy, a.ld_dy, ab) && rows16(d_table, a.ld_d, 4);
+  const int v = wide ? 8 : 1, chunks = (T + a.chunk - 1) / a.chunk;
+  const dim3 grid(chunks, (c->width + NT * v - 1) / (NT * v));
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(NT), 0, s, a); };
+  if (ab == 4) { if (wide) go(embedding_bwd_kernel<float, 8>); else go(embedding_bwd_kernel<float, 1>); }
+  else { if (wide) go(embedding_bwd_kernel<bf16, 8>); else go(embedding_bwd_kernel<bf16, 1>); }
+  if (wide) hipLaunchKernelGGL(embedding_join_kernel<8>, grid, dim3(NT), 0, s, a, chunks);
+  else hipLaunchKernelGGL(embedding_join_kernel<1>, grid, dim3(NT), 0, s, a, chunks);
+  return hip_status(hipGetLastError(), "ah_embedding_bwd");
+}

@@ -1,0 +1,349 @@
+// Layer norm (with or without the mean) of rows of any width, forward and backward (declared in include/ah_ops.h).  Bound by HBM: x read and y written once;
+// backward x and dy read, dx written, and the partial sums behind the gradients of gain and bias.
+//
+// A row stays in the registers of a wave or of a block from its load to its result.  Sums over a row: forward the mean, then the squares around it; backward the sums of x and of
+// w = dy gain, then of (x - mean)^2 and of w (x - mean), from which all that dx needs follows:
+//   n = (x - mean) r;  dx = r (w - mean(w) - n mean(w n)).
+#include "ah_ops.h"
+#include "capi_util.h"
+#include "wide.h"
+
+#include <algorithm>
+#include <cfloat>
+#include <cmath>
+
+using namespace ah;
+
+namespace {
+
+constexpr int kMaxRows = 1 << 25, kMaxWidth = 16384, kMaxBlocks = 512;
+
+struct NormArgs {
+  const void *x, *dy, *gain, *bias;
+  void* out;
+  float* part;                 // [blocks][2][width]
+  size_t ld_x, ld_y, ld_out;
+  int T, width, param32;
+  float eps, inv;              // inv: 1 / width
+};
+
+__device__ __forceinline__ float param(const void* p, int i, int param32) { return param32 ? ((const float*)p)[i] : (float)((const bf16*)p)[i]; }
+
+// Sums of two values over the lanes of a row: NTH = 64: of a wave, else of the block.  `slot` alternates, so that a wave that is ahead does not
+// write where another one still reads.
+template <int NTH>
+__device__ __forceinline__ void row_sums(float& a, float& b, float (&lds)[2][2][16], int slot) {
+  a = wave_sum(a);
+  b = wave_sum(b);
+  if constexpr (NTH > 64) {
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) { lds[slot][0][wave] = a; lds[slot][1][wave] = b; }
+    __syncthreads();
+    a = b = 0.f;
+#pragma unroll
+    for (int w = 0; w < NTH / 64; w++) { a += lds[slot][0][w]; b += lds[slot][1][w]; }
+  }
+}
+
+// NTH lanes to a row, of which each holds CH pieces of V elements; blocks of at least 256 lanes
+template <int NTH> constexpr int block_of() { return NTH < 256 ? 256 : NTH; }
+
+template <class T, int V, int NTH, int CH, bool RMS>
+__global__ __launch_bounds__(block_of<NTH>()) void layer_norm_fwd_kernel(NormArgs a) {
+  __shared__ float lds[2][2][16];
+  constexpr int ROWS = block_of<NTH>() / NTH;
+  const int lane = threadIdx.x % NTH;
+  for (int64_t t = (int64_t)blockIdx.x * ROWS + threadIdx.x / NTH; t < a.T; t += (int64_t)gridDim.x * ROWS) {
+    const T* x = (const T*)a.x + (size_t)t * a.ld_x;
+    T* y = (T*)a.out + (size_t)t * a.ld_out;
+    float v[CH][V], sum = 0.f, none = 0.f;
+#pragma unroll
+    for (int i = 0; i < CH; i++) {
+      const int c = (i * NTH + lane) * V;
+#pragma unroll
+      for (int j = 0; j < V; j++) v[i][j] = 0.f;
+      if (c < a.width) {
+        const wide_t<T, V> r = load_wide<V>(x + c);
+#pragma unroll
+        for (int j = 0; j < V; j++) { v[i][j] = (float)r[j]; sum += v[i][j]; }
+      }
+    }
+    float mean = 0.f;
+    if constexpr (!RMS) {
+      row_sums<NTH>(sum, none, lds, 0);
+      mean = sum * a.inv;
+    }
+    float ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < CH; i++) {
+      if ((i * NTH + lane) * V < a.width) {
+#pragma unroll
+        for (int j = 0; j < V; j++) { const float d = v[i][j] - mean; ss = __builtin_fmaf(d, d, ss); }
+      }
+    }
+    row_sums<NTH>(ss, none, lds, 1);
+    if constexpr (NTH > 64 && RMS) __syncthreads();     // (the one slot is written again in the next row)
+    const float r = rsqrtf(ss * a.inv + a.eps);
+#pragma unroll
+    for (int i = 0; i < CH; i++) {
+      const int c = (i * NTH + lane) * V;
+      if (c < a.width) {
+        wide_t<T, V> o;
+#pragma unroll
+        for (int j = 0; j < V; j++) {
+          float n = (v[i][j] - mean) * r;
+          if (a.gain) n *= param(a.gain, c + j, a.param32);
+          if (a.bias) n += param(a.bias, c + j, a.param32);
+          o[j] = (T)n;
+        }
+        store_wide<V>(y + c, o);
+      }
+    }
+  }
+}
+
+template <class T, int V, int NTH, int CH, bool RMS>
+__global__ __launch_bounds__(block_of<NTH>()) void layer_norm_bwd_kernel(NormArgs a) {
+  __shared__ float lds[2][2][16];
+  constexpr int ROWS = block_of<NTH>() / NTH;
+  const int lane = threadIdx.x % NTH;
+  float dg[CH][V], db[CH][V];
+#pragma unroll
+  for (int i = 0; i < CH; i++)
+#pragma unroll
+    for (int j = 0; j < V; j++) dg[i][j] = db[i][j] = 0.f;
+  for (int64_t t = (int64_t)blockIdx.x * ROWS + threadIdx.x / NTH; t < a.T; t += (int64_t)gridDim.x * ROWS) {
+    const T *x = (const T*)a.x + (size_t)t * a.ld_x, *dy = (const T*)a.dy + (size_t)t * a.ld_y;
+    T* dx = (T*)a.out + (size_t)t * a.ld_out;
+    wide_t<T, V> xv[CH], yv[CH];
+    float sx = 0.f, sw = 0.f;
+#pragma unroll
+    for (int i = 0; i < CH; i++) {
+      const int c = (i * NTH + lane) * V;
+      if (c < a.width) {
+        xv[i] = load_wide<V>(x + c);
+        yv[i] = load_wide<V>(dy + c);
+      }
+    }
+    auto w_of = [&](int i, int j, int c) { const float g = (float)yv[i][j]; return a.gain ? g * param(a.gain, c + j, a.param32) : g; };
+    float mean = 0.f, mean_w = 0.f;
+    if constexpr (!RMS) {
+#pragma unroll
+      for (int i = 0; i < CH; i++) {
+        const int c = (i * NTH + lane) * V;
+        if (c < a.width) {
+#pragma unroll
+          for (int j = 0; j < V; j++) { sx += (float)xv[i][j]; sw += w_of(i, j, c); }
+        }
+      }
+      row_sums<NTH>(sx, sw, lds, 0);
+      mean = sx * a.inv;
+      mean_w = sw * a.inv;
+    }
+    float ss = 0.f, sd = 0.f;
+#pragma unroll
+    for (int i = 0; i < CH; i++) {
+      const int c = (i * NTH + lane) * V;
+      if (c < a.width) {
+#pragma unroll
+        for (int j = 0; j < V; j++) {
+          const float d = (float)xv[i][j] - mean;
+          ss = __builtin_fmaf(d, d, ss);
+          sd = __builtin_fmaf(d, w_of(i, j, c), sd);
+        }
+      }
+    }
+    row_sums<NTH>(ss, sd, lds, 1);
+    if constexpr (NTH > 64 && RMS) __syncthreads();
+    const float r = rsqrtf(ss * a.inv + a.eps), k = sd * a.inv * r * r;     // n mean(w n) = (x - mean) k
+#pragma unroll
+    for (int i = 0; i < CH; i++) {
+      const int c = (i * NTH + lane) * V;
+      if (c < a.width) {
+        wide_t<T, V> o;
+#pragma unroll
+        for (int j = 0; j < V; j++) {
+          const float d = (float)xv[i][j] - mean, g = (float)yv[i][j];
+          dg[i][j] = __builtin_fmaf(g, d * r, dg[i][j]);
+          db[i][j] += g;
+          o[j] = (T)(r * (w_of(i, j, c) - mean_w - d * k));
+        }
+        store_wide<V>(dx + c, o);
+      }
+    }
+  }
+  // the block's rows of partial sums: rows side by side meet in LDS
+  float* part = a.part + (size_t)blockIdx.x * 2 * a.width;
+  if constexpr (ROWS > 1) {
+    __shared__ float red[ROWS][2][NTH * CH * V];
+    const int row = threadIdx.x / NTH;
+#pragma unroll
+    for (int i = 0; i < CH; i++)
+#pragma unroll
+      for (int j = 0; j < V; j++) {
+        const int c = (i * NTH + lane) * V + j;
+        red[row][0][c] = dg[i][j];
+        red[row][1][c] = db[i][j];
+      }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * a.width; i += block_of<NTH>()) {
+      const int which = i >= a.width, c = which ? i - a.width : i;
+      float s = red[0][which][c];
+#pragma unroll
+      for (int k = 1; k < ROWS; k++) s += red[k][which][c];
+      part[i] = s;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < CH; i++) {
+      const int c = (i * NTH + lane) * V;
+      if (c < a.width) {
+#pragma unroll
+        for (int j = 0; j < V; j++) { part[c + j] = dg[i][j]; part[a.width + c + j] = db[i][j]; }
+      }
+    }
+  }
+}
+
+// d[c] = beta * d[c] + the sum of part[b][which][c] over the blocks: 64 columns a block, every fourth row a wave
+__global__ __launch_bounds__(1024) void norm_fold_kernel(const float* part, int blocks, int width, float* d_gain, float* d_bias, int beta) {
+  __shared__ float red[16][64];
+  float* d = blockIdx.y ? d_bias : d_gain;
+  if (!d) return;
+  const int c = blockIdx.x * 64 + (threadIdx.x & 63), wave = threadIdx.x >> 6;
+  float s = 0.f;
+  if (c < width) {
+    const float* p = part + (size_t)blockIdx.y * width + c;
+#pragma unroll 8
+    for (int b = wave; b < blocks; b += 16) s += p[(size_t)b * 2 * width];
+  }
+  red[wave][threadIdx.x & 63] = s;
+  __syncthreads();
+  if (wave == 0 && c < width) {
+#pragma unroll
+    for (int w = 1; w < 16; w++) s += red[w][threadIdx.x];
+    d[c] = beta ? d[c] + s : s;
+  }
+}
+
+int check_sizes(const char* who, const ah_layer_norm_t* c) {
+  if (!c) return set_error(AH_EINVAL, "%s: config is NULL", who);
+  if (c->struct_size != sizeof(ah_layer_norm_t)) return set_error(AH_EINVAL, "%s: struct_size %u != %zu", who, c->struct_size, sizeof(ah_layer_norm_t));
+  if (c->rows < 0 || c->width < 1) return set_error(AH_EINVAL, "%s: need rows >= 0 and width >= 1", who);
+  if (c->rows > kMaxRows || c->width > kMaxWidth) return set_error(AH_EUNSUPPORTED, "%s: more than 2^25 rows or a width of 16384", who);
+  return AH_OK;
+}
+
+int check(const char* who, const ah_layer_norm_t* c) {
+  if (int rc = check_sizes(who, c)) return rc;
+  if ((c->act_type != AH_BF16 && c->act_type != AH_FP32) || (c->param_type != AH_BF16 && c->param_type != AH_FP32))
+    return set_error(AH_EINVAL, "%s: types must be AH_BF16 or AH_FP32", who);
+  if (c->rms != 0 && c->rms != 1) return set_error(AH_EINVAL, "%s: rms must be 0 or 1", who);
+  if (!(c->eps >= FLT_MIN) || !std::isfinite(c->eps)) return set_error(AH_EINVAL, "%s: eps must be finite and at least 2^-126", who);
+  const int pb = c->param_type == AH_FP32 ? 4 : 2;
+  if (!aligned_to(c->gain, pb) || !aligned_to(c->bias, pb)) return set_error(AH_EINVAL, "%s: gain or bias is misaligned", who);
+  for (int64_t ld : {c->ld_x, c->ld_y, c->ld_dx})
+    if (ld != 0 && (ld < c->width || ld > (1ll << 31))) return set_error(AH_EINVAL, "%s: a row stride must be at least the width, %d, and at most 2^31", who, c->width);
+  return AH_OK;
+}
+
+NormArgs args(const ah_layer_norm_t* c, const void* x, const void* dy, void* out, int64_t ld_out, float* part) {
+  NormArgs a = {};
+  a.x = x; a.dy = dy; a.out = out; a.gain = c->gain; a.bias = c->bias; a.part = part;
+  a.ld_x = c->ld_x ? c->ld_x : c->width; a.ld_y = c->ld_y ? c->ld_y : c->width; a.ld_out = ld_out ? ld_out : c->width;
+  a.T = c->rows; a.width = c->width; a.param32 = c->param_type == AH_FP32; a.eps = c->eps; a.inv = 1.f / c->width;
+  return a;
+}
+
+// Lanes to a row, by its width alone
+int row_lanes(int width) { return width <= 1024 ? 64 : width <= 4096 ? 256 : 1024; }
+int bwd_blocks(const ah_layer_norm_t* c) {
+  const int rows = std::max(1, 256 / row_lanes(c->width));
+  return std::max(1, std::min(kMaxBlocks, (c->rows + rows - 1) / rows));
+}
+
+// go(lanes, pieces a lane) as constants for rows of `width` elements in pieces of V
+template <int V, class F>
+void by_width(int width, const F& go) {
+  typedef std::integral_constant<int, 64> L64;
+  typedef std::integral_constant<int, 256> L256;
+  typedef std::integral_constant<int, 1024> L1024;
+  typedef std::integral_constant<int, 8 / V> One;         // 8 elements a lane
+  typedef std::integral_constant<int, 16 / V> Two;
+  if (width <= 512) go(L64(), One());
+  else if (width <= 1024) go(L64(), Two());
+  else if (width <= 2048) go(L256(), One());
+  else if (width <= 4096) go(L256(), Two());
+  else if (width <= 8192) go(L1024(), One());
+  else go(L1024(), Two());
+}
+
+template <bool BWD>
+hipError_t run(const NormArgs& a, bool act32, bool rms, bool wide, int blocks, hipStream_t s) {
+  auto typed = [&](auto t, auto v, auto r) {
+    typedef decltype(t) T;
+    constexpr int V = decltype(v)::value;
+    constexpr bool RMS = decltype(r)::value;
+    by_width<V>(a.width, [&](auto lanes, auto pieces) {
+      constexpr int NTH = decltype(lanes)::value, CH = decltype(pieces)::value;
+      if constexpr (BWD) hipLaunchKernelGGL((layer_norm_bwd_kernel<T, V, NTH, CH, RMS>), dim3(blocks), dim3(block_of<NTH>()), 0, s, a);
+      else hipLaunchKernelGGL((layer_norm_fwd_kernel<T, V, NTH, CH, RMS>), dim3(blocks), dim3(block_of<NTH>()), 0, s, a);
+    });
+  };
+  auto by_kind = [&](auto t, auto v) {
+    if (rms) typed(t, v, std::true_type());
+    else typed(t, v, std::false_type());
+  };
+  auto by_align = [&](auto t) {
+    if (wide) by_kind(t, std::integral_constant<int, 8>());
+    else by_kind(t, std::integral_constant<int, 1>());
+  };
+  if (act32) by_align(float());
+  else by_align(bf16());
+  return hipGetLastError();
+}
+
+// Results in the place of what a call reads: row for row only
+bool shifted(const void* in, size_t ld_in, const NormArgs& a) { return a.out == in && a.T > 1 && ld_in != a.ld_out; }
+
+}  // namespace
+
+extern "C" int ah_layer_norm_fwd(const ah_layer_norm_t* c, const void* x, void* y, void* stream) {
+  discard_stale_hip_error();
+  if (int rc = check("ah_layer_norm_fwd", c)) return rc;
+  if (c->rows == 0) return AH_OK;
+  const int ab = c->act_type == AH_FP32 ? 4 : 2;
+  if (!x || !y || !aligned_to(x, ab) || !aligned_to(y, ab)) return set_error(AH_EINVAL, "ah_layer_norm_fwd: x or y is NULL or misaligned");
+  const NormArgs a = args(c, x, nullptr, y, c->ld_y, nullptr);
+  if (shifted(x, a.ld_x, a)) return set_error(AH_EINVAL, "ah_layer_norm_fwd: y in the place of x needs x's row stride");
+  const bool wide = c->width % 8 == 0 && rows16(x, a.ld_x, ab) && rows16(y, a.ld_out, ab);
+  const int rows = std::max(1, 256 / row_lanes(c->width));
+  return hip_status(run<false>(a, ab == 4, c->rms, wide, std::min((c->rows + rows - 1) / rows, 1 << 21), (hipStream_t)stream), "ah_layer_norm_fwd");
+}
+
+extern "C" int ah_layer_norm_bwd_workspace(const ah_layer_norm_t* c, uint64_t* bytes) {
+  if (!bytes) return set_error(AH_EINVAL, "ah_layer_norm_bwd_workspace: bytes is NULL");
+  if (int rc = check_sizes("ah_layer_norm_bwd_workspace", c)) return rc;
+  *bytes = (uint64_t)bwd_blocks(c) * 2 * c->width * sizeof(float);
+  return AH_OK;
+}
+
+extern "C" int ah_layer_norm_bwd(const ah_layer_norm_t* c, const void* x, const void* dy, void* dx, float* d_gain, float* d_bias, int beta, void* workspace, void* stream) {
+  discard_stale_hip_error();
+  if (int rc = check("ah_layer_norm_bwd", c)) return rc;
+  if (beta != 0 && beta != 1) return set_error(AH_EINVAL, "ah_layer_norm_bwd: beta must be 0 or 1");
+  const int ab = c->act_type == AH_FP32 ? 4 : 2;
+  if (!workspace || !aligned_to(workspace, 16) || !aligned_to(d_gain, 4) || !aligned_to(d_bias, 4))
+    return set_error(AH_EINVAL, "ah_layer_norm_bwd: the workspace is NULL or it or a gradient is misaligned");
+  if (c->rows && (!x || !dy || !dx || !aligned_to(x, ab) || !aligned_to(dy, ab) || !aligned_to(dx, ab))) return set_error(AH_EINVAL, "ah_layer_norm_bwd: x, dy or dx is NULL or misaligned");
+  const NormArgs a = args(c, x, dy, dx, c->ld_dx, (float*)workspace);
+  if (shifted(x, a.ld_x, a) || shifted(dy, a.ld_y, a)) return set_error(AH_EINVAL, "ah_layer_norm_bwd: dx in the place of x or dy needs its row stride");
+  const bool wide = c->width % 8 == 0 && rows16(x, a.ld_x, ab) && rows16(dy, a.ld_y, ab) && rows16(dx, a.ld_out, ab);
+  const int blocks = bwd_blocks(c);
+  hipError_t e = run<true>(a, ab == 4, c->rms, wide, blocks, (hipStream_t)stream);      // (no rows: writes zeros)
+  if (e == hipSuccess && (d_gain || d_bias)) {
+    hipLaunchKernelGGL(norm_fold_kernel, dim3((c->width + 63) / 64, 2), dim3(1024), 0, (hipStream_t)stream, a.part, blocks, c->width, d_gain, d_bias, beta);
+    e = hipGetLastError();
+  }
+  return hip_status(e, "ah_layer_norm_bwd");
+}
