@@ -17,7 +17,9 @@ using namespace ah;
 namespace {
 
 constexpr int NT = 256, NW = NT / 64, kMaxRows = 1 << 25, kMaxVocab = 1 << 30, kMaxWidth = 65536;
-constexpr int kMaxChunks = 2048, kMinChunk = 32;
+constexpr int kFlight = 2;                             // pieces of a row that a lane has in flight
+constexpr int kMaxChunks = 2048, kMinChunk = 16;
+constexpr int kFillBlocks = 1024;                      // beside the sort of few tokens
 constexpr int kItems = 16, kSortBlock = NT * kItems;   // numbers that a block of the sort takes
 
 struct FwdArgs {
@@ -40,30 +42,32 @@ __global__ __launch_bounds__(NT) void embedding_fwd_kernel(FwdArgs a, int lanes_
     const TT* row = (const TT*)a.table + (size_t)(none || bad ? 0 : token) * a.ld_table;
     const TT* prow = (const TT*)a.pos_table + (size_t)(bad ? 0 : pos) * a.ld_pos;
     AT* y = (AT*)a.y + (size_t)t * a.ld_y;
-    for (int c = lane * V; c < a.width; c += lanes * V) {
+    if (bad) {
       wide_t<AT, V> out;
-      if (bad) {
 #pragma unroll
-        for (int j = 0; j < V; j++) out[j] = (AT)__builtin_nanf("");
-      } else {
-        float v[V];
-        if (none) {
+      for (int j = 0; j < V; j++) out[j] = (AT)__builtin_nanf("");
+      for (int c = lane * V; c < a.width; c += lanes * V) store_wide<V>(y + c, out);
+      continue;
+    }
+    for (int c = lane * V; c < a.width; c += kFlight * lanes * V) {
+      wide_t<TT, V> e[kFlight] = {}, q[kFlight] = {};
 #pragma unroll
-          for (int j = 0; j < V; j++) v[j] = 0.f;
-        } else {
-          const wide_t<TT, V> r = load_wide<V>(row + c);
-#pragma unroll
-          for (int j = 0; j < V; j++) v[j] = (float)r[j] * a.scale;
-        }
-        if (a.pos_table) {
-          const wide_t<TT, V> r = load_wide<V>(prow + c);
-#pragma unroll
-          for (int j = 0; j < V; j++) v[j] += (float)r[j];
-        }
-#pragma unroll
-        for (int j = 0; j < V; j++) out[j] = (AT)v[j];
+      for (int i = 0; i < kFlight; i++) {
+        const int at = c + i * lanes * V;
+        if (at < a.width && !none) e[i] = load_wide<V>(row + at);
+        if (at < a.width && a.pos_table) q[i] = load_wide<V>(prow + at);
       }
-      store_wide<V>(y + c, out);
+#pragma unroll
+      for (int i = 0; i < kFlight; i++) {
+        const int at = c + i * lanes * V;
+        wide_t<AT, V> out;
+#pragma unroll
+        for (int j = 0; j < V; j++) {
+          const float v = none ? 0.f : (float)e[i][j] * a.scale;
+          out[j] = (AT)(a.pos_table ? v + (float)q[i][j] : v);
+        }
+        if (at < a.width) store_wide<V>(y + at, out);
+      }
     }
   }
 }
@@ -169,6 +173,109 @@ __global__ __launch_bounds__(NT) void digit_place_kernel(SortArgs a) {
   }
 }
 
+// All of it in one block, for as many tokens as its LDS holds: the list goes through LDS once a digit.
+constexpr int kSmall = 8192, kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64, kSmallItems = kSmall / kSmallThreads;
+struct FillArgs {
+  float* d;
+  size_t ld;
+  int rows, width, lanes_log2, vec;
+};
+__device__ __forceinline__ void fill_rows(const FillArgs& f, int64_t block, int64_t blocks, int threads) {
+  const int lanes = 1 << f.lanes_log2, lane = threadIdx.x & (lanes - 1), per = threads >> f.lanes_log2;
+  for (int64_t r = block * per + (threadIdx.x >> f.lanes_log2); r < f.rows; r += blocks * per) {
+    float* p = f.d + (size_t)r * f.ld;
+    if (f.vec) for (int c = lane * 4; c < f.width; c += lanes * 4) *(f32x4*)(p + c) = f32x4{0.f, 0.f, 0.f, 0.f};
+    else for (int c = lane; c < f.width; c += lanes) p[c] = 0.f;
+  }
+}
+
+// BITS of a digit; the blocks behind the first set the rows of the table to zeros meanwhile (f.d NULL: there are none)
+template <int BITS>
+__global__ __launch_bounds__(kSmallThreads) void small_sort_kernel(SortArgs a, int passes, FillArgs f) {
+  constexpr int D = 1 << BITS, PER = (D + 63) / 64;
+  __shared__ uint32_t keys[kSmall], ats[kSmall], place[kSmallWaves][D], total[D];
+  if (blockIdx.x > 0) return fill_rows(f, blockIdx.x - 1, gridDim.x - 1, kSmallThreads);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int first = wave * 64 * kSmallItems;         // a wave's part of the list
+  uint32_t key[kSmallItems], at[kSmallItems];
+#pragma unroll
+  for (int i = 0; i < kSmallItems; i++) {
+    const int t = first + i * 64 + lane;
+    at[i] = t;
+    key[i] = t < a.T ? key_of(a.tokens, t, a.bits, a.vocab) : ~0u;       // (behind all others: every digit the largest)
+  }
+  for (int p = 0; p < passes; p++) {
+    const int shift = p * BITS;
+    for (int i = threadIdx.x; i < kSmallWaves * D; i += kSmallThreads) place[0][i] = 0;
+    __syncthreads();
+    uint32_t behind[kSmallItems];
+    // a lane's place among the wave's numbers of its digit: those that the wave took before, and those of lanes before it
+#pragma unroll
+    for (int i = 0; i < kSmallItems; i++) {
+      const uint32_t d = (key[i] >> shift) & (D - 1);
+      uint64_t same = ~0ull;
+#pragma unroll
+      for (int b = 0; b < BITS; b++) {
+        const uint64_t m = __ballot((d >> b) & 1);
+        same &= (d >> b) & 1 ? m : ~m;
+      }
+      volatile uint32_t* mine = &place[wave][d];
+      const uint32_t before = *mine, among = __popcll(same & ((1ull << lane) - 1));
+      behind[i] = before + among;
+      if (among == 0) *mine = before + __popcll(same);
+    }
+    __syncthreads();
+    // where a digit begins: sums over the waves, then over the digits before it
+    if (threadIdx.x < D) {
+      uint32_t n = 0;
+#pragma unroll
+      for (int w = 0; w < kSmallWaves; w++) {
+        const uint32_t m = place[w][threadIdx.x];
+        place[w][threadIdx.x] = n;
+        n += m;
+      }
+      total[threadIdx.x] = n;
+    }
+    __syncthreads();
+    if (wave == 0) {
+      uint32_t own[PER], n = 0;
+#pragma unroll
+      for (int i = 0; i < PER; i++) {
+        own[i] = n;
+        n += total[lane * PER + i];
+      }
+      uint32_t s = n;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t u = __shfl_up(s, o, 64);
+        if (lane >= o) s += u;
+      }
+#pragma unroll
+      for (int i = 0; i < PER; i++) total[lane * PER + i] = s - n + own[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSmallItems; i++) {
+      const uint32_t d = (key[i] >> shift) & (D - 1), to = total[d] + place[wave][d] + behind[i];
+      keys[to] = key[i];
+      ats[to] = at[i];
+    }
+    __syncthreads();
+    if (p + 1 < passes) {
+#pragma unroll
+      for (int i = 0; i < kSmallItems; i++) {
+        key[i] = keys[first + i * 64 + lane];
+        at[i] = ats[first + i * 64 + lane];
+      }
+      __syncthreads();
+    }
+  }
+  for (int i = threadIdx.x; i < a.T; i += kSmallThreads) {
+    a.key_out[i] = keys[i];
+    a.at_out[i] = ats[i];
+  }
+}
+
 struct BwdArgs {
   const uint32_t *key, *at;     // sorted
   const void* dy;
@@ -178,15 +285,7 @@ struct BwdArgs {
   float scale;
 };
 
-// rows of the table set to zeros
-__global__ __launch_bounds__(NT) void fill_rows_kernel(float* d, size_t ld, int rows, int width, int lanes_log2, int vec) {
-  const int lanes = 1 << lanes_log2, lane = threadIdx.x & (lanes - 1), per = NT >> lanes_log2;
-  for (int64_t r = (int64_t)blockIdx.x * per + (threadIdx.x >> lanes_log2); r < rows; r += (int64_t)gridDim.x * per) {
-    float* p = d + (size_t)r * ld;
-    if (vec) for (int c = lane * 4; c < width; c += lanes * 4) *(f32x4*)(p + c) = f32x4{0.f, 0.f, 0.f, 0.f};
-    else for (int c = lane; c < width; c += lanes) p[c] = 0.f;
-  }
-}
+__global__ __launch_bounds__(NT) void fill_rows_kernel(FillArgs f) { fill_rows(f, blockIdx.x, gridDim.x, NT); }
 
 template <int V>
 __device__ __forceinline__ void put(const BwdArgs& a, uint32_t row, int c, const float (&s)[V]) {
@@ -360,9 +459,16 @@ extern "C" int ah_embedding_bwd(const ah_embedding_t* c, const void* tokens, con
   BwdArgs a = {};
   a.dy = dy; a.d = d_table; a.ld_d = c->ld_table ? c->ld_table : c->width; a.ld_dy = c->ld_act ? c->ld_act : c->width;
   a.T = T; a.vocab = c->vocab; a.width = c->width; a.chunk = chunk_of(T); a.beta = beta; a.scale = c->scale;
+  FillArgs f = {};
   if (!beta) {
-    const int vec = c->width % 4 == 0 && rows16(d_table, a.ld_d, 4), l = log2_lanes(c->width, vec ? 4 : 1), per = NT >> l;
-    hipLaunchKernelGGL(fill_rows_kernel, dim3(std::min<int64_t>(((int64_t)c->vocab + per - 1) / per, 1 << 22)), dim3(NT), 0, s, d_table, a.ld_d, c->vocab, c->width, l, vec);
+    f.d = d_table; f.ld = a.ld_d; f.rows = c->vocab; f.width = c->width;
+    f.vec = c->width % 4 == 0 && rows16(d_table, a.ld_d, 4);
+    f.lanes_log2 = log2_lanes(c->width, f.vec ? 4 : 1);
+  }
+  const bool small = T > 0 && T <= kSmall;
+  if (!beta && !small) {
+    const int per = NT >> f.lanes_log2;
+    hipLaunchKernelGGL(fill_rows_kernel, dim3(std::min<int64_t>(((int64_t)c->vocab + per - 1) / per, 1 << 22)), dim3(NT), 0, s, f);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return hip_status(e, "ah_embedding_bwd");
   }
   if (T == 0) return AH_OK;
@@ -372,15 +478,27 @@ extern "C" int ah_embedding_bwd(const ah_embedding_t* c, const void* tokens, con
   SortArgs q = {};
   q.T = T; q.vocab = c->vocab; q.bits = c->token_bits; q.blocks = sort_blocks(T); q.count = (uint32_t*)(w + p.count);
   q.tokens = tokens;
-  int to = 0;
-  for (q.shift = 0; q.shift < 32 && (q.shift == 0 || (c->vocab >> q.shift) != 0); q.shift += 8, to ^= 1) {   // (the largest key is vocab)
-    q.key_out = (uint32_t*)(w + p.key[to]); q.at_out = (uint32_t*)(w + p.at[to]);
-    hipLaunchKernelGGL(digit_count_kernel, dim3(q.blocks), dim3(NT), 0, s, q);
-    hipLaunchKernelGGL(digit_scan_kernel, dim3(1), dim3(1024), 0, s, q.count, 256 * q.blocks);
-    hipLaunchKernelGGL(digit_place_kernel, dim3(q.blocks), dim3(NT), 0, s, q);
+  int key_bits = 1;                                       // of the largest key, vocab
+  while (key_bits < 31 && (c->vocab >> key_bits) != 0) key_bits++;
+  if (small) {
+    q.key_out = (uint32_t*)(w + p.key[0]); q.at_out = (uint32_t*)(w + p.at[0]);
+    const int blocks = beta ? 1 : 1 + std::min<int64_t>(((int64_t)c->vocab * c->width + 65535) / 65536, kFillBlocks);
+    auto go = [&](auto kernel, int bits) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kSmallThreads), 0, s, q, (key_bits + bits - 1) / bits, f); };
+    if ((key_bits + 7) / 8 > (key_bits + 8) / 9) go(small_sort_kernel<9>, 9);        // (17 and 18 bits: two passes for three)
+    else go(small_sort_kernel<8>, 8);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return hip_status(e, "ah_embedding_bwd");
-    q.tokens = nullptr;
     q.key_in = q.key_out; q.at_in = q.at_out;
+  } else {
+    int to = 0;
+    for (q.shift = 0; q.shift < key_bits; q.shift += 8, to ^= 1) {
+      q.key_out = (uint32_t*)(w + p.key[to]); q.at_out = (uint32_t*)(w + p.at[to]);
+      hipLaunchKernelGGL(digit_count_kernel, dim3(q.blocks), dim3(NT), 0, s, q);
+      hipLaunchKernelGGL(digit_scan_kernel, dim3(1), dim3(1024), 0, s, q.count, 256 * q.blocks);
+      hipLaunchKernelGGL(digit_place_kernel, dim3(q.blocks), dim3(NT), 0, s, q);
+      if (hipError_t e = hipGetLastError(); e != hipSuccess) return hip_status(e, "ah_embedding_bwd");
+      q.tokens = nullptr;
+      q.key_in = q.key_out; q.at_in = q.at_out;
+    }
   }
   a.key = q.key_in; a.at = q.at_in;
   const bool wide = c->width % 8 == 0 && rows16(dy, a.ld_dy, ab) && rows16(d_table, a.ld_d, 4);

@@ -16,18 +16,16 @@ using namespace ah;
 
 namespace {
 
-constexpr int kMaxRows = 1 << 25, kMaxWidth = 16384, kMaxBlocks = 512;
+constexpr int kMaxRows = 1 << 25, kMaxWidth = 16384, kMaxBlocks = 512, kFwdBlocks = 2048;   // blocks of 256 lanes forward
 
 struct NormArgs {
   const void *x, *dy, *gain, *bias;
   void* out;
   float* part;                 // [blocks][2][width]
   size_t ld_x, ld_y, ld_out;
-  int T, width, param32;
+  int T, width, params16;      // params16: gain and bias can be read in whole pieces
   float eps, inv;              // inv: 1 / width
 };
-
-__device__ __forceinline__ float param(const void* p, int i, int param32) { return param32 ? ((const float*)p)[i] : (float)((const bf16*)p)[i]; }
 
 // Sums of two values over the lanes of a row: NTH = 64: of a wave, else of the block.  `slot` alternates, so that a wave that is ahead does not
 // write where another one still reads.
@@ -48,114 +46,142 @@ __device__ __forceinline__ void row_sums(float& a, float& b, float (&lds)[2][2][
 // NTH lanes to a row, of which each holds CH pieces of V elements; blocks of at least 256 lanes
 template <int NTH> constexpr int block_of() { return NTH < 256 ? 256 : NTH; }
 
-template <class T, int V, int NTH, int CH, bool RMS>
+// Gain or bias of the lane's columns, kept as they lie in memory; NULL: `none` in all of them.  W: in whole pieces (V elements, 16-byte aligned)
+template <class PT, int V, int NTH, int CH>
+__device__ __forceinline__ void load_param(wide_t<PT, V> (&r)[CH], const void* p, float none, int lane, int width, bool whole) {
+#pragma unroll
+  for (int i = 0; i < CH; i++) {
+    const int c = (i * NTH + lane) * V;
+#pragma unroll
+    for (int j = 0; j < V; j++) r[i][j] = (PT)none;
+    if (!p || c >= width) continue;
+    if (whole) {
+      r[i] = load_wide<V>((const PT*)p + c);
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; j++) r[i][j] = ((const PT*)p)[c + j];
+    }
+  }
+}
+
+template <class T, int V, int NTH, int CH>
+__device__ __forceinline__ void load_row(wide_t<T, V> (&r)[CH], const T* p, int lane, int width) {
+#pragma unroll
+  for (int i = 0; i < CH; i++) {
+    const int c = (i * NTH + lane) * V;
+    if (c < width) r[i] = load_wide<V>(p + c);
+  }
+}
+
+// A block takes rows gridDim apart and asks for the next one's elements before it works on the present one's.
+template <class T, class PT, int V, int NTH, int CH, bool RMS>
 __global__ __launch_bounds__(block_of<NTH>()) void layer_norm_fwd_kernel(NormArgs a) {
   __shared__ float lds[2][2][16];
   constexpr int ROWS = block_of<NTH>() / NTH;
   const int lane = threadIdx.x % NTH;
-  for (int64_t t = (int64_t)blockIdx.x * ROWS + threadIdx.x / NTH; t < a.T; t += (int64_t)gridDim.x * ROWS) {
-    const T* x = (const T*)a.x + (size_t)t * a.ld_x;
-    T* y = (T*)a.out + (size_t)t * a.ld_out;
-    float v[CH][V], sum = 0.f, none = 0.f;
+  const int64_t step = (int64_t)gridDim.x * ROWS;
+  int64_t t = (int64_t)blockIdx.x * ROWS + threadIdx.x / NTH;
+  if (t >= a.T) return;          // (all lanes of a row, which is a block's only one where they meet in LDS)
+  wide_t<PT, V> gain[CH], bias[CH];
+  load_param<PT, V, NTH, CH>(gain, a.gain, 1.f, lane, a.width, a.params16);
+  load_param<PT, V, NTH, CH>(bias, a.bias, 0.f, lane, a.width, a.params16);
+  wide_t<T, V> x[CH], next[CH];
+  load_row<T, V, NTH, CH>(next, (const T*)a.x + (size_t)t * a.ld_x, lane, a.width);
+  for (; t < a.T; t += step) {
 #pragma unroll
-    for (int i = 0; i < CH; i++) {
-      const int c = (i * NTH + lane) * V;
-#pragma unroll
-      for (int j = 0; j < V; j++) v[i][j] = 0.f;
-      if (c < a.width) {
-        const wide_t<T, V> r = load_wide<V>(x + c);
-#pragma unroll
-        for (int j = 0; j < V; j++) { v[i][j] = (float)r[j]; sum += v[i][j]; }
-      }
-    }
-    float mean = 0.f;
+    for (int i = 0; i < CH; i++) x[i] = next[i];
+    if (t + step < a.T) load_row<T, V, NTH, CH>(next, (const T*)a.x + (size_t)(t + step) * a.ld_x, lane, a.width);
+    float mean = 0.f, none = 0.f;
     if constexpr (!RMS) {
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < CH; i++)
+        if ((i * NTH + lane) * V < a.width) {
+#pragma unroll
+          for (int j = 0; j < V; j++) sum += (float)x[i][j];
+        }
       row_sums<NTH>(sum, none, lds, 0);
       mean = sum * a.inv;
     }
     float ss = 0.f;
 #pragma unroll
-    for (int i = 0; i < CH; i++) {
+    for (int i = 0; i < CH; i++)
       if ((i * NTH + lane) * V < a.width) {
 #pragma unroll
-        for (int j = 0; j < V; j++) { const float d = v[i][j] - mean; ss = __builtin_fmaf(d, d, ss); }
+        for (int j = 0; j < V; j++) { const float d = (float)x[i][j] - mean; ss = __builtin_fmaf(d, d, ss); }
       }
-    }
     row_sums<NTH>(ss, none, lds, 1);
     if constexpr (NTH > 64 && RMS) __syncthreads();     // (the one slot is written again in the next row)
     const float r = rsqrtf(ss * a.inv + a.eps);
+    T* y = (T*)a.out + (size_t)t * a.ld_out;
 #pragma unroll
     for (int i = 0; i < CH; i++) {
       const int c = (i * NTH + lane) * V;
       if (c < a.width) {
         wide_t<T, V> o;
 #pragma unroll
-        for (int j = 0; j < V; j++) {
-          float n = (v[i][j] - mean) * r;
-          if (a.gain) n *= param(a.gain, c + j, a.param32);
-          if (a.bias) n += param(a.bias, c + j, a.param32);
-          o[j] = (T)n;
-        }
+        for (int j = 0; j < V; j++) o[j] = (T)__builtin_fmaf(((float)x[i][j] - mean) * r, (float)gain[i][j], (float)bias[i][j]);
         store_wide<V>(y + c, o);
       }
     }
   }
 }
 
-template <class T, int V, int NTH, int CH, bool RMS>
+template <class T, class PT, int V, int NTH, int CH, bool RMS>
 __global__ __launch_bounds__(block_of<NTH>()) void layer_norm_bwd_kernel(NormArgs a) {
   __shared__ float lds[2][2][16];
   constexpr int ROWS = block_of<NTH>() / NTH;
   const int lane = threadIdx.x % NTH;
+  const int64_t step = (int64_t)gridDim.x * ROWS;
+  wide_t<PT, V> gain[CH];
+  load_param<PT, V, NTH, CH>(gain, a.gain, 1.f, lane, a.width, a.params16);
   float dg[CH][V], db[CH][V];
 #pragma unroll
   for (int i = 0; i < CH; i++)
 #pragma unroll
     for (int j = 0; j < V; j++) dg[i][j] = db[i][j] = 0.f;
-  for (int64_t t = (int64_t)blockIdx.x * ROWS + threadIdx.x / NTH; t < a.T; t += (int64_t)gridDim.x * ROWS) {
-    const T *x = (const T*)a.x + (size_t)t * a.ld_x, *dy = (const T*)a.dy + (size_t)t * a.ld_y;
-    T* dx = (T*)a.out + (size_t)t * a.ld_out;
-    wide_t<T, V> xv[CH], yv[CH];
-    float sx = 0.f, sw = 0.f;
+  constexpr bool AHEAD = NTH * CH * V <= 8192;      // (registers: the widest rows leave a lane of their 1024 no more)
+  wide_t<T, V> x[CH], y[CH], next_x[CH], next_y[CH];
+  int64_t t = (int64_t)blockIdx.x * ROWS + threadIdx.x / NTH;
+  auto ask = [&](int64_t at) {
+    if (at >= a.T) return;
+    load_row<T, V, NTH, CH>(next_x, (const T*)a.x + (size_t)at * a.ld_x, lane, a.width);
+    load_row<T, V, NTH, CH>(next_y, (const T*)a.dy + (size_t)at * a.ld_y, lane, a.width);
+  };
+  if (AHEAD) ask(t);
+  for (; t < a.T; t += step) {
+    if (!AHEAD) ask(t);
 #pragma unroll
-    for (int i = 0; i < CH; i++) {
-      const int c = (i * NTH + lane) * V;
-      if (c < a.width) {
-        xv[i] = load_wide<V>(x + c);
-        yv[i] = load_wide<V>(dy + c);
-      }
-    }
-    auto w_of = [&](int i, int j, int c) { const float g = (float)yv[i][j]; return a.gain ? g * param(a.gain, c + j, a.param32) : g; };
+    for (int i = 0; i < CH; i++) { x[i] = next_x[i]; y[i] = next_y[i]; }
+    if (AHEAD) ask(t + step);
     float mean = 0.f, mean_w = 0.f;
     if constexpr (!RMS) {
+      float sx = 0.f, sw = 0.f;
 #pragma unroll
-      for (int i = 0; i < CH; i++) {
-        const int c = (i * NTH + lane) * V;
-        if (c < a.width) {
+      for (int i = 0; i < CH; i++)
+        if ((i * NTH + lane) * V < a.width) {
 #pragma unroll
-          for (int j = 0; j < V; j++) { sx += (float)xv[i][j]; sw += w_of(i, j, c); }
+          for (int j = 0; j < V; j++) { sx += (float)x[i][j]; sw = __builtin_fmaf((float)y[i][j], (float)gain[i][j], sw); }
         }
-      }
       row_sums<NTH>(sx, sw, lds, 0);
       mean = sx * a.inv;
       mean_w = sw * a.inv;
     }
     float ss = 0.f, sd = 0.f;
 #pragma unroll
-    for (int i = 0; i < CH; i++) {
-      const int c = (i * NTH + lane) * V;
-      if (c < a.width) {
+    for (int i = 0; i < CH; i++)
+      if ((i * NTH + lane) * V < a.width) {
 #pragma unroll
         for (int j = 0; j < V; j++) {
-          const float d = (float)xv[i][j] - mean;
+          const float d = (float)x[i][j] - mean;
           ss = __builtin_fmaf(d, d, ss);
-          sd = __builtin_fmaf(d, w_of(i, j, c), sd);
+          sd = __builtin_fmaf(d, (float)y[i][j] * (float)gain[i][j], sd);
         }
       }
-    }
     row_sums<NTH>(ss, sd, lds, 1);
     if constexpr (NTH > 64 && RMS) __syncthreads();
     const float r = rsqrtf(ss * a.inv + a.eps), k = sd * a.inv * r * r;     // n mean(w n) = (x - mean) k
+    T* dx = (T*)a.out + (size_t)t * a.ld_out;
 #pragma unroll
     for (int i = 0; i < CH; i++) {
       const int c = (i * NTH + lane) * V;
@@ -163,10 +189,10 @@ __global__ __launch_bounds__(block_of<NTH>()) void layer_norm_bwd_kernel(NormArg
         wide_t<T, V> o;
 #pragma unroll
         for (int j = 0; j < V; j++) {
-          const float d = (float)xv[i][j] - mean, g = (float)yv[i][j];
+          const float d = (float)x[i][j] - mean, g = (float)y[i][j];
           dg[i][j] = __builtin_fmaf(g, d * r, dg[i][j]);
           db[i][j] += g;
-          o[j] = (T)(r * (w_of(i, j, c) - mean_w - d * k));
+          o[j] = (T)(r * (g * (float)gain[i][j] - mean_w - d * k));
         }
         store_wide<V>(dx + c, o);
       }
@@ -251,7 +277,7 @@ NormArgs args(const ah_layer_norm_t* c, const void* x, const void* dy, void* out
   NormArgs a = {};
   a.x = x; a.dy = dy; a.out = out; a.gain = c->gain; a.bias = c->bias; a.part = part;
   a.ld_x = c->ld_x ? c->ld_x : c->width; a.ld_y = c->ld_y ? c->ld_y : c->width; a.ld_out = ld_out ? ld_out : c->width;
-  a.T = c->rows; a.width = c->width; a.param32 = c->param_type == AH_FP32; a.eps = c->eps; a.inv = 1.f / c->width;
+  a.T = c->rows; a.width = c->width; a.params16 = aligned_to(c->gain, 16) && aligned_to(c->bias, 16); a.eps = c->eps; a.inv = 1.f / c->width;
   return a;
 }
 
@@ -279,27 +305,32 @@ void by_width(int width, const F& go) {
 }
 
 template <bool BWD>
-hipError_t run(const NormArgs& a, bool act32, bool rms, bool wide, int blocks, hipStream_t s) {
-  auto typed = [&](auto t, auto v, auto r) {
+hipError_t run(const NormArgs& a, const ah_layer_norm_t* c, bool wide, int blocks, hipStream_t s) {
+  auto typed = [&](auto t, auto p, auto v, auto r) {
     typedef decltype(t) T;
+    typedef decltype(p) PT;
     constexpr int V = decltype(v)::value;
     constexpr bool RMS = decltype(r)::value;
     by_width<V>(a.width, [&](auto lanes, auto pieces) {
       constexpr int NTH = decltype(lanes)::value, CH = decltype(pieces)::value;
-      if constexpr (BWD) hipLaunchKernelGGL((layer_norm_bwd_kernel<T, V, NTH, CH, RMS>), dim3(blocks), dim3(block_of<NTH>()), 0, s, a);
-      else hipLaunchKernelGGL((layer_norm_fwd_kernel<T, V, NTH, CH, RMS>), dim3(blocks), dim3(block_of<NTH>()), 0, s, a);
+      if constexpr (BWD) hipLaunchKernelGGL((layer_norm_bwd_kernel<T, PT, V, NTH, CH, RMS>), dim3(blocks), dim3(block_of<NTH>()), 0, s, a);
+      else hipLaunchKernelGGL((layer_norm_fwd_kernel<T, PT, V, NTH, CH, RMS>), dim3(blocks), dim3(block_of<NTH>()), 0, s, a);
     });
   };
-  auto by_kind = [&](auto t, auto v) {
-    if (rms) typed(t, v, std::true_type());
-    else typed(t, v, std::false_type());
+  auto by_kind = [&](auto t, auto p, auto v) {
+    if (c->rms) typed(t, p, v, std::true_type());
+    else typed(t, p, v, std::false_type());
   };
-  auto by_align = [&](auto t) {
-    if (wide) by_kind(t, std::integral_constant<int, 8>());
-    else by_kind(t, std::integral_constant<int, 1>());
+  auto by_align = [&](auto t, auto p) {
+    if (wide) by_kind(t, p, std::integral_constant<int, 8>());
+    else by_kind(t, p, std::integral_constant<int, 1>());
   };
-  if (act32) by_align(float());
-  else by_align(bf16());
+  auto by_param = [&](auto t) {
+    if (c->param_type == AH_FP32) by_align(t, float());
+    else by_align(t, bf16());
+  };
+  if (c->act_type == AH_FP32) by_param(float());
+  else by_param(bf16());
   return hipGetLastError();
 }
 
@@ -317,8 +348,8 @@ extern "C" int ah_layer_norm_fwd(const ah_layer_norm_t* c, const void* x, void* 
   const NormArgs a = args(c, x, nullptr, y, c->ld_y, nullptr);
   if (shifted(x, a.ld_x, a)) return set_error(AH_EINVAL, "ah_layer_norm_fwd: y in the place of x needs x's row stride");
   const bool wide = c->width % 8 == 0 && rows16(x, a.ld_x, ab) && rows16(y, a.ld_out, ab);
-  const int rows = std::max(1, 256 / row_lanes(c->width));
-  return hip_status(run<false>(a, ab == 4, c->rms, wide, std::min((c->rows + rows - 1) / rows, 1 << 21), (hipStream_t)stream), "ah_layer_norm_fwd");
+  const int block = std::max(256, row_lanes(c->width)), rows = block / row_lanes(c->width);
+  return hip_status(run<false>(a, c, wide, std::min((c->rows + rows - 1) / rows, kFwdBlocks * 256 / block), (hipStream_t)stream), "ah_layer_norm_fwd");
 }
 
 extern "C" int ah_layer_norm_bwd_workspace(const ah_layer_norm_t* c, uint64_t* bytes) {
@@ -340,7 +371,7 @@ extern "C" int ah_layer_norm_bwd(const ah_layer_norm_t* c, const void* x, const 
   if (shifted(x, a.ld_x, a) || shifted(dy, a.ld_y, a)) return set_error(AH_EINVAL, "ah_layer_norm_bwd: dx in the place of x or dy needs its row stride");
   const bool wide = c->width % 8 == 0 && rows16(x, a.ld_x, ab) && rows16(dy, a.ld_y, ab) && rows16(dx, a.ld_out, ab);
   const int blocks = bwd_blocks(c);
-  hipError_t e = run<true>(a, ab == 4, c->rms, wide, blocks, (hipStream_t)stream);      // (no rows: writes zeros)
+  hipError_t e = run<true>(a, c, wide, blocks, (hipStream_t)stream);      // (no rows: writes zeros)
   if (e == hipSuccess && (d_gain || d_bias)) {
     hipLaunchKernelGGL(norm_fold_kernel, dim3((c->width + 63) / 64, 2), dim3(1024), 0, (hipStream_t)stream, a.part, blocks, c->width, d_gain, d_bias, beta);
     e = hipGetLastError();
