@@ -18,8 +18,10 @@ namespace {
 
 constexpr int NT = 256, NW = NT / 64, kMaxRows = 1 << 25, kMaxVocab = 1 << 30, kMaxWidth = 65536;
 constexpr int kFlight = 2;                             // pieces of a row that a lane has in flight
-constexpr int kMaxChunks = 2048, kMinChunk = 16;
-constexpr int kFillBlocks = 1024;                      // beside the sort of few tokens
+constexpr int kMaxChunks = 2048, kMinChunk = 16, kAhead = 8, kJoin = 8;
+constexpr int kRowThreads = 1024;
+constexpr int kSmall = 16384;                          // tokens up to which places are counted (rank_kernel)
+constexpr int kFillBlocks = 1024;                      // beside that
 constexpr int kItems = 16, kSortBlock = NT * kItems;   // numbers that a block of the sort takes
 
 struct FwdArgs {
@@ -73,26 +75,36 @@ __global__ __launch_bounds__(NT) void embedding_fwd_kernel(FwdArgs a, int lanes_
 }
 
 // ---- the tokens' numbers sorted by token, those of no row behind the others (their key: vocab)
-__device__ __forceinline__ uint32_t key_of(const void* tokens, size_t t, int bits, int vocab) {
-  const int64_t k = load_index(tokens, t, bits);
-  return (uint64_t)k < (uint64_t)vocab ? (uint32_t)k : (uint32_t)vocab;
+// (BITS as a constant: a branch for each load would wait for each)
+template <int BITS>
+__device__ __forceinline__ uint32_t key_of(const void* tokens, size_t t, int vocab) {
+  if constexpr (BITS == 64) {
+    const uint64_t k = ((const uint64_t*)tokens)[t];
+    return k < (uint64_t)vocab ? (uint32_t)k : (uint32_t)vocab;
+  } else {
+    return min(((const uint32_t*)tokens)[t], (uint32_t)vocab);
+  }
 }
 
 struct SortArgs {
-  const void* tokens;           // the first digit's keys come from here, with the numbers 0 .. T - 1
-  const uint32_t *key_in, *at_in;
+  const void* tokens;           // the first digit's keys come from here, with the numbers 0 .. T - 1 ...
+  const uint32_t *key_in, *at_in;   // ... the others' from here
   uint32_t *key_out, *at_out;
   uint32_t* count;              // [256][blocks]
-  int T, vocab, bits, shift, blocks;
+  int T, vocab, shift, blocks;
 };
 
+// BITS of a token where the digit is the first one, else 0
+template <int BITS>
 __global__ __launch_bounds__(NT) void digit_count_kernel(SortArgs a) {
   __shared__ uint32_t n[256];
   n[threadIdx.x] = 0;
   __syncthreads();
   const int first = blockIdx.x * kSortBlock;
   for (int i = threadIdx.x; i < kSortBlock && first + i < a.T; i += NT) {
-    const uint32_t k = a.tokens ? key_of(a.tokens, first + i, a.bits, a.vocab) : a.key_in[first + i];
+    uint32_t k;
+    if constexpr (BITS) k = key_of<BITS>(a.tokens, first + i, a.vocab);
+    else k = a.key_in[first + i];
     atomicAdd(&n[(k >> a.shift) & 255], 1u);
   }
   __syncthreads();
@@ -127,6 +139,7 @@ __global__ __launch_bounds__(1024) void digit_scan_kernel(uint32_t* count, int n
 }
 
 // A wave takes 64 numbers after the other; among those, a lane's place is behind the lanes before it with the same digit.
+template <int BITS>
 __global__ __launch_bounds__(NT) void digit_place_kernel(SortArgs a) {
   __shared__ uint32_t place[NW][256];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -138,11 +151,13 @@ __global__ __launch_bounds__(NT) void digit_place_kernel(SortArgs a) {
   for (int i = 0; i < kItems; i++) {
     const int t = first + i * 64 + lane;
     if (t < a.T) {
-      key[i] = a.tokens ? key_of(a.tokens, t, a.bits, a.vocab) : a.key_in[t];
-      at[i] = a.tokens ? t : a.at_in[t];
-      atomicAdd(&place[wave][(key[i] >> a.shift) & 255], 1u);
+      if constexpr (BITS) { key[i] = key_of<BITS>(a.tokens, t, a.vocab); at[i] = t; }
+      else { key[i] = a.key_in[t]; at[i] = a.at_in[t]; }
     }
   }
+#pragma unroll
+  for (int i = 0; i < kItems; i++)
+    if (first + i * 64 + lane < a.T) atomicAdd(&place[wave][(key[i] >> a.shift) & 255], 1u);
   __syncthreads();
   uint32_t base = a.count[threadIdx.x * a.blocks + blockIdx.x];
 #pragma unroll
@@ -173,8 +188,6 @@ __global__ __launch_bounds__(NT) void digit_place_kernel(SortArgs a) {
   }
 }
 
-// All of it in one block, for as many tokens as its LDS holds: the list goes through LDS once a digit.
-constexpr int kSmall = 8192, kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64, kSmallItems = kSmall / kSmallThreads;
 struct FillArgs {
   float* d;
   size_t ld;
@@ -189,90 +202,47 @@ __device__ __forceinline__ void fill_rows(const FillArgs& f, int64_t block, int6
   }
 }
 
-// BITS of a digit; the blocks behind the first set the rows of the table to zeros meanwhile (f.d NULL: there are none)
+// Few tokens: a number's place in the sorted list is how many lie before it, which a block counts for kRanked of them against all others (one comparison for 64 of
+// those).  The blocks behind the first `rank_blocks` set the rows of the table to zeros meanwhile.
+constexpr uint32_t kNone = 0x7ffffffe;       // (twice that and 2 more fit)
+constexpr int kRanked = 16, kRankThreads = 1024, kRankWaves = kRankThreads / 64;
 template <int BITS>
-__global__ __launch_bounds__(kSmallThreads) void small_sort_kernel(SortArgs a, int passes, FillArgs f) {
-  constexpr int D = 1 << BITS, PER = (D + 63) / 64;
-  __shared__ uint32_t keys[kSmall], ats[kSmall], place[kSmallWaves][D], total[D];
-  if (blockIdx.x > 0) return fill_rows(f, blockIdx.x - 1, gridDim.x - 1, kSmallThreads);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int first = wave * 64 * kSmallItems;         // a wave's part of the list
-  uint32_t key[kSmallItems], at[kSmallItems];
+__global__ __launch_bounds__(kRankThreads) void rank_kernel(SortArgs a, int rank_blocks, FillArgs f) {
+  __shared__ uint32_t keys[kSmall], count[kRankWaves][kRanked];
+  if ((int)blockIdx.x >= rank_blocks) return fill_rows(f, blockIdx.x - rank_blocks, gridDim.x - rank_blocks, kRankThreads);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = blockIdx.x * kRanked;
+#pragma unroll 8
+  for (int t = threadIdx.x; t < (a.T + 63) / 64 * 64; t += kRankThreads) keys[t] = t < a.T ? key_of<BITS>(a.tokens, t, a.vocab) : kNone;
+  __syncthreads();
+  uint32_t key[kRanked], n[kRanked];
 #pragma unroll
-  for (int i = 0; i < kSmallItems; i++) {
-    const int t = first + i * 64 + lane;
-    at[i] = t;
-    key[i] = t < a.T ? key_of(a.tokens, t, a.bits, a.vocab) : ~0u;       // (behind all others: every digit the largest)
+  for (int i = 0; i < kRanked; i++) {
+    key[i] = 2 * __builtin_amdgcn_readfirstlane(keys[first + i]) + 1;
+    n[i] = 0;
   }
-  for (int p = 0; p < passes; p++) {
-    const int shift = p * BITS;
-    for (int i = threadIdx.x; i < kSmallWaves * D; i += kSmallThreads) place[0][i] = 0;
-    __syncthreads();
-    uint32_t behind[kSmallItems];
-    // a lane's place among the wave's numbers of its digit: those that the wave took before, and those of lanes before it
+#pragma unroll 1
+  for (int g = wave * 64; g < a.T; g += kRankThreads) {
+    const uint32_t k = keys[g + lane];
+    if (first >= g && first < g + 64) {      // these 64 hold the block's own (which begin at a multiple of kRanked)
 #pragma unroll
-    for (int i = 0; i < kSmallItems; i++) {
-      const uint32_t d = (key[i] >> shift) & (D - 1);
-      uint64_t same = ~0ull;
+      for (int i = 0; i < kRanked; i++) n[i] += __popcll(__ballot(2 * k + (lane < first - g + i ? 0u : 2u) < key[i]));
+    } else {
+      const uint32_t k2 = 2 * k + (g < first ? 0u : 2u);       // of those before the block's own the equal ones count, too
 #pragma unroll
-      for (int b = 0; b < BITS; b++) {
-        const uint64_t m = __ballot((d >> b) & 1);
-        same &= (d >> b) & 1 ? m : ~m;
-      }
-      volatile uint32_t* mine = &place[wave][d];
-      const uint32_t before = *mine, among = __popcll(same & ((1ull << lane) - 1));
-      behind[i] = before + among;
-      if (among == 0) *mine = before + __popcll(same);
-    }
-    __syncthreads();
-    // where a digit begins: sums over the waves, then over the digits before it
-    if (threadIdx.x < D) {
-      uint32_t n = 0;
-#pragma unroll
-      for (int w = 0; w < kSmallWaves; w++) {
-        const uint32_t m = place[w][threadIdx.x];
-        place[w][threadIdx.x] = n;
-        n += m;
-      }
-      total[threadIdx.x] = n;
-    }
-    __syncthreads();
-    if (wave == 0) {
-      uint32_t own[PER], n = 0;
-#pragma unroll
-      for (int i = 0; i < PER; i++) {
-        own[i] = n;
-        n += total[lane * PER + i];
-      }
-      uint32_t s = n;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t u = __shfl_up(s, o, 64);
-        if (lane >= o) s += u;
-      }
-#pragma unroll
-      for (int i = 0; i < PER; i++) total[lane * PER + i] = s - n + own[i];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kSmallItems; i++) {
-      const uint32_t d = (key[i] >> shift) & (D - 1), to = total[d] + place[wave][d] + behind[i];
-      keys[to] = key[i];
-      ats[to] = at[i];
-    }
-    __syncthreads();
-    if (p + 1 < passes) {
-#pragma unroll
-      for (int i = 0; i < kSmallItems; i++) {
-        key[i] = keys[first + i * 64 + lane];
-        at[i] = ats[first + i * 64 + lane];
-      }
-      __syncthreads();
+      for (int i = 0; i < kRanked; i++) n[i] += __popcll(__ballot(k2 < key[i]));
     }
   }
-  for (int i = threadIdx.x; i < a.T; i += kSmallThreads) {
-    a.key_out[i] = keys[i];
-    a.at_out[i] = ats[i];
+  if (lane == 0) {
+#pragma unroll
+    for (int i = 0; i < kRanked; i++) count[wave][i] = n[i];
+  }
+  __syncthreads();
+  if (threadIdx.x < kRanked && first + (int)threadIdx.x < a.T) {
+    uint32_t to = 0;
+#pragma unroll
+    for (int w = 0; w < kRankWaves; w++) to += count[w][threadIdx.x];
+    a.key_out[to] = keys[first + threadIdx.x];
+    a.at_out[to] = first + threadIdx.x;
   }
 }
 
@@ -288,78 +258,89 @@ struct BwdArgs {
 __global__ __launch_bounds__(NT) void fill_rows_kernel(FillArgs f) { fill_rows(f, blockIdx.x, gridDim.x, NT); }
 
 template <int V>
-__device__ __forceinline__ void put(const BwdArgs& a, uint32_t row, int c, const float (&s)[V]) {
-  float* p = a.d + (size_t)row * a.ld_d + c;
-  wide_t<float, V> v;
-#pragma unroll
-  for (int j = 0; j < V; j++) v[j] = s[j] * a.scale;
-  if (a.beta) v += load_wide<V>((const float*)p);
-  store_wide<V>(p, v);
+__device__ __forceinline__ void put(const BwdArgs& a, uint32_t row, int c, const wide_t<float, V>& s, const wide_t<float, V>& old) {
+  store_wide<V>(a.d + (size_t)row * a.ld_d + c, s * a.scale + old);
+}
+template <int V>
+__device__ __forceinline__ wide_t<float, V> old_row(const BwdArgs& a, uint32_t row, int c) {
+  wide_t<float, V> r = {};
+  if (a.beta) r = load_wide<V>((const float*)a.d + (size_t)row * a.ld_d + c);
+  return r;
 }
 
-// A block adds up V columns a lane of one chunk.  The list is the same for all lanes: keys and numbers are scalars.
+// A block adds up V columns a lane of one chunk.  A wave's lanes hold the keys and numbers of 64 entries, which are the same for all lanes of a row; rows of dy, and those
+// of the table that get a sum (beta), are asked for kAhead at a time.
 template <class AT, int V>
-__global__ __launch_bounds__(NT) void embedding_bwd_kernel(BwdArgs a) {
-  constexpr int AHEAD = 8;       // rows in flight
-  const int c = (blockIdx.y * NT + threadIdx.x) * V;
+__global__ __launch_bounds__(kRowThreads) void embedding_bwd_kernel(BwdArgs a) {
+  const int c = (blockIdx.y * blockDim.x + threadIdx.x) * V, lane = threadIdx.x & 63;
   const int first = blockIdx.x * a.chunk, end = min(first + a.chunk, a.T);
-  if (c >= a.width) return;
-  const AT* dy = (const AT*)a.dy + c;
-  float s[V];
-#pragma unroll
-  for (int j = 0; j < V; j++) s[j] = 0.f;
+  const bool on = c < a.width;
+  const AT* dy = (const AT*)a.dy + (on ? c : 0);
+  float* part = a.part + (size_t)blockIdx.x * 2 * a.width + c;
+  wide_t<float, V> s = {};
   bool began = first == 0 || a.key[first - 1] != a.key[first];      // whether the present sum began in this chunk
-  for (int i = first; i < end; i += AHEAD) {
-    wide_t<AT, V> r[AHEAD];
-    uint32_t key[AHEAD + 1];
+  for (int i0 = first; i0 < end; i0 += 64) {
+    const int e = min(i0 + lane, a.T - 1);
+    const uint32_t keys = a.key[e], ats = a.at[e];
+    const uint64_t last = __ballot(e + 1 >= a.T || a.key[min(e + 1, a.T - 1)] != keys);     // entries that end a sum
+    const int n = min(min(end - i0, 64), (int)__popcll(__ballot(i0 + lane < a.T && keys < (uint32_t)a.vocab)));   // (tokens of no row lie behind all others)
+    for (int i = 0; i < n; i += kAhead) {
+      wide_t<AT, V> r[kAhead];
+      wide_t<float, V> old[kAhead];
+      uint32_t key[kAhead];
 #pragma unroll
-    for (int k = 0; k < AHEAD; k++) {
-      const int e = min(i + k, a.T - 1);
-      key[k] = a.key[e];
-      if (key[k] < (uint32_t)a.vocab) r[k] = load_wide<V>(dy + (size_t)a.at[e] * a.ld_dy);
-    }
-    key[AHEAD] = a.key[min(i + AHEAD, a.T - 1)];
-#pragma unroll
-    for (int k = 0; k < AHEAD; k++) {
-      if (i + k >= end || key[k] >= (uint32_t)a.vocab) return;       // (tokens of no row: behind all others)
-#pragma unroll
-      for (int j = 0; j < V; j++) s[j] += (float)r[k][j];
-      const bool last = i + k + 1 == a.T || key[k + 1] != key[k], cut = i + k + 1 == end;
-      if (last || cut) {
-        if (last && began) {
-          put<V>(a, key[k], c, s);
-        } else {
-          float* p = a.part + ((size_t)blockIdx.x * 2 + (began ? 1 : 0)) * a.width + c;
-          wide_t<float, V> v;
-#pragma unroll
-          for (int j = 0; j < V; j++) v[j] = s[j];
-          store_wide<V>(p, v);
+      for (int k = 0; k < kAhead; k++) {
+        key[k] = __builtin_amdgcn_readlane(keys, min(i + k, 63));
+        const uint32_t at = __builtin_amdgcn_readlane(ats, min(i + k, 63));
+        if (i + k < n && on) {
+          r[k] = load_wide<V>(dy + (size_t)at * a.ld_dy);
+          if ((last >> (i + k)) & 1) old[k] = old_row<V>(a, key[k], c);
         }
+      }
 #pragma unroll
-        for (int j = 0; j < V; j++) s[j] = 0.f;
-        began = true;
+      for (int k = 0; k < kAhead; k++) {
+        if (i + k >= n || !on) break;
+#pragma unroll
+        for (int j = 0; j < V; j++) s[j] += (float)r[k][j];
+        const bool done = (last >> (i + k)) & 1;
+        if (done || i0 + i + k + 1 == end) {
+          if (done && began) put<V>(a, key[k], c, s, old[k]);
+          else store_wide<V>(part + (began ? a.width : 0), s);
+          s = wide_t<float, V>{};
+          began = true;
+        }
       }
     }
+    if (n < min(end - i0, 64)) return;
   }
 }
 
 // The chunk in which a sum begins that goes on behind it adds up what the following ones left of it.
 template <int V>
-__global__ __launch_bounds__(NT) void embedding_join_kernel(BwdArgs a, int chunks) {
+__global__ __launch_bounds__(kRowThreads) void embedding_join_kernel(BwdArgs a, int chunks) {
   const int first = blockIdx.x * a.chunk, end = first + a.chunk;
   if (end >= a.T) return;
   const uint32_t k = a.key[end - 1];
   if (k >= (uint32_t)a.vocab || a.key[end] != k) return;
   if (a.key[first] == k && first > 0 && a.key[first - 1] == k) return;      // it began earlier
-  const int c = (blockIdx.y * NT + threadIdx.x) * V;
+  const int c = (blockIdx.y * blockDim.x + threadIdx.x) * V;
   if (c >= a.width) return;
   const float* p = a.part + (size_t)blockIdx.x * 2 * a.width + c;
+  const wide_t<float, V> old = old_row<V>(a, k, c);
   wide_t<float, V> s = load_wide<V>(p + a.width);
-  for (int b = blockIdx.x + 1; b < chunks && a.key[(size_t)b * a.chunk] == k; b++) s += load_wide<V>(p + (size_t)(b - blockIdx.x) * 2 * a.width);
-  float v[V];
+  int b = blockIdx.x + 1;
+  for (bool more = true; more; b += kJoin) {
+    wide_t<float, V> r[kJoin];
 #pragma unroll
-  for (int j = 0; j < V; j++) v[j] = s[j];
-  put<V>(a, k, c, v);
+    for (int i = 0; i < kJoin; i++) {
+      more = more && b + i < chunks && a.key[(size_t)(b + i) * a.chunk] == k;
+      r[i] = wide_t<float, V>{};
+      if (more) r[i] = load_wide<V>(p + (size_t)(b + i - blockIdx.x) * 2 * a.width);
+    }
+#pragma unroll
+    for (int i = 0; i < kJoin; i++) s += r[i];
+  }
+  put<V>(a, k, c, s, old);
 }
 
 int sort_blocks(int T) { return (T + kSortBlock - 1) / kSortBlock; }
@@ -476,38 +457,42 @@ extern "C" int ah_embedding_bwd(const ah_embedding_t* c, const void* tokens, con
   char* w = (char*)workspace;
   a.part = (float*)(w + p.part);
   SortArgs q = {};
-  q.T = T; q.vocab = c->vocab; q.bits = c->token_bits; q.blocks = sort_blocks(T); q.count = (uint32_t*)(w + p.count);
+  q.T = T; q.vocab = c->vocab; q.blocks = sort_blocks(T); q.count = (uint32_t*)(w + p.count);
   q.tokens = tokens;
   int key_bits = 1;                                       // of the largest key, vocab
   while (key_bits < 31 && (c->vocab >> key_bits) != 0) key_bits++;
   if (small) {
     q.key_out = (uint32_t*)(w + p.key[0]); q.at_out = (uint32_t*)(w + p.at[0]);
-    const int blocks = beta ? 1 : 1 + std::min<int64_t>(((int64_t)c->vocab * c->width + 65535) / 65536, kFillBlocks);
-    auto go = [&](auto kernel, int bits) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kSmallThreads), 0, s, q, (key_bits + bits - 1) / bits, f); };
-    if ((key_bits + 7) / 8 > (key_bits + 8) / 9) go(small_sort_kernel<9>, 9);        // (17 and 18 bits: two passes for three)
-    else go(small_sort_kernel<8>, 8);
+    const int ranks = (T + kRanked - 1) / kRanked, fills = beta ? 0 : (int)std::min<int64_t>(((int64_t)c->vocab * c->width + 65535) / 65536, kFillBlocks);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(ranks + fills), dim3(kRankThreads), 0, s, q, ranks, f); };
+    if (c->token_bits == 64) go(rank_kernel<64>);
+    else go(rank_kernel<32>);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return hip_status(e, "ah_embedding_bwd");
     q.key_in = q.key_out; q.at_in = q.at_out;
   } else {
     int to = 0;
     for (q.shift = 0; q.shift < key_bits; q.shift += 8, to ^= 1) {
       q.key_out = (uint32_t*)(w + p.key[to]); q.at_out = (uint32_t*)(w + p.at[to]);
-      hipLaunchKernelGGL(digit_count_kernel, dim3(q.blocks), dim3(NT), 0, s, q);
+      auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(q.blocks), dim3(NT), 0, s, q); };
+      const int bits = q.shift ? 0 : c->token_bits;
+      if (bits == 64) go(digit_count_kernel<64>); else if (bits == 32) go(digit_count_kernel<32>); else go(digit_count_kernel<0>);
       hipLaunchKernelGGL(digit_scan_kernel, dim3(1), dim3(1024), 0, s, q.count, 256 * q.blocks);
-      hipLaunchKernelGGL(digit_place_kernel, dim3(q.blocks), dim3(NT), 0, s, q);
+      if (bits == 64) go(digit_place_kernel<64>); else if (bits == 32) go(digit_place_kernel<32>); else go(digit_place_kernel<0>);
       if (hipError_t e = hipGetLastError(); e != hipSuccess) return hip_status(e, "ah_embedding_bwd");
-      q.tokens = nullptr;
       q.key_in = q.key_out; q.at_in = q.at_out;
     }
   }
   a.key = q.key_in; a.at = q.at_in;
-  const bool wide = c->width % 8 == 0 && rows16(dy, a.ld_dy, ab) && rows16(d_table, a.ld_d, 4);
-  const int v = wide ? 8 : 1, chunks = (T + a.chunk - 1) / a.chunk;
-  const dim3 grid(chunks, (c->width + NT * v - 1) / (NT * v));
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(NT), 0, s, a); };
-  if (ab == 4) { if (wide) go(embedding_bwd_kernel<float, 8>); else go(embedding_bwd_kernel<float, 1>); }
-  else { if (wide) go(embedding_bwd_kernel<bf16, 8>); else go(embedding_bwd_kernel<bf16, 1>); }
-  if (wide) hipLaunchKernelGGL(embedding_join_kernel<8>, grid, dim3(NT), 0, s, a, chunks);
-  else hipLaunchKernelGGL(embedding_join_kernel<1>, grid, dim3(NT), 0, s, a, chunks);
+  // four columns a lane: 16 bytes of the table's gradient, 8 or 16 of dy
+  const bool wide = c->width % 4 == 0 && aligned_to(dy, 4 * ab) && a.ld_dy % 4 == 0 && rows16(d_table, a.ld_d, 4);
+  const int v = wide ? 4 : 1, chunks = (T + a.chunk - 1) / a.chunk;
+  // lanes for a whole row, or 1024 of them
+  const int slices = (c->width + kRowThreads * v - 1) / (kRowThreads * v), lanes = ((c->width + slices * v - 1) / (slices * v) + 63) / 64 * 64;
+  const dim3 grid(chunks, (c->width + lanes * v - 1) / (lanes * v));
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(lanes), 0, s, a); };
+  if (ab == 4) { if (wide) go(embedding_bwd_kernel<float, 4>); else go(embedding_bwd_kernel<float, 1>); }
+  else { if (wide) go(embedding_bwd_kernel<bf16, 4>); else go(embedding_bwd_kernel<bf16, 1>); }
+  if (wide) hipLaunchKernelGGL(embedding_join_kernel<4>, grid, dim3(lanes), 0, s, a, chunks);
+  else hipLaunchKernelGGL(embedding_join_kernel<1>, grid, dim3(lanes), 0, s, a, chunks);
   return hip_status(hipGetLastError(), "ah_embedding_bwd");
 }

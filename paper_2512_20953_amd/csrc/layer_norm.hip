@@ -16,7 +16,7 @@ using namespace ah;
 
 namespace {
 
-constexpr int kMaxRows = 1 << 25, kMaxWidth = 16384, kMaxBlocks = 512, kFwdBlocks = 2048;   // blocks of 256 lanes forward
+constexpr int kMaxRows = 1 << 25, kMaxWidth = 16384, kMaxBlocks = 256, kFwdBlocks = 2048;   // backward: of 1024 lanes, each with a row of partial sums; forward: of 256
 
 struct NormArgs {
   const void *x, *dy, *gain, *bias;
@@ -27,24 +27,25 @@ struct NormArgs {
   float eps, inv;              // inv: 1 / width
 };
 
-// Sums of two values over the lanes of a row: NTH = 64: of a wave, else of the block.  `slot` alternates, so that a wave that is ahead does not
+// Sums of two values over the lanes of a row: NTH = 64: of a wave, else of the row's waves of a block.  `slot` alternates, so that a wave that is ahead does not
 // write where another one still reads.
 template <int NTH>
 __device__ __forceinline__ void row_sums(float& a, float& b, float (&lds)[2][2][16], int slot) {
   a = wave_sum(a);
   b = wave_sum(b);
   if constexpr (NTH > 64) {
-    const int wave = threadIdx.x >> 6;
+    const int wave = threadIdx.x >> 6, first = wave / (NTH / 64) * (NTH / 64);
     if ((threadIdx.x & 63) == 0) { lds[slot][0][wave] = a; lds[slot][1][wave] = b; }
     __syncthreads();
     a = b = 0.f;
 #pragma unroll
-    for (int w = 0; w < NTH / 64; w++) { a += lds[slot][0][w]; b += lds[slot][1][w]; }
+    for (int w = 0; w < NTH / 64; w++) { a += lds[slot][0][first + w]; b += lds[slot][1][first + w]; }
   }
 }
 
-// NTH lanes to a row, of which each holds CH pieces of V elements; blocks of at least 256 lanes
+// NTH lanes to a row, of which each holds CH pieces of V elements; forward in blocks of at least 256 lanes, backward of 1024
 template <int NTH> constexpr int block_of() { return NTH < 256 ? 256 : NTH; }
+constexpr int kBwdThreads = 1024;
 
 // Gain or bias of the lane's columns, kept as they lie in memory; NULL: `none` in all of them.  W: in whole pieces (V elements, 16-byte aligned)
 template <class PT, int V, int NTH, int CH>
@@ -128,9 +129,9 @@ __global__ __launch_bounds__(block_of<NTH>()) void layer_norm_fwd_kernel(NormArg
 }
 
 template <class T, class PT, int V, int NTH, int CH, bool RMS>
-__global__ __launch_bounds__(block_of<NTH>()) void layer_norm_bwd_kernel(NormArgs a) {
+__global__ __launch_bounds__(kBwdThreads) void layer_norm_bwd_kernel(NormArgs a) {
   __shared__ float lds[2][2][16];
-  constexpr int ROWS = block_of<NTH>() / NTH;
+  constexpr int ROWS = kBwdThreads / NTH, COLS = NTH * CH * V;
   const int lane = threadIdx.x % NTH;
   const int64_t step = (int64_t)gridDim.x * ROWS;
   wide_t<PT, V> gain[CH];
@@ -140,16 +141,20 @@ __global__ __launch_bounds__(block_of<NTH>()) void layer_norm_bwd_kernel(NormArg
   for (int i = 0; i < CH; i++)
 #pragma unroll
     for (int j = 0; j < V; j++) dg[i][j] = db[i][j] = 0.f;
-  constexpr bool AHEAD = NTH * CH * V <= 8192;      // (registers: the widest rows leave a lane of their 1024 no more)
+  constexpr bool AHEAD = CH * V <= 8;       // (16 elements a lane leave no room for the next row in its 128 registers)
   wide_t<T, V> x[CH], y[CH], next_x[CH], next_y[CH];
-  int64_t t = (int64_t)blockIdx.x * ROWS + threadIdx.x / NTH;
+  const int row = threadIdx.x / NTH;
   auto ask = [&](int64_t at) {
+#pragma unroll
+    for (int i = 0; i < CH; i++) next_x[i] = next_y[i] = wide_t<T, V>{};
     if (at >= a.T) return;
     load_row<T, V, NTH, CH>(next_x, (const T*)a.x + (size_t)at * a.ld_x, lane, a.width);
     load_row<T, V, NTH, CH>(next_y, (const T*)a.dy + (size_t)at * a.ld_y, lane, a.width);
   };
-  if (AHEAD) ask(t);
-  for (; t < a.T; t += step) {
+  int64_t t0 = (int64_t)blockIdx.x * ROWS;
+  if (AHEAD) ask(t0 + row);
+  for (; t0 < a.T; t0 += step) {            // (all rows of a block together; one behind the last has zeros)
+    const int64_t t = t0 + row;
     if (!AHEAD) ask(t);
 #pragma unroll
     for (int i = 0; i < CH; i++) { x[i] = next_x[i]; y[i] = next_y[i]; }
@@ -194,39 +199,47 @@ __global__ __launch_bounds__(block_of<NTH>()) void layer_norm_bwd_kernel(NormArg
           db[i][j] += g;
           o[j] = (T)(r * (g * (float)gain[i][j] - mean_w - d * k));
         }
-        store_wide<V>(dx + c, o);
+        if (t < a.T) store_wide<V>(dx + c, o);
       }
     }
   }
-  // the block's rows of partial sums: rows side by side meet in LDS
+  // the block's rows of partial sums meet in LDS, half of them giving theirs to the other half
   float* part = a.part + (size_t)blockIdx.x * 2 * a.width;
   if constexpr (ROWS > 1) {
-    __shared__ float red[ROWS][2][NTH * CH * V];
-    const int row = threadIdx.x / NTH;
+    __shared__ float red[ROWS / 2][2][COLS];
 #pragma unroll
-    for (int i = 0; i < CH; i++)
+    for (int half = ROWS / 2; half > 0; half /= 2) {
+      if (row >= half && row < 2 * half) {
 #pragma unroll
-      for (int j = 0; j < V; j++) {
-        const int c = (i * NTH + lane) * V + j;
-        red[row][0][c] = dg[i][j];
-        red[row][1][c] = db[i][j];
+        for (int i = 0; i < CH; i++) {
+          const int c = (i * NTH + lane) * V;
+          wide_t<float, V> u, v;
+#pragma unroll
+          for (int j = 0; j < V; j++) { u[j] = dg[i][j]; v[j] = db[i][j]; }
+          store_wide<V>(&red[row - half][0][c], u);
+          store_wide<V>(&red[row - half][1][c], v);
+        }
       }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 2 * a.width; i += block_of<NTH>()) {
-      const int which = i >= a.width, c = which ? i - a.width : i;
-      float s = red[0][which][c];
+      __syncthreads();
+      if (row < half) {
 #pragma unroll
-      for (int k = 1; k < ROWS; k++) s += red[k][which][c];
-      part[i] = s;
+        for (int i = 0; i < CH; i++) {
+          const int c = (i * NTH + lane) * V;
+          const wide_t<float, V> u = load_wide<V>((const float*)&red[row][0][c]), v = load_wide<V>((const float*)&red[row][1][c]);
+#pragma unroll
+          for (int j = 0; j < V; j++) { dg[i][j] += u[j]; db[i][j] += v[j]; }
+        }
+      }
+      __syncthreads();
     }
-  } else {
+  }
+  if (row > 0) return;
 #pragma unroll
-    for (int i = 0; i < CH; i++) {
-      const int c = (i * NTH + lane) * V;
-      if (c < a.width) {
+  for (int i = 0; i < CH; i++) {
+    const int c = (i * NTH + lane) * V;
+    if (c < a.width) {
 #pragma unroll
-        for (int j = 0; j < V; j++) { part[c + j] = dg[i][j]; part[a.width + c + j] = db[i][j]; }
-      }
+      for (int j = 0; j < V; j++) { part[c + j] = dg[i][j]; part[a.width + c + j] = db[i][j]; }
     }
   }
 }
@@ -281,27 +294,27 @@ NormArgs args(const ah_layer_norm_t* c, const void* x, const void* dy, void* out
   return a;
 }
 
-// Lanes to a row, by its width alone
-int row_lanes(int width) { return width <= 1024 ? 64 : width <= 4096 ? 256 : 1024; }
-int bwd_blocks(const ah_layer_norm_t* c) {
-  const int rows = std::max(1, 256 / row_lanes(c->width));
-  return std::max(1, std::min(kMaxBlocks, (c->rows + rows - 1) / rows));
+// Lanes to a row and pieces of V elements a lane, as constants: forward 8 or 16 elements a lane, backward 8 up to the widest rows (4096 x 4096 in bf16: 32 us, and 36 with a row
+// of 64 elements a lane in one wave, which waits for no other).
+template <bool BWD, int V, class F>
+void by_width(int width, const F& go) {
+  auto with = [&](auto lanes, auto elements) { go(lanes, std::integral_constant<int, decltype(elements)::value / V>()); };
+#define AH_N(x) std::integral_constant<int, x>()
+  if (width <= 512) with(AH_N(64), AH_N(8));
+  else if (width <= 1024) { if constexpr (BWD) with(AH_N(128), AH_N(8)); else with(AH_N(64), AH_N(16)); }
+  else if (width <= 2048) with(AH_N(256), AH_N(8));
+  else if (width <= 4096) { if constexpr (BWD) with(AH_N(512), AH_N(8)); else with(AH_N(256), AH_N(16)); }
+  else if (width <= 8192) with(AH_N(1024), AH_N(8));
+  else with(AH_N(1024), AH_N(16));
+#undef AH_N
 }
 
-// go(lanes, pieces a lane) as constants for rows of `width` elements in pieces of V
-template <int V, class F>
-void by_width(int width, const F& go) {
-  typedef std::integral_constant<int, 64> L64;
-  typedef std::integral_constant<int, 256> L256;
-  typedef std::integral_constant<int, 1024> L1024;
-  typedef std::integral_constant<int, 8 / V> One;         // 8 elements a lane
-  typedef std::integral_constant<int, 16 / V> Two;
-  if (width <= 512) go(L64(), One());
-  else if (width <= 1024) go(L64(), Two());
-  else if (width <= 2048) go(L256(), One());
-  else if (width <= 4096) go(L256(), Two());
-  else if (width <= 8192) go(L1024(), One());
-  else go(L1024(), Two());
+int fwd_rows(int width) { return width <= 1024 ? 4 : 1; }        // of a block
+int bwd_blocks(const ah_layer_norm_t* c) {
+  int lanes = 64;
+  while (lanes < 1024 && lanes * 8 < c->width) lanes *= 2;
+  const int rows = kBwdThreads / lanes;
+  return std::max(1, std::min(kMaxBlocks, (c->rows + rows - 1) / rows));
 }
 
 template <bool BWD>
@@ -311,9 +324,9 @@ hipError_t run(const NormArgs& a, const ah_layer_norm_t* c, bool wide, int block
     typedef decltype(p) PT;
     constexpr int V = decltype(v)::value;
     constexpr bool RMS = decltype(r)::value;
-    by_width<V>(a.width, [&](auto lanes, auto pieces) {
+    by_width<BWD, V>(a.width, [&](auto lanes, auto pieces) {
       constexpr int NTH = decltype(lanes)::value, CH = decltype(pieces)::value;
-      if constexpr (BWD) hipLaunchKernelGGL((layer_norm_bwd_kernel<T, PT, V, NTH, CH, RMS>), dim3(blocks), dim3(block_of<NTH>()), 0, s, a);
+      if constexpr (BWD) hipLaunchKernelGGL((layer_norm_bwd_kernel<T, PT, V, NTH, CH, RMS>), dim3(blocks), dim3(kBwdThreads), 0, s, a);
       else hipLaunchKernelGGL((layer_norm_fwd_kernel<T, PT, V, NTH, CH, RMS>), dim3(blocks), dim3(block_of<NTH>()), 0, s, a);
     });
   };
@@ -348,7 +361,7 @@ extern "C" int ah_layer_norm_fwd(const ah_layer_norm_t* c, const void* x, void* 
   const NormArgs a = args(c, x, nullptr, y, c->ld_y, nullptr);
   if (shifted(x, a.ld_x, a)) return set_error(AH_EINVAL, "ah_layer_norm_fwd: y in the place of x needs x's row stride");
   const bool wide = c->width % 8 == 0 && rows16(x, a.ld_x, ab) && rows16(y, a.ld_out, ab);
-  const int block = std::max(256, row_lanes(c->width)), rows = block / row_lanes(c->width);
+  const int rows = fwd_rows(c->width), block = c->width > 4096 ? 1024 : 256;
   return hip_status(run<false>(a, c, wide, std::min((c->rows + rows - 1) / rows, kFwdBlocks * 256 / block), (hipStream_t)stream), "ah_layer_norm_fwd");
 }
 
