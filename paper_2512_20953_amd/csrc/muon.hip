@@ -105,17 +105,23 @@ __global__ __launch_bounds__(NT) void momentum_kernel(Table t, Hyper h) {
 }
 
 // 1 / (norm + eps): a block a matrix
-__global__ __launch_bounds__(NT) void norm_kernel(Table t, Hyper h) {
-  __shared__ double red[NT / 64];
+constexpr int kNormThreads = 1024;
+__global__ __launch_bounds__(kNormThreads) void norm_kernel(Table t, Hyper h) {
+  __shared__ double red[kNormThreads / 64];
   const Matrix& e = t.e[blockIdx.x];
   const int n = ((e.rows + kPiece - 1) / kPiece) * ((e.cols + kPiece - 1) / kPiece);
   double s = 0;
-  for (int i = threadIdx.x; i < n; i += NT) s += e.part[i];
+#pragma unroll 4
+  for (int i = threadIdx.x; i < n; i += kNormThreads) s += e.part[i];
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
   __syncthreads();
-  if (threadIdx.x == 0) *e.inv = 1.0 / (sqrt(red[0] + red[1] + red[2] + red[3]) + h.eps64);
+  if (threadIdx.x == 0) {
+#pragma unroll
+    for (int w = 1; w < kNormThreads / 64; w++) s += red[w];
+    *e.inv = 1.0 / (sqrt(s) + h.eps64);
+  }
 }
 
 // X of fp32 as two fp16 numbers
@@ -204,22 +210,24 @@ __global__ __launch_bounds__(NT) void apply_kernel(Table t, Hyper h, int last) {
 // ---- the products.  S x S tiles, four waves of S / 2 x S / 2.  SYM_A: A = X X^T; SYM_B: B = b A + c A A^T; STEP: X = a X + B X.
 enum Product { SYM_A, SYM_B, STEP };
 
-// block -> tile of its matrix.  Blocks are dealt to the 8 XCDs round-robin: consecutive tiles go to one XCD, down groups of 4 tile rows (symmetric: along the rows).
-__device__ __forceinline__ uint32_t xcd_order(uint32_t block, uint32_t blocks) {
-  return (block & 7) * (blocks >> 3) + min(block & 7, blocks & 7) + (block >> 3);
+// Blocks are dealt to the 8 XCDs round-robin.  Each XCD gets every eighth of the blocks of each matrix (which has a multiple of 8 of them) and of its tiles a row of consecutive ones, so
+// that all XCDs have as many of every matrix, the largest first: -1 where there is none left.
+__device__ __forceinline__ int xcd_tile(uint32_t block, int tiles) {
+  const int xcd = block & 7, at = block >> 3, most = tiles >> 3, more = tiles & 7;
+  return at < most + (xcd < more) ? xcd * most + min(xcd, more) + at : -1;
 }
 
 template <int S, Product P, int DEPTH>
-__global__ __launch_bounds__(NT) void product_kernel(Table t, uint32_t blocks, int from) {
+__global__ __launch_bounds__(NT) void product_kernel(Table t, int from) {
   constexpr int W = S / 2, TB = W / 16;
   constexpr bool BKS = P == STEP;                  // X is [k, columns] there
   constexpr int RING = k64::ring_bytes<S, S, DEPTH, true>();
   __shared__ __attribute__((aligned(1024))) char ring[RING];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / 2, wn = wave % 2;
-  const uint32_t logical = xcd_order(blockIdx.x, blocks);
-  const int which = __builtin_amdgcn_readfirstlane(find(t, logical));
+  const int which = __builtin_amdgcn_readfirstlane(find(t, blockIdx.x));
   const Matrix& e = t.e[which];
-  const int tile = (int)(logical - t.first[which]);
+  const int tile = xcd_tile(blockIdx.x - t.first[which], P == STEP ? (e.n / S) * (e.k / S) : (e.n / S) * (e.n / S + 1) / 2);
+  if (tile < 0) return;
   int ti, tj;
   if constexpr (P == STEP) {
     const int tm = e.n / S, tn = e.k / S, group = tile / (4 * tn), rows = min(tm - 4 * group, 4), in = tile - group * 4 * tn;
@@ -411,12 +419,12 @@ hipError_t launch(Table& t, const Group& g, const F& blocks_of, const G& go) {
 
 template <int S, int DEPTH>
 hipError_t products(Table& t, const Group& g, int steps, hipStream_t s) {
-  auto triangle = [](const Matrix& e) { const uint64_t n = e.n / S; return n * (n + 1) / 2; };
-  auto all = [](const Matrix& e) { return (uint64_t)(e.n / S) * (e.k / S); };
+  auto triangle = [](const Matrix& e) { const uint64_t n = e.n / S; return up(n * (n + 1) / 2, 8); };
+  auto all = [](const Matrix& e) { return up((uint64_t)(e.n / S) * (e.k / S), 8); };
   for (int i = 0; i < steps; i++) {
-    hipError_t e = launch(t, g, triangle, [&](uint32_t b) { hipLaunchKernelGGL((product_kernel<S, SYM_A, DEPTH>), dim3(b), dim3(NT), 0, s, t, b, i & 1); });
-    if (e == hipSuccess) e = launch(t, g, triangle, [&](uint32_t b) { hipLaunchKernelGGL((product_kernel<S, SYM_B, DEPTH>), dim3(b), dim3(NT), 0, s, t, b, i & 1); });
-    if (e == hipSuccess) e = launch(t, g, all, [&](uint32_t b) { hipLaunchKernelGGL((product_kernel<S, STEP, DEPTH>), dim3(b), dim3(NT), 0, s, t, b, i & 1); });
+    hipError_t e = launch(t, g, triangle, [&](uint32_t b) { hipLaunchKernelGGL((product_kernel<S, SYM_A, DEPTH>), dim3(b), dim3(NT), 0, s, t, i & 1); });
+    if (e == hipSuccess) e = launch(t, g, triangle, [&](uint32_t b) { hipLaunchKernelGGL((product_kernel<S, SYM_B, DEPTH>), dim3(b), dim3(NT), 0, s, t, i & 1); });
+    if (e == hipSuccess) e = launch(t, g, all, [&](uint32_t b) { hipLaunchKernelGGL((product_kernel<S, STEP, DEPTH>), dim3(b), dim3(NT), 0, s, t, i & 1); });
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
@@ -447,7 +455,7 @@ hipError_t step_group(const ah_muon_t* c, const ah_muon_matrix_t* x, const Group
   hipError_t e = launch(t, g, pieces, [&](uint32_t b) {
     if (g32) hipLaunchKernelGGL(momentum_kernel<float>, dim3(b), dim3(NT), 0, s, t, h);
     else hipLaunchKernelGGL(momentum_kernel<bf16>, dim3(b), dim3(NT), 0, s, t, h);
-    hipLaunchKernelGGL(norm_kernel, dim3(g.which.size()), dim3(NT), 0, s, t, h);
+    hipLaunchKernelGGL(norm_kernel, dim3(g.which.size()), dim3(kNormThreads), 0, s, t, h);
   });
   if (e == hipSuccess)
     e = launch(t, g, pieces_x, [&](uint32_t b) {
