@@ -58,56 +58,6 @@ __device__ __forceinline__ void ring_step(const char* gA, const char* gB, uint32
 
 }  // namespace k32
 
-namespace ksplit {
-// The pipeline of the tiles whose waves share a sub-tile and split the k axis: of the four k-steps of a 64-wide
-// k-block, wave wk takes 4 / WGK.  The partial sums meet in the epilogue's staging strips.
-//  64 x 64 with four shares and 64 x 128 with two are for outputs of fewer than 256 tiles of 128 x 128.  Such a launch
-//    lasts as long as one block's chain of k-blocks; these have four (two) times the blocks, and a chain a quarter as
-//    long.  256 x 256 x 1024: 9.3 -> 5.5 us, 1024 x 1024 x 2048: 21.6 -> 8.8, 2048 x 1024 x 2048: 21.6 -> 13.2 (NT).
-//  128 x 128 with four shares: every wave owns the whole tile, so a k-block costs 32 KB of fragment reads instead of
-//    the 64 KB of four 64 x 64 sub-tiles.  Beside 512 clocks of MFMA the CU's path to and from the LDS was busy ~950
-//    (reads at 128 B per clock, the 32 KB fill at 1.7 times its bytes), now ~690; what bounds it then is the rate at
-//    which the loads arrive (64 B per clock and CU).  2048 x 2048 x 8192: 76 -> 61 us (NT; against the 32x32x16 loop:
-//    the present one has closed the gap, see kWholeCuMinK, and the tile is there for its shorter sums).  The epilogue moves four
-//    times the partial sums (3 us): at k = 2048 the two are level, and where two blocks of the 64 x 64 sub-tiles share
-//    a CU (more than 256 tiles) those are faster; in the weight gradient, whose transposing reads are half as long,
-//    there is no gain (67 against 67 us), so it is not built there.
-constexpr int BK = 64;
-template <int BM, int BN> constexpr int stage_bytes() { return (BM + BN) * 2 * BK; }
-// ring depth: all of a CU's 160 KB for the 128 x 128 tile, half of it for the small ones (two blocks share a CU): 5, 3 and 5 stages
-template <int BM, int BN> constexpr int stages() { return (BM * BN < 128 * 128 ? 81920 : 163840) / stage_bytes<BM, BN>(); }
-
-// Second (or only) part of a k-block: the block's slot is free (its fragments are in registers, the barrier is
-// passed), so the loads of the stage NS ahead go there while the next stage's first fragments are read.  The two
-// slots are distinct: the restrict qualifiers keep the LDS reads from waiting for the loads in flight.
-template <int BM, int BN, int WGM, int WGN, bool AKS, bool BKS>
-__device__ __forceinline__ void last_step(const char* pA, const char* pB, uint32_t* offA, uint32_t* offB, char* __restrict__ fill,
-                                          const char* __restrict__ next, int ks, const Frags<BK, BM, BN, WGM, WGN, AKS, BKS>& f,
-                                          Frags<BK, BM, BN, WGM, WGN, AKS, BKS>& fn, f32x16 (&acc)[BM / WGM / 32][BN / WGN / 32], int wave,
-                                          int wm, int wn, int lane) {
-  constexpr int TM = BM / WGM / 32, TN = BN / WGN / 32, NW = 4;
-  constexpr int NR = TM * (AKS ? 2 : 1) + TN * (BKS ? 2 : 1), NM = TM * TN, LPS = (BM + BN) / 8 / NW;
-  issue_tile_loads<BK, BM, NW>(pA, offA, fill, wave);
-  issue_tile_loads<BK, BN, NW>(pB, offB, fill + BM * 2 * BK, wave);
-  fn.load(next, next + BM * 2 * BK, ks, wm, wn, lane);
-  mma_step<BK, BM, BN, WGM, WGN, AKS, BKS>(f, acc);
-  interleave<0, NM, NR, LPS, NM / 2>();
-}
-
-// First part of a two-step k-block
-template <int BM, int BN, int WGM, int WGN, bool AKS, bool BKS>
-__device__ __forceinline__ void first_step(const char* __restrict__ cur, int ks, const Frags<BK, BM, BN, WGM, WGN, AKS, BKS>& f,
-                                           Frags<BK, BM, BN, WGM, WGN, AKS, BKS>& fn, f32x16 (&acc)[BM / WGM / 32][BN / WGN / 32], int wm,
-                                           int wn, int lane) {
-  constexpr int TM = BM / WGM / 32, TN = BN / WGN / 32;
-  constexpr int NR = TM * (AKS ? 2 : 1) + TN * (BKS ? 2 : 1), NM = TM * TN;
-  fn.load(cur, cur + BM * 2 * BK, ks, wm, wn, lane);
-  mma_step<BK, BM, BN, WGM, WGN, AKS, BKS>(f, acc);
-  interleave<0, NM, NR, 0, NM / 2>();
-}
-
-}  // namespace ksplit
-
 // One tile of a product: block `block` of the (M / BM) (N / BN) k_shares that cover it.
 template <int BM, int BN, int WGM, int WGN, int WGK, bool AKS, bool BKS, int EPI, int DEPTH = 2>
 __device__ __forceinline__ void gemm_tile(const GemmArgs& g, int block) {

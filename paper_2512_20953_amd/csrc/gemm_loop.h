@@ -148,14 +148,20 @@ __device__ __forceinline__ void interleave() {
   }
 }
 
-template <int BK, int BM, int BN, int WGM, int WGN, bool AKS, bool BKS>
+template <bool F16, int BK, int BM, int BN, int WGM, int WGN, bool AKS, bool BKS>
 __device__ __forceinline__ void mma_step(const Frags<BK, BM, BN, WGM, WGN, AKS, BKS>& f, f32x16 (&acc)[BM / WGM / 32][BN / WGN / 32]) {
   constexpr int TM = BM / WGM / 32, TN = BN / WGN / 32;
 #pragma unroll
   for (int tm = 0; tm < TM; tm++)
 #pragma unroll
-    for (int tn = 0; tn < TN; tn++)
-      acc[tm][tn] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.b[tn], f.a[tm], acc[tm][tn], 0, 0, 0);
+    for (int tn = 0; tn < TN; tn++) {
+      if constexpr (F16) {
+        typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+        acc[tm][tn] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, f.b[tn]), __builtin_bit_cast(f16x8, f.a[tm]), acc[tm][tn], 0, 0, 0);
+      } else {
+        acc[tm][tn] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.b[tn], f.a[tm], acc[tm][tn], 0, 0, 0);
+      }
+    }
 }
 
 // The 16 x 16 x 32 instruction does the flops of the 32 x 32 x 16 one at less power, which is what bounds a loop that keeps the matrix
@@ -311,5 +317,101 @@ __device__ __forceinline__ void run(const char* gA, const char* gB, int lda, int
 }
 
 }  // namespace k64
+
+namespace ksplit {
+// The pipeline of the tiles whose waves share a sub-tile and split the k axis: of the four k-steps of a 64-wide
+// k-block, wave wk takes 4 / WGK.  The partial sums meet in the epilogue's staging strips.
+//  64 x 64 with four shares and 64 x 128 with two are for outputs of fewer than 256 tiles of 128 x 128.  Such a launch
+//    lasts as long as one block's chain of k-blocks; these have four (two) times the blocks, and a chain a quarter as
+//    long.  256 x 256 x 1024: 9.3 -> 5.5 us, 1024 x 1024 x 2048: 21.6 -> 8.8, 2048 x 1024 x 2048: 21.6 -> 13.2 (NT).
+//  128 x 128 with four shares: every wave owns the whole tile, so a k-block costs 32 KB of fragment reads instead of
+//    the 64 KB of four 64 x 64 sub-tiles.  Beside 512 clocks of MFMA the CU's path to and from the LDS was busy ~950
+//    (reads at 128 B per clock, the 32 KB fill at 1.7 times its bytes), now ~690; what bounds it then is the rate at
+//    which the loads arrive (64 B per clock and CU).  2048 x 2048 x 8192: 76 -> 61 us (NT; against the 32x32x16 loop:
+//    the present one has closed the gap, see kWholeCuMinK, and the tile is there for its shorter sums).  The epilogue moves four
+//    times the partial sums (3 us): at k = 2048 the two are level, and where two blocks of the 64 x 64 sub-tiles share
+//    a CU (more than 256 tiles) those are faster; in the weight gradient, whose transposing reads are half as long,
+//    there is no gain (67 against 67 us), so it is not built there.
+constexpr int BK = 64;
+template <int BM, int BN> constexpr int stage_bytes() { return (BM + BN) * 2 * BK; }
+// ring depth: all of a CU's 160 KB for the 128 x 128 tile, half of it for the small ones (two blocks share a CU): 5, 3 and 5 stages
+template <int BM, int BN> constexpr int stages() { return (BM * BN < 128 * 128 ? 81920 : 163840) / stage_bytes<BM, BN>(); }
+
+// Second (or only) part of a k-block: the block's slot is free (its fragments are in registers, the barrier is
+// passed), so the loads of the stage NS ahead go there while the next stage's first fragments are read.  The two
+// slots are distinct: the restrict qualifiers keep the LDS reads from waiting for the loads in flight.
+template <int BM, int BN, int WGM, int WGN, bool AKS, bool BKS, bool F16 = false>
+__device__ __forceinline__ void last_step(const char* pA, const char* pB, uint32_t* offA, uint32_t* offB, char* __restrict__ fill,
+                                          const char* __restrict__ next, int ks, const Frags<BK, BM, BN, WGM, WGN, AKS, BKS>& f,
+                                          Frags<BK, BM, BN, WGM, WGN, AKS, BKS>& fn, f32x16 (&acc)[BM / WGM / 32][BN / WGN / 32], int wave,
+                                          int wm, int wn, int lane) {
+  constexpr int TM = BM / WGM / 32, TN = BN / WGN / 32, NW = 4;
+  constexpr int NR = TM * (AKS ? 2 : 1) + TN * (BKS ? 2 : 1), NM = TM * TN, LPS = (BM + BN) / 8 / NW;
+  issue_tile_loads<BK, BM, NW>(pA, offA, fill, wave);
+  issue_tile_loads<BK, BN, NW>(pB, offB, fill + BM * 2 * BK, wave);
+  fn.load(next, next + BM * 2 * BK, ks, wm, wn, lane);
+  mma_step<F16, BK, BM, BN, WGM, WGN, AKS, BKS>(f, acc);
+  interleave<0, NM, NR, LPS, NM / 2>();
+}
+
+// First part of a two-step k-block
+template <int BM, int BN, int WGM, int WGN, bool AKS, bool BKS, bool F16 = false>
+__device__ __forceinline__ void first_step(const char* __restrict__ cur, int ks, const Frags<BK, BM, BN, WGM, WGN, AKS, BKS>& f,
+                                           Frags<BK, BM, BN, WGM, WGN, AKS, BKS>& fn, f32x16 (&acc)[BM / WGM / 32][BN / WGN / 32], int wm,
+                                           int wn, int lane) {
+  constexpr int TM = BM / WGM / 32, TN = BN / WGN / 32;
+  constexpr int NR = TM * (AKS ? 2 : 1) + TN * (BKS ? 2 : 1), NM = TM * TN;
+  fn.load(cur, cur + BM * 2 * BK, ks, wm, wn, lane);
+  mma_step<F16, BK, BM, BN, WGM, WGN, AKS, BKS>(f, acc);
+  interleave<0, NM, NR, 0, NM / 2>();
+}
+
+// The whole loop where each of four waves takes one k-step in four of the whole tile, over one piece of the k axis (K a multiple of 128): acc are the wave's partial sums.
+// The wave's redundant tail loads are still in flight behind it.
+template <int BM, int BN, bool AKS, bool BKS, bool F16>
+__device__ __forceinline__ void run(const char* gA, const char* gB, int lda, int ldb, int K, char* ring, f32x16 (&acc)[BM / 32][BN / 32], int wave, int lane) {
+  constexpr int STAGE = stage_bytes<BM, BN>(), NS = stages<BM, BN>(), NW = 4, LA = BM / 8 / NW, LB = BN / 8 / NW, LPS = LA + LB;
+  const size_t stepA = (AKS ? (size_t)BK * lda : (size_t)BK) * 2, stepB = (BKS ? (size_t)BK * ldb : (size_t)BK) * 2;   // bytes per k-block
+  uint32_t offA[LA], offB[LB];
+#pragma unroll
+  for (int i = 0; i < LA; i++) offA[i] = loader_src_offset<BK, BM, AKS, true>(wave + NW * i, lane, lda);
+#pragma unroll
+  for (int i = 0; i < LB; i++) offB[i] = loader_src_offset<BK, BN, BKS, true>(wave + NW * i, lane, ldb);
+  // The stage to be fetched next; past the last one that stage is fetched again into dead slots, which keeps the number of loads in flight uniform for the counted wait.
+  const int nk = K / BK;
+  const char *pA = gA, *pB = gB;
+  int fetched = 1;
+  auto advance = [&]() {
+    const bool more = fetched < nk;
+    fetched++;
+    pA = more ? pA + stepA : pA;
+    pB = more ? pB + stepB : pB;
+  };
+#pragma unroll
+  for (int t = 0; t < NS; t++) {
+    issue_tile_loads<BK, BM, NW>(pA, offA, ring + t * STAGE, wave);
+    issue_tile_loads<BK, BN, NW>(pB, offB, ring + t * STAGE + BM * 2 * BK, wave);
+    advance();
+  }
+  __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0((NS - 1) * LPS));
+  __builtin_amdgcn_s_barrier();
+  Frags<BK, BM, BN, 1, 1, AKS, BKS> f0, f1;
+  f0.load(ring, ring + BM * 2 * BK, wave, 0, 0, lane);
+  int c = 0;  // ring slot of k-block j
+  for (int j = 0; j < nk; j += 2) {
+    const int n = c + 1 == NS ? 0 : c + 1, n2 = n + 1 == NS ? 0 : n + 1;
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0((NS - 2) * LPS));
+    __builtin_amdgcn_s_barrier();
+    last_step<BM, BN, 1, 1, AKS, BKS, F16>(pA, pB, offA, offB, ring + c * STAGE, ring + n * STAGE, wave, f0, f1, acc, wave, 0, 0, lane);
+    advance();
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0((NS - 2) * LPS));
+    __builtin_amdgcn_s_barrier();
+    last_step<BM, BN, 1, 1, AKS, BKS, F16>(pA, pB, offA, offB, ring + n * STAGE, ring + n2 * STAGE, wave, f1, f0, acc, wave, 0, 0, lane);
+    advance();
+    c = n2;
+  }
+}
+
+}  // namespace ksplit
 
 }  // namespace ah

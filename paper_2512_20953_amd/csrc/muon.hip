@@ -45,6 +45,7 @@ struct Matrix {
   int64_t ld_p, ld_g, ld_m, ld_master;
   int rows, cols, n, k;        // n x k: the padded X
   float wd, scale;
+  int aligned;                 // rows of all four begin at whole multiples of 4 elements
 };
 
 struct Table {
@@ -67,15 +68,57 @@ __device__ __forceinline__ int find(const Table& t, uint32_t block) {
   return k;
 }
 
-template <class GT>
-__device__ __forceinline__ float gradient(const Matrix& e, int64_t r, int64_t c, float factor) {
-  return (float)((const GT*)e.g)[r * e.ld_g + c] * factor;
-}
-
 // m += rest (g - m); the update is m, or (nesterov) the same once more
 __device__ __forceinline__ float blend(float m, float g, float rest) { return m + rest * (g - m); }
 
-// ---- momentum and the sum of squares of each piece.  Lanes lie along a row.
+// The element-wise passes take a piece of 64 x 64 a block.  V = 4: whole pieces of aligned matrices, 4 elements a lane and 16 rows at once, all loads in flight together;
+// V = 1: any piece, every row and column looked at.
+template <int V> struct Walk {
+  static constexpr int kAcross = kPiece / V, kRows = NT / kAcross, kTurns = kPiece / kRows, kBatch = V == 4 ? kTurns : 4;
+};
+
+// Elements (r, c) .. of a row of T; those outside the matrix read as 0
+template <int V, class T>
+__device__ __forceinline__ wide_t<T, V> get(const void* p, int64_t ld, int64_t r, int64_t c, const Matrix& e) {
+  wide_t<T, V> v = {};
+  if (V == 4 || (r < e.rows && c < e.cols)) v = load_wide<V>((const T*)p + r * ld + c);
+  return v;
+}
+template <int V, class T>
+__device__ __forceinline__ void set(void* p, int64_t ld, int64_t r, int64_t c, const Matrix& e, wide_t<T, V> v) {
+  if (V == 4 || (r < e.rows && c < e.cols)) store_wide<V>((T*)p + r * ld + c, v);
+}
+__device__ __forceinline__ bool whole(const Matrix& e, int64_t r0, int64_t c0) { return e.aligned && r0 + kPiece <= e.rows && c0 + kPiece <= e.cols; }
+
+// ---- momentum and the sum of squares of each piece
+template <class GT, int V>
+__device__ __forceinline__ double momentum_piece(const Matrix& e, const Hyper& h, int64_t r0, int64_t c0, float factor) {
+  typedef Walk<V> W;
+  const int64_t row = r0 + threadIdx.x / W::kAcross, c = c0 + threadIdx.x % W::kAcross * V;
+  double s = 0;
+  for (int turn = 0; turn < W::kTurns; turn += W::kBatch) {
+    wide_t<float, V> m[W::kBatch];
+    wide_t<GT, V> g[W::kBatch];
+#pragma unroll
+    for (int i = 0; i < W::kBatch; i++) {
+      const int64_t r = row + (turn + i) * W::kRows;
+      m[i] = get<V, float>(e.m, e.ld_m, r, c, e);
+      g[i] = get<V, GT>(e.g, e.ld_g, r, c, e);
+    }
+#pragma unroll
+    for (int i = 0; i < W::kBatch; i++) {
+#pragma unroll
+      for (int j = 0; j < V; j++) {
+        const float gj = (float)g[i][j] * factor, v = blend(m[i][j], gj, h.rest), u = h.nesterov ? blend(v, gj, h.rest) : v;
+        m[i][j] = v;
+        s += (double)u * u;             // (outside the matrix 0, unless the factor is not finite: then the norm is not either)
+      }
+      set<V, float>(e.m, e.ld_m, row + (turn + i) * W::kRows, c, e, m[i]);
+    }
+  }
+  return s;
+}
+
 template <class GT>
 __global__ __launch_bounds__(NT) void momentum_kernel(Table t, Hyper h) {
   __shared__ double red[NT / 64];
@@ -83,20 +126,10 @@ __global__ __launch_bounds__(NT) void momentum_kernel(Table t, Hyper h) {
   const Matrix& e = t.e[k];
   const uint32_t piece = blockIdx.x - t.first[k];
   const int across = (e.cols + kPiece - 1) / kPiece;
-  const int64_t r0 = (int64_t)(piece / across) * kPiece, c = (int64_t)(piece % across) * kPiece + (threadIdx.x & 63);
+  const int64_t r0 = (int64_t)(piece / across) * kPiece, c0 = (int64_t)(piece % across) * kPiece;
   const float factor = h.grad_norm ? h.grad_norm[1] : 1.f;
   double s = 0;
-  if (factor == factor && c < e.cols) {
-    const int64_t end = min(r0 + kPiece, (int64_t)e.rows);
-    for (int64_t r = r0 + (threadIdx.x >> 6); r < end; r += NT / 64) {
-      float* m = e.m + r * e.ld_m + c;
-      const float g = gradient<GT>(e, r, c, factor);
-      const float v = blend(*m, g, h.rest);
-      *m = v;
-      const float u = h.nesterov ? blend(v, g, h.rest) : v;
-      s += (double)u * u;
-    }
-  }
+  if (factor == factor) s = whole(e, r0, c0) ? momentum_piece<GT, 4>(e, h, r0, c0, factor) : momentum_piece<GT, 1>(e, h, r0, c0, factor);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
@@ -130,81 +163,143 @@ __device__ __forceinline__ void split(float x, f16& hi, f16& lo) {
   lo = (f16)((x - (float)hi) * kLo);
 }
 
+// V elements of X from (row, col) on: 4 of them are aligned, as X is padded to whole pieces
+template <int V>
+__device__ __forceinline__ void set_x(const Matrix& e, int64_t row, int64_t col, const float (&x)[V]) {
+  wide_t<f16, V> hi, lo;
+#pragma unroll
+  for (int j = 0; j < V; j++) {
+    f16 a, b;
+    split(x[j], a, b);
+    hi[j] = a;
+    lo[j] = b;
+  }
+  store_wide<V>(e.hi[0] + row * e.k + col, hi);
+  store_wide<V>(e.lo + row * e.k + col, lo);
+}
+
 // ---- X = u / norm, transposed where there are more rows than columns, zeros in what pads it: a piece of X a block
-template <class GT>
-__global__ __launch_bounds__(NT) void lay_out_kernel(Table t, Hyper h) {
-  __shared__ float turn[kPiece][kPiece + 1];
-  const int k = find(t, blockIdx.x);
-  const Matrix& e = t.e[k];
-  const uint32_t piece = blockIdx.x - t.first[k];
-  const int across = e.k / kPiece, lane = threadIdx.x & 63, row = threadIdx.x >> 6;
-  const int64_t i0 = (int64_t)(piece / across) * kPiece, j0 = (int64_t)(piece % across) * kPiece;      // of X
+template <class GT, int V>
+__device__ __forceinline__ void lay_out_piece(const Matrix& e, const Hyper& h, int64_t i0, int64_t j0, float (&turned)[kPiece][kPiece + 1]) {
+  typedef Walk<V> W;
+  const int row = threadIdx.x / W::kAcross, col = threadIdx.x % W::kAcross * V;
   const float factor = h.grad_norm ? h.grad_norm[1] : 1.f;
   const double inv = *e.inv * kX;
   const bool tall = e.rows > e.cols;
   const int64_t r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;
-#pragma unroll 4
-  for (int s = row; s < kPiece; s += NT / 64) {
-    const int64_t r = r0 + s, c = c0 + lane;
-    float v = 0.f;
-    if (r < e.rows && c < e.cols) {
-      v = e.m[r * e.ld_m + c];
-      if (h.nesterov) v = blend(v, gradient<GT>(e, r, c, factor), h.rest);
-      v = (float)(v * inv);
+  for (int turn = 0; turn < W::kTurns; turn += W::kBatch) {
+    wide_t<float, V> m[W::kBatch];
+    wide_t<GT, V> g[W::kBatch] = {};
+#pragma unroll
+    for (int i = 0; i < W::kBatch; i++) {
+      const int64_t r = r0 + row + (turn + i) * W::kRows;
+      m[i] = get<V, float>(e.m, e.ld_m, r, c0 + col, e);
+      if (h.nesterov) g[i] = get<V, GT>(e.g, e.ld_g, r, c0 + col, e);
     }
-    if (tall) {
-      turn[s][lane] = v;
-    } else {
-      const int64_t at = (i0 + s) * e.k + j0 + lane;
-      split(v, e.hi[0][at], e.lo[at]);
+#pragma unroll
+    for (int i = 0; i < W::kBatch; i++) {
+      const int s = row + (turn + i) * W::kRows;
+      float x[V];
+#pragma unroll
+      for (int j = 0; j < V; j++) x[j] = (float)((h.nesterov ? blend(m[i][j], (float)g[i][j] * factor, h.rest) : m[i][j]) * inv);
+      if (tall) {
+#pragma unroll
+        for (int j = 0; j < V; j++) turned[s][col + j] = x[j];
+      } else {
+        set_x<V>(e, i0 + s, j0 + col, x);
+      }
     }
   }
+}
+
+template <class GT>
+__global__ __launch_bounds__(NT) void lay_out_kernel(Table t, Hyper h) {
+  __shared__ float turned[kPiece][kPiece + 1];
+  const int k = find(t, blockIdx.x);
+  const Matrix& e = t.e[k];
+  const uint32_t piece = blockIdx.x - t.first[k];
+  const int across = e.k / kPiece;
+  const int64_t i0 = (int64_t)(piece / across) * kPiece, j0 = (int64_t)(piece % across) * kPiece;      // of X
+  const bool tall = e.rows > e.cols;
+  if (whole(e, tall ? j0 : i0, tall ? i0 : j0)) lay_out_piece<GT, 4>(e, h, i0, j0, turned);
+  else lay_out_piece<GT, 1>(e, h, i0, j0, turned);
   if (!tall) return;
   __syncthreads();
-#pragma unroll 4
-  for (int s = row; s < kPiece; s += NT / 64) {
-    const int64_t at = (i0 + s) * e.k + j0 + lane;
-    split(turn[lane][s], e.hi[0][at], e.lo[at]);
+  typedef Walk<4> W;
+  const int row = threadIdx.x / W::kAcross, col = threadIdx.x % W::kAcross * 4;
+#pragma unroll
+  for (int turn = 0; turn < W::kTurns; turn++) {
+    const int s = row + turn * W::kRows;
+    const float x[4] = {turned[col][s], turned[col + 1][s], turned[col + 2][s], turned[col + 3][s]};
+    set_x<4>(e, i0 + s, j0 + col, x);
   }
 }
 
 // ---- the step of the parameters: X back, transposed again
+template <class PT, bool MASTER, int V>
+__device__ __forceinline__ void apply_piece(const Matrix& e, int64_t r0, int64_t c0, float keep, float by, int last, float (&turned)[kPiece][kPiece + 1]) {
+  typedef Walk<V> W;
+  typedef std::conditional_t<MASTER, float, PT> ST;          // what is stepped
+  const int row = threadIdx.x / W::kAcross, col = threadIdx.x % W::kAcross * V;
+  const bool tall = e.rows > e.cols;
+  for (int turn = 0; turn < W::kTurns; turn += W::kBatch) {
+    wide_t<ST, V> old[W::kBatch];
+    float x[W::kBatch][V];
+#pragma unroll
+    for (int i = 0; i < W::kBatch; i++) {
+      const int s = row + (turn + i) * W::kRows;
+      old[i] = get<V, ST>(MASTER ? (const void*)e.master : e.p, MASTER ? e.ld_master : e.ld_p, r0 + s, c0 + col, e);
+      if (tall) {
+#pragma unroll
+        for (int j = 0; j < V; j++) x[i][j] = turned[s][col + j];
+      } else {                                               // (X is padded to whole pieces)
+        const wide_t<f16, V> hi = load_wide<V>((const f16*)e.hi[last] + (r0 + s) * e.k + c0 + col), lo = load_wide<V>((const f16*)e.lo + (r0 + s) * e.k + c0 + col);
+#pragma unroll
+        for (int j = 0; j < V; j++) x[i][j] = (float)hi[j] + (float)lo[j] * (1.f / kLo);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < W::kBatch; i++) {
+      const int64_t r = r0 + row + (turn + i) * W::kRows;
+      wide_t<PT, V> p;
+      wide_t<float, V> q;
+#pragma unroll
+      for (int j = 0; j < V; j++) {
+        q[j] = (float)old[i][j] * keep - by * x[i][j];
+        p[j] = (PT)q[j];
+      }
+      if constexpr (MASTER) set<V, float>(e.master, e.ld_master, r, c0 + col, e, q);
+      set<V, PT>(e.p, e.ld_p, r, c0 + col, e, p);
+    }
+  }
+}
+
 template <class PT, bool MASTER>
 __global__ __launch_bounds__(NT) void apply_kernel(Table t, Hyper h, int last) {
-  __shared__ float turn[kPiece][kPiece + 1];
+  __shared__ float turned[kPiece][kPiece + 1];
   if (h.grad_norm && h.grad_norm[1] != h.grad_norm[1]) return;
   const int k = find(t, blockIdx.x);
   const Matrix& e = t.e[k];
   const uint32_t piece = blockIdx.x - t.first[k];
-  const int across = (e.cols + kPiece - 1) / kPiece, lane = threadIdx.x & 63, row = threadIdx.x >> 6;
+  const int across = (e.cols + kPiece - 1) / kPiece;
   const int64_t r0 = (int64_t)(piece / across) * kPiece, c0 = (int64_t)(piece % across) * kPiece;
   const float lr = h.lr_dev ? *h.lr_dev : h.lr;
   const float keep = 1.f - lr * e.wd, by = lr * e.scale * (1.f / kX);
-  const f16* hi = e.hi[last];
-  const bool tall = e.rows > e.cols;
-  auto value = [&](int64_t at) { return (float)hi[at] + (float)e.lo[at] * (1.f / kLo); };
-  if (tall) {
-#pragma unroll 4
-    for (int s = row; s < kPiece; s += NT / 64) turn[s][lane] = value((c0 + s) * e.k + r0 + lane);    // (X is padded to whole pieces)
+  if (e.rows > e.cols) {
+    typedef Walk<4> W;
+    const int row = threadIdx.x / W::kAcross, col = threadIdx.x % W::kAcross * 4;
+#pragma unroll
+    for (int turn = 0; turn < W::kTurns; turn++) {
+      const int s = row + turn * W::kRows;
+      const int64_t at = (c0 + s) * e.k + r0 + col;
+      const wide_t<f16, 4> hi = load_wide<4>((const f16*)e.hi[last] + at), lo = load_wide<4>((const f16*)e.lo + at);
+#pragma unroll
+      for (int j = 0; j < 4; j++) turned[col + j][s] = (float)hi[j] + (float)lo[j] * (1.f / kLo);
+    }
     __syncthreads();
   }
-  const int64_t c = c0 + lane;
-  if (c >= e.cols) return;
-#pragma unroll 4
-  for (int s = row; s < kPiece; s += NT / 64) {
-    const int64_t r = r0 + s;
-    if (r >= e.rows) break;
-    const float x = tall ? turn[lane][s] : value(r * e.k + c);
-    PT* p = (PT*)e.p + r * e.ld_p + c;
-    if constexpr (MASTER) {
-      float* q = e.master + r * e.ld_master + c;
-      const float v = *q * keep - by * x;
-      *q = v;
-      *p = (PT)v;
-    } else {
-      *p = (PT)((float)*p * keep - by * x);
-    }
-  }
+  if (whole(e, r0, c0)) apply_piece<PT, MASTER, 4>(e, r0, c0, keep, by, last, turned);
+  else apply_piece<PT, MASTER, 1>(e, r0, c0, keep, by, last, turned);
 }
 
 // ---- the products.  S x S tiles, four waves of S / 2 x S / 2.  SYM_A: A = X X^T; SYM_B: B = b A + c A A^T; STEP: X = a X + B X.
@@ -217,6 +312,66 @@ __device__ __forceinline__ int xcd_tile(uint32_t block, int tiles) {
   return at < most + (xcd < more) ? xcd * most + min(xcd, more) + at : -1;
 }
 
+// Which tile a block computes, and its operands
+struct Job {
+  int ti, tj, m0, n0, lda, ldb, K;
+  const f16 *a, *b;
+};
+template <int S, Product P>
+__device__ __forceinline__ bool find_job(const Matrix& e, uint32_t block, int from, Job& j) {
+  const int tile = xcd_tile(block, P == STEP ? (e.n / S) * (e.k / S) : (e.n / S) * (e.n / S + 1) / 2);
+  if (tile < 0) return false;
+  if constexpr (P == STEP) {                       // down groups of 4 tile rows
+    const int tm = e.n / S, tn = e.k / S, group = tile / (4 * tn), rows = min(tm - 4 * group, 4), in = tile - group * 4 * tn;
+    j.ti = group * 4 + in % rows;
+    j.tj = in / rows;
+  } else {                                         // row ti of the triangle holds ti + 1 tiles
+    int ti = (int)((sqrtf(8.f * tile + 1.f) - 1.f) * 0.5f);
+    while (ti * (ti + 1) / 2 > tile) ti--;
+    while ((ti + 1) * (ti + 2) / 2 <= tile) ti++;
+    j.ti = ti;
+    j.tj = tile - ti * (ti + 1) / 2;
+  }
+  j.m0 = j.ti * S;
+  j.n0 = j.tj * S;
+  const f16* X = e.hi[from];
+  if constexpr (P == SYM_A) { j.lda = j.ldb = j.K = e.k; j.a = X + (size_t)j.m0 * e.k; j.b = X + (size_t)j.n0 * e.k; }
+  else if constexpr (P == SYM_B) { j.lda = j.ldb = j.K = e.n; j.a = e.A + (size_t)j.m0 * e.n; j.b = e.A + (size_t)j.n0 * e.n; }
+  else { j.lda = j.K = e.n; j.ldb = e.k; j.a = e.B + (size_t)j.m0 * e.n; j.b = X + j.n0; }
+  return true;
+}
+
+// 8 elements of a result from (row, col) on, whose sums are v
+template <Product P>
+__device__ __forceinline__ void put8(const Matrix& e, int from, int row, int col, const float (&v)[8]) {
+  if constexpr (P == STEP) {
+    const size_t at = (size_t)row * e.k + col;
+    const f16x8 xh = *(const f16x8*)(e.hi[from] + at), xl = *(const f16x8*)(e.lo + at);
+    f16x8 oh, ol;
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+      f16 hi, lo;
+      split(__builtin_fmaf(kA_, (float)xh[j] + (float)xl[j] * (1.f / kLo), v[j] * (1.f / kA)), hi, lo);
+      oh[j] = hi;
+      ol[j] = lo;
+    }
+    *(f16x8*)(e.hi[from ^ 1] + at) = oh;
+    *(f16x8*)(e.lo + at) = ol;
+  } else {
+    const size_t at = (size_t)row * e.n + col;
+    f16x8 o;
+    if constexpr (P == SYM_A) {
+#pragma unroll
+      for (int j = 0; j < 8; j++) o[j] = (f16)(v[j] * (kA / (kX * kX)));
+    } else {
+      const f16x8 x = *(const f16x8*)(e.A + at);   // (A is symmetric bit for bit)
+#pragma unroll
+      for (int j = 0; j < 8; j++) o[j] = (f16)__builtin_fmaf(kB_, (float)x[j], v[j] * (kC_ / kA));
+    }
+    *(f16x8*)((P == SYM_A ? e.A : e.B) + at) = o;
+  }
+}
+
 template <int S, Product P, int DEPTH>
 __global__ __launch_bounds__(NT) void product_kernel(Table t, int from) {
   constexpr int W = S / 2, TB = W / 16;
@@ -226,32 +381,14 @@ __global__ __launch_bounds__(NT) void product_kernel(Table t, int from) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / 2, wn = wave % 2;
   const int which = __builtin_amdgcn_readfirstlane(find(t, blockIdx.x));
   const Matrix& e = t.e[which];
-  const int tile = xcd_tile(blockIdx.x - t.first[which], P == STEP ? (e.n / S) * (e.k / S) : (e.n / S) * (e.n / S + 1) / 2);
-  if (tile < 0) return;
-  int ti, tj;
-  if constexpr (P == STEP) {
-    const int tm = e.n / S, tn = e.k / S, group = tile / (4 * tn), rows = min(tm - 4 * group, 4), in = tile - group * 4 * tn;
-    ti = group * 4 + in % rows;
-    tj = in / rows;
-  } else {                                         // row ti of the triangle holds ti + 1 tiles
-    ti = (int)((sqrtf(8.f * tile + 1.f) - 1.f) * 0.5f);
-    while (ti * (ti + 1) / 2 > tile) ti--;
-    while ((ti + 1) * (ti + 2) / 2 <= tile) ti++;
-    tj = tile - ti * (ti + 1) / 2;
-  }
-  const int m0 = ti * S, n0 = tj * S;
-  const f16* X = e.hi[from];
-  const f16 *a, *b;
-  int lda, ldb, K;
-  if constexpr (P == SYM_A) { lda = ldb = K = e.k; a = X + (size_t)m0 * lda; b = X + (size_t)n0 * ldb; }
-  else if constexpr (P == SYM_B) { lda = ldb = K = e.n; a = e.A + (size_t)m0 * lda; b = e.A + (size_t)n0 * ldb; }
-  else { lda = K = e.n; ldb = e.k; a = e.B + (size_t)m0 * lda; b = X + n0; }
+  Job g;
+  if (!find_job<S, P>(e, blockIdx.x - t.first[which], from, g)) return;
   f32x4 acc[TB][TB];
 #pragma unroll
   for (int i = 0; i < TB; i++)
 #pragma unroll
     for (int j = 0; j < TB; j++) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  k64::run<S, S, 2, 2, false, BKS, DEPTH, true>((const char*)a, (const char*)b, lda, ldb, 0, K, ring, acc, wave, wm, wn, lane);
+  k64::run<S, S, 2, 2, false, BKS, DEPTH, true>((const char*)g.a, (const char*)g.b, g.lda, g.ldb, 0, g.K, ring, acc, wave, wm, wn, lane);
   __builtin_amdgcn_s_waitcnt(0);                   // the redundant tail loads are over before the ring is used again
   // The compiler does not see that the accumulators come from matrix instructions: 16 wait states before the first read
   // of the last one's result.
@@ -265,10 +402,10 @@ __global__ __launch_bounds__(NT) void product_kernel(Table t, int from) {
   static_assert(4 * 32 * ROWB <= RING, "the strips fit in the ring");
   __syncthreads();
   char* strip = ring + wave * (32 * ROWB);
-  const int cp = lane % PPR, row0 = lane / PPR, col = n0 + wn * W + cp * 8;
+  const int cp = lane % PPR, row0 = lane / PPR, n0 = g.n0 + wn * W;
 #pragma unroll
   for (int tm = 0; tm < W / 32; tm++) {
-    const int mbase = m0 + wm * W + tm * 32;
+    const int mbase = g.m0 + wm * W + tm * 32;
 #pragma unroll
     for (int tr = 0; tr < 2; tr++)
 #pragma unroll
@@ -281,54 +418,86 @@ __global__ __launch_bounds__(NT) void product_kernel(Table t, int from) {
       const char* q = strip + row * ROWB + cp * 32;
       const f32x4 v0 = *(const f32x4*)q, v1 = *(const f32x4*)(q + 16);
       const float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-      if constexpr (P == STEP) {
-        const size_t at = (size_t)(mbase + row) * e.k + col;
-        const f16x8 xh = *(const f16x8*)(X + at), xl = *(const f16x8*)(e.lo + at);
-        f16x8 oh, ol;
-#pragma unroll
-        for (int j = 0; j < 8; j++) {
-          f16 hi, lo;
-          split(__builtin_fmaf(kA_, (float)xh[j] + (float)xl[j] * (1.f / kLo), v[j] * (1.f / kA)), hi, lo);
-          oh[j] = hi;
-          ol[j] = lo;
-        }
-        *(f16x8*)(e.hi[from ^ 1] + at) = oh;
-        *(f16x8*)(e.lo + at) = ol;
-      } else {
-        const size_t at = (size_t)(mbase + row) * e.n + col;
-        f16x8 o;
-        if constexpr (P == SYM_A) {
-#pragma unroll
-          for (int j = 0; j < 8; j++) o[j] = (f16)(v[j] * (kA / (kX * kX)));
-        } else {
-          const f16x8 x = *(const f16x8*)(e.A + at);
-#pragma unroll
-          for (int j = 0; j < 8; j++) o[j] = (f16)__builtin_fmaf(kB_, (float)x[j], v[j] * (kC_ / kA));
-        }
-        *(f16x8*)((P == SYM_A ? e.A : e.B) + at) = o;
-      }
+      put8<P>(e, from, mbase + row, n0 + cp * 8, v);
     }
     if constexpr (P != STEP) {
-      if (ti != tj) {                              // the tile across the diagonal: 8 rows of a column a lane
+      if (g.ti != g.tj) {                          // the tile across the diagonal: 8 rows of a column a lane
 #pragma unroll
         for (int half = 0; half < W / 64; half++)
 #pragma unroll
           for (int r = 0; r < 4; r++) {
             const int c = half * 64 + lane;
-            const size_t at = (size_t)(n0 + wn * W + c) * e.n + mbase + r * 8;
-            f16x8 o, x = {};
-            if constexpr (P == SYM_B) x = *(const f16x8*)(e.A + at);          // (A is symmetric bit for bit)
+            float v[8];
 #pragma unroll
-            for (int j = 0; j < 8; j++) {
-              const float v = *(const float*)(strip + (r * 8 + j) * ROWB + c * 4);
-              o[j] = P == SYM_A ? (f16)(v * (kA / (kX * kX))) : (f16)__builtin_fmaf(kB_, (float)x[j], v * (kC_ / kA));
-            }
-            *(f16x8*)((P == SYM_A ? e.A : e.B) + at) = o;
+            for (int j = 0; j < 8; j++) v[j] = *(const float*)(strip + (r * 8 + j) * ROWB + c * 4);
+            put8<P>(e, from, n0 + c, mbase + r * 8, v);
           }
       }
     }
     __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(63));
     __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// The same for few tiles: 64 x 64, each wave one k-step in four of the whole tile.  Four times the blocks, whose chains of k-steps are a quarter as long.
+template <Product P>
+__global__ __launch_bounds__(NT) void small_product_kernel(Table t, int from) {
+  constexpr int S = 64, ROWB = S * 4 + 16, STRIP = S * ROWB;
+  constexpr int RING = ksplit::stages<S, S>() * ksplit::stage_bytes<S, S>();
+  static_assert(4 * STRIP <= RING, "the partial sums fit in the ring");
+  __shared__ __attribute__((aligned(1024))) char ring[RING];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int which = __builtin_amdgcn_readfirstlane(find(t, blockIdx.x));
+  const Matrix& e = t.e[which];
+  Job g;
+  if (!find_job<S, P>(e, blockIdx.x - t.first[which], from, g)) return;
+  f32x16 acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; i++)
+#pragma unroll
+    for (int j = 0; j < 2; j++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) acc[i][j][r] = 0.f;
+  ksplit::run<S, S, false, P == STEP, true>((const char*)g.a, (const char*)g.b, g.lda, g.ldb, g.K, ring, acc, wave, lane);
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  char* strip = ring + wave * STRIP;
+#pragma unroll
+  for (int tr = 0; tr < 2; tr++)
+#pragma unroll
+    for (int tn = 0; tn < 2; tn++)
+#pragma unroll
+      for (int q = 0; q < 4; q++) {
+        const f32x16& a = acc[tr][tn];
+        *(f32x4*)(strip + (tr * 32 + (lane & 31)) * ROWB + (tn * 32 + 8 * q + 4 * (lane >> 5)) * 4) = f32x4{a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
+      }
+  __syncthreads();
+  // a wave writes 16 of the rows, the four partial sums added up in the order of the k shares
+#pragma unroll
+  for (int it = 0; it < 2; it++) {
+    const int row = wave * 16 + it * 8 + lane / 8, cp = lane % 8;
+    const char* q = ring + row * ROWB + cp * 32;
+    f32x4 v0 = *(const f32x4*)q, v1 = *(const f32x4*)(q + 16);
+#pragma unroll
+    for (int w = 1; w < 4; w++) { v0 += *(const f32x4*)(q + w * STRIP); v1 += *(const f32x4*)(q + w * STRIP + 16); }
+    const float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+    put8<P>(e, from, g.m0 + row, g.n0 + cp * 8, v);
+  }
+  if constexpr (P != STEP) {
+    if (g.ti != g.tj) {
+#pragma unroll
+      for (int r = 0; r < 2; r++) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+          const char* q = ring + (wave * 16 + r * 8 + j) * ROWB + lane * 4;
+          v[j] = *(const float*)q;
+#pragma unroll
+          for (int w = 1; w < 4; w++) v[j] += *(const float*)(q + w * STRIP);
+        }
+        put8<P>(e, from, g.n0 + lane, g.m0 + wave * 16 + r * 8, v);
+      }
+    }
   }
 }
 
@@ -345,11 +514,32 @@ struct Group {
 int64_t small_side(const ah_muon_matrix_t& x) { return std::min(x.rows, x.cols); }
 int64_t large_side(const ah_muon_matrix_t& x) { return std::max(x.rows, x.cols); }
 
-// 256 x 256 tiles where they are as many as two thirds of the CUs, else 128 x 128
+// The tile that a group's products are expected to be fastest with, from what its rounds of blocks take (us, K in thousands; times that the tiles share, such as that of
+// the results' bytes, left out).  Measured (one box, us a step, tiles of 64, 128, 256): one 1024 x 1024 167, 236, 533; one 1024 x 4096 276, 335, 782; one 2048 x 2048 474, 375,
+// 825; 7 of 1024 x 2048 815, 678, 840; 24 of 1024 x 1024 1470, 1199, 1503; 4 of 2048 x 2048 1563, 1136, 1124; one 4096 x 4096 2792, 1793, 1654; one 4096 x 11008 6344, 4146, 3688.
 int tile_of(const ah_muon_matrix_t* x, const std::vector<int>& which) {
-  uint64_t tiles = 0;
-  for (int i : which) tiles += (up(small_side(x[i]), 256) / 256) * (up(large_side(x[i]), 256) / 256);
-  return tiles >= 170 ? 256 : 128;
+  struct { int tile; double alone0, alone1, full0, full1; } kinds[] = {{64, 4.5, 4.0, 0.4, 4.2}, {128, 4.5, 7.8, 3.5, 8.1}, {256, 6.0, 22.0, 6.0, 22.0}};
+  int best = 64;
+  double least = 0;
+  for (const auto& k : kinds) {
+    double total = 0;
+    for (Product p : {SYM_A, SYM_B, STEP}) {
+      double sum = 0, longest = 0;               // of all blocks, of one that has its CU to itself
+      uint64_t tiles = 0;
+      for (int i : which) {
+        const uint64_t n = up(small_side(x[i]), std::max(k.tile, 128)), m = up(large_side(x[i]), std::max(k.tile, 128));
+        const uint64_t rows = n / k.tile, count = p == STEP ? rows * (m / k.tile) : rows * (rows + 1) / 2;
+        const double K = (p == SYM_A ? m : n) * 1e-3;
+        sum += count * (k.full0 + k.full1 * K);
+        longest = std::max(longest, k.alone0 + k.alone1 * K);
+        tiles += count;
+      }
+      // (a block of 256 x 256 has its CU to itself: whole rounds)
+      total += std::max(longest, k.tile == 256 ? sum / tiles * ((tiles + 255) / 256) : sum / 256);
+    }
+    if (least == 0 || total < least) { least = total; best = k.tile; }
+  }
+  return best;
 }
 
 struct Offsets { uint64_t hi0, hi1, lo, A, B, part, inv, end; };
@@ -385,8 +575,8 @@ std::vector<Group> plan(const ah_muon_matrix_t* x, int n) {
     g.tile = tile_of(x, g.which);
     g.bytes = 0;
     for (int i : g.which) {
-      g.n.push_back((int)up(small_side(x[i]), g.tile));
-      g.k.push_back((int)up(large_side(x[i]), g.tile));
+      g.n.push_back((int)up(small_side(x[i]), std::max(g.tile, 128)));       // (the products' k axis: a multiple of 128)
+      g.k.push_back((int)up(large_side(x[i]), std::max(g.tile, 128)));
       g.bytes = offsets(x[i], g.n.back(), g.k.back(), g.bytes).end;
     }
   }
@@ -417,14 +607,24 @@ hipError_t launch(Table& t, const Group& g, const F& blocks_of, const G& go) {
   return hipGetLastError();
 }
 
-template <int S, int DEPTH>
+template <int S>
 hipError_t products(Table& t, const Group& g, int steps, hipStream_t s) {
   auto triangle = [](const Matrix& e) { const uint64_t n = e.n / S; return up(n * (n + 1) / 2, 8); };
   auto all = [](const Matrix& e) { return up((uint64_t)(e.n / S) * (e.k / S), 8); };
+  auto product = [&](auto p, const auto& blocks_of, int from) {
+    constexpr Product P = decltype(p)::value;
+    return launch(t, g, blocks_of, [&](uint32_t b) {
+      auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(b), dim3(NT), 0, s, t, from); };
+      if constexpr (S == 64) go(small_product_kernel<P>);
+      else if constexpr (S == 256) go(product_kernel<S, P, 2>);
+      else if (b <= 256) go(product_kernel<S, P, 3>);
+      else go(product_kernel<S, P, 2>);
+    });
+  };
   for (int i = 0; i < steps; i++) {
-    hipError_t e = launch(t, g, triangle, [&](uint32_t b) { hipLaunchKernelGGL((product_kernel<S, SYM_A, DEPTH>), dim3(b), dim3(NT), 0, s, t, i & 1); });
-    if (e == hipSuccess) e = launch(t, g, triangle, [&](uint32_t b) { hipLaunchKernelGGL((product_kernel<S, SYM_B, DEPTH>), dim3(b), dim3(NT), 0, s, t, i & 1); });
-    if (e == hipSuccess) e = launch(t, g, all, [&](uint32_t b) { hipLaunchKernelGGL((product_kernel<S, STEP, DEPTH>), dim3(b), dim3(NT), 0, s, t, i & 1); });
+    hipError_t e = product(std::integral_constant<Product, SYM_A>(), triangle, i & 1);
+    if (e == hipSuccess) e = product(std::integral_constant<Product, SYM_B>(), triangle, i & 1);
+    if (e == hipSuccess) e = product(std::integral_constant<Product, STEP>(), all, i & 1);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
@@ -444,6 +644,8 @@ hipError_t step_group(const ah_muon_t* c, const ah_muon_matrix_t* x, const Group
     e.ld_m = y.ld_momentum ? y.ld_momentum : y.cols; e.ld_master = y.ld_master ? y.ld_master : y.cols;
     e.rows = (int)y.rows; e.cols = (int)y.cols; e.n = g.n[i]; e.k = g.k[i];
     e.wd = y.weight_decay; e.scale = y.scale;
+    const int pb = c->param_type == AH_FP32 ? 4 : 2, gb = c->grad_type == AH_FP32 ? 4 : 2;
+    e.aligned = ((e.ld_p | e.ld_g | e.ld_m | e.ld_master) & 3) == 0 && aligned_to(e.p, 4 * pb) && aligned_to(e.g, 4 * gb) && aligned_to(e.m, 16) && aligned_to(e.master, 16);
     at = o.end;
   }
   Hyper h = {};
@@ -462,7 +664,7 @@ hipError_t step_group(const ah_muon_t* c, const ah_muon_matrix_t* x, const Group
       if (g32) hipLaunchKernelGGL(lay_out_kernel<float>, dim3(b), dim3(NT), 0, s, t, h);
       else hipLaunchKernelGGL(lay_out_kernel<bf16>, dim3(b), dim3(NT), 0, s, t, h);
     });
-  if (e == hipSuccess) e = g.tile == 256 ? products<256, 2>(t, g, c->ns_steps, s) : products<128, 2>(t, g, c->ns_steps, s);
+  if (e == hipSuccess) e = g.tile == 256 ? products<256>(t, g, c->ns_steps, s) : g.tile == 128 ? products<128>(t, g, c->ns_steps, s) : products<64>(t, g, c->ns_steps, s);
   if (e == hipSuccess)
     e = launch(t, g, pieces, [&](uint32_t b) {
       const int last = c->ns_steps & 1;
