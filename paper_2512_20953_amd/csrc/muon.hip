@@ -341,34 +341,39 @@ __device__ __forceinline__ bool find_job(const Matrix& e, uint32_t block, int fr
   return true;
 }
 
-// 8 elements of a result from (row, col) on, whose sums are v
+// What 8 elements of a result from (row, col) on need beside their sums: of X the two halves, of B those of A.  Asked for ahead: the compiler would not move these loads
+// over the stores of the elements before.
+template <Product P> struct Beside { f16x8 hi, lo; };
 template <Product P>
-__device__ __forceinline__ void put8(const Matrix& e, int from, int row, int col, const float (&v)[8]) {
+__device__ __forceinline__ Beside<P> ask8(const Matrix& e, int from, int row, int col) {
+  Beside<P> x = {};
   if constexpr (P == STEP) {
-    const size_t at = (size_t)row * e.k + col;
-    const f16x8 xh = *(const f16x8*)(e.hi[from] + at), xl = *(const f16x8*)(e.lo + at);
-    f16x8 oh, ol;
+    x.hi = *(const f16x8*)(e.hi[from] + (size_t)row * e.k + col);
+    x.lo = *(const f16x8*)(e.lo + (size_t)row * e.k + col);
+  } else if constexpr (P == SYM_B) {
+    x.hi = *(const f16x8*)(e.A + (size_t)row * e.n + col);
+  }
+  return x;
+}
+// ... and those elements, whose sums are v
+template <Product P>
+__device__ __forceinline__ void put8(const Matrix& e, int from, int row, int col, const float (&v)[8], const Beside<P>& x) {
+  f16x8 o;
+  if constexpr (P == STEP) {
+    f16x8 ol;
 #pragma unroll
     for (int j = 0; j < 8; j++) {
       f16 hi, lo;
-      split(__builtin_fmaf(kA_, (float)xh[j] + (float)xl[j] * (1.f / kLo), v[j] * (1.f / kA)), hi, lo);
-      oh[j] = hi;
+      split(__builtin_fmaf(kA_, (float)x.hi[j] + (float)x.lo[j] * (1.f / kLo), v[j] * (1.f / kA)), hi, lo);
+      o[j] = hi;
       ol[j] = lo;
     }
-    *(f16x8*)(e.hi[from ^ 1] + at) = oh;
-    *(f16x8*)(e.lo + at) = ol;
+    *(f16x8*)(e.hi[from ^ 1] + (size_t)row * e.k + col) = o;
+    *(f16x8*)(e.lo + (size_t)row * e.k + col) = ol;
   } else {
-    const size_t at = (size_t)row * e.n + col;
-    f16x8 o;
-    if constexpr (P == SYM_A) {
 #pragma unroll
-      for (int j = 0; j < 8; j++) o[j] = (f16)(v[j] * (kA / (kX * kX)));
-    } else {
-      const f16x8 x = *(const f16x8*)(e.A + at);   // (A is symmetric bit for bit)
-#pragma unroll
-      for (int j = 0; j < 8; j++) o[j] = (f16)__builtin_fmaf(kB_, (float)x[j], v[j] * (kC_ / kA));
-    }
-    *(f16x8*)((P == SYM_A ? e.A : e.B) + at) = o;
+    for (int j = 0; j < 8; j++) o[j] = P == SYM_A ? (f16)(v[j] * (kA / (kX * kX))) : (f16)__builtin_fmaf(kB_, (float)x.hi[j], v[j] * (kC_ / kA));
+    *(f16x8*)((P == SYM_A ? e.A : e.B) + (size_t)row * e.n + col) = o;
   }
 }
 
@@ -403,9 +408,24 @@ __global__ __launch_bounds__(NT) void product_kernel(Table t, int from) {
   __syncthreads();
   char* strip = ring + wave * (32 * ROWB);
   const int cp = lane % PPR, row0 = lane / PPR, n0 = g.n0 + wn * W;
+  Beside<P> x[2][NIT], xt[W / 64][4];
+  auto ask = [&](int tm) {
+#pragma unroll
+    for (int it = 0; it < NIT; it++) x[tm & 1][it] = ask8<P>(e, from, g.m0 + wm * W + tm * 32 + row0 + it * RPI, n0 + cp * 8);
+  };
+  ask(0);
 #pragma unroll
   for (int tm = 0; tm < W / 32; tm++) {
     const int mbase = g.m0 + wm * W + tm * 32;
+    if (tm + 1 < W / 32) ask(tm + 1);
+    if constexpr (P == SYM_B) {                    // (A is symmetric bit for bit: the same elements across the diagonal)
+      if (g.ti != g.tj) {
+#pragma unroll
+        for (int half = 0; half < W / 64; half++)
+#pragma unroll
+          for (int r = 0; r < 4; r++) xt[half][r] = ask8<P>(e, from, n0 + half * 64 + lane, mbase + r * 8);
+      }
+    }
 #pragma unroll
     for (int tr = 0; tr < 2; tr++)
 #pragma unroll
@@ -418,7 +438,7 @@ __global__ __launch_bounds__(NT) void product_kernel(Table t, int from) {
       const char* q = strip + row * ROWB + cp * 32;
       const f32x4 v0 = *(const f32x4*)q, v1 = *(const f32x4*)(q + 16);
       const float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-      put8<P>(e, from, mbase + row, n0 + cp * 8, v);
+      put8<P>(e, from, mbase + row, n0 + cp * 8, v, x[tm & 1][it]);
     }
     if constexpr (P != STEP) {
       if (g.ti != g.tj) {                          // the tile across the diagonal: 8 rows of a column a lane
@@ -430,7 +450,7 @@ __global__ __launch_bounds__(NT) void product_kernel(Table t, int from) {
             float v[8];
 #pragma unroll
             for (int j = 0; j < 8; j++) v[j] = *(const float*)(strip + (r * 8 + j) * ROWB + c * 4);
-            put8<P>(e, from, n0 + c, mbase + r * 8, v);
+            put8<P>(e, from, n0 + c, mbase + r * 8, v, xt[half][r]);
           }
       }
     }
@@ -460,6 +480,17 @@ __global__ __launch_bounds__(NT) void small_product_kernel(Table t, int from) {
       for (int r = 0; r < 16; r++) acc[i][j][r] = 0.f;
   ksplit::run<S, S, false, P == STEP, true>((const char*)g.a, (const char*)g.b, g.lda, g.ldb, g.K, ring, acc, wave, lane);
   __builtin_amdgcn_s_waitcnt(0);
+  // a wave writes 16 of the rows, and as many columns across the diagonal
+  const int row0 = wave * 16 + lane / 8, cp = lane % 8;
+  Beside<P> x[2], xt[2] = {};
+#pragma unroll
+  for (int it = 0; it < 2; it++) x[it] = ask8<P>(e, from, g.m0 + row0 + it * 8, g.n0 + cp * 8);
+  if constexpr (P == SYM_B) {
+    if (g.ti != g.tj) {
+#pragma unroll
+      for (int r = 0; r < 2; r++) xt[r] = ask8<P>(e, from, g.n0 + lane, g.m0 + wave * 16 + r * 8);
+    }
+  }
   __syncthreads();
   char* strip = ring + wave * STRIP;
 #pragma unroll
@@ -472,16 +503,16 @@ __global__ __launch_bounds__(NT) void small_product_kernel(Table t, int from) {
         *(f32x4*)(strip + (tr * 32 + (lane & 31)) * ROWB + (tn * 32 + 8 * q + 4 * (lane >> 5)) * 4) = f32x4{a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
       }
   __syncthreads();
-  // a wave writes 16 of the rows, the four partial sums added up in the order of the k shares
+  // the four partial sums are added up in the order of the k shares
 #pragma unroll
   for (int it = 0; it < 2; it++) {
-    const int row = wave * 16 + it * 8 + lane / 8, cp = lane % 8;
+    const int row = row0 + it * 8;
     const char* q = ring + row * ROWB + cp * 32;
     f32x4 v0 = *(const f32x4*)q, v1 = *(const f32x4*)(q + 16);
 #pragma unroll
     for (int w = 1; w < 4; w++) { v0 += *(const f32x4*)(q + w * STRIP); v1 += *(const f32x4*)(q + w * STRIP + 16); }
     const float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-    put8<P>(e, from, g.m0 + row, g.n0 + cp * 8, v);
+    put8<P>(e, from, g.m0 + row, g.n0 + cp * 8, v, x[it]);
   }
   if constexpr (P != STEP) {
     if (g.ti != g.tj) {
@@ -495,7 +526,7 @@ __global__ __launch_bounds__(NT) void small_product_kernel(Table t, int from) {
 #pragma unroll
           for (int w = 1; w < 4; w++) v[j] += *(const float*)(q + w * STRIP);
         }
-        put8<P>(e, from, g.n0 + lane, g.m0 + wave * 16 + r * 8, v);
+        put8<P>(e, from, g.n0 + lane, g.m0 + wave * 16 + r * 8, v, xt[r]);
       }
     }
   }
