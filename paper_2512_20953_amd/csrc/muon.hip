@@ -52,7 +52,6 @@ struct Table {
   uint32_t first[kTable];      // the block at which a matrix begins; behind the last: UINT32_MAX
   Matrix e[kTable];
 };
-static_assert(sizeof(Table) <= 3900, "a kernel's arguments");
 
 struct Hyper {
   float rest, lr;              // rest: 1 - momentum
@@ -305,11 +304,30 @@ __global__ __launch_bounds__(NT) void apply_kernel(Table t, Hyper h, int last) {
 // ---- the products.  S x S tiles, four waves of S / 2 x S / 2.  SYM_A: A = X X^T; SYM_B: B = b A + c A A^T; STEP: X = a X + B X.
 enum Product { SYM_A, SYM_B, STEP };
 
-// Blocks are dealt to the 8 XCDs round-robin.  Each XCD gets every eighth of the blocks of each matrix (which has a multiple of 8 of them) and of its tiles a row of consecutive ones, so
-// that all XCDs have as many of every matrix, the largest first: -1 where there is none left.
-__device__ __forceinline__ int xcd_tile(uint32_t block, int tiles) {
-  const int xcd = block & 7, at = block >> 3, most = tiles >> 3, more = tiles & 7;
-  return at < most + (xcd < more) ? xcd * most + min(xcd, more) + at : -1;
+// Blocks are dealt to the 8 XCDs round-robin, and each XCD has an L2 of its own: a matrix is given to `span` XCDs from `first` on, and each of those a row of consecutive tiles of it.
+struct Deal {
+  uint32_t tiles[kTable];
+  uint8_t first[kTable], span[kTable];
+  int n;
+};
+
+static_assert(sizeof(Table) + sizeof(Deal) <= 4000, "a kernel's arguments");
+
+// The matrix and the tile of a block (-1: none left for its XCD)
+__device__ __forceinline__ int dealt(const Deal& d, uint32_t block, int& tile) {
+  const uint32_t xcd = block & 7;
+  uint32_t at = block >> 3;
+  for (int i = 0; i < d.n; i++) {
+    const uint32_t share = xcd - d.first[i], span = d.span[i];
+    if (share >= span) continue;
+    const uint32_t most = d.tiles[i] / span, more = d.tiles[i] % span, count = most + (share < more);
+    if (at < count) {
+      tile = (int)(share * most + min(share, more) + at);
+      return i;
+    }
+    at -= count;
+  }
+  return -1;
 }
 
 // Which tile a block computes, and its operands
@@ -318,9 +336,7 @@ struct Job {
   const f16 *a, *b;
 };
 template <int S, Product P>
-__device__ __forceinline__ bool find_job(const Matrix& e, uint32_t block, int from, Job& j) {
-  const int tile = xcd_tile(block, P == STEP ? (e.n / S) * (e.k / S) : (e.n / S) * (e.n / S + 1) / 2);
-  if (tile < 0) return false;
+__device__ __forceinline__ void find_job(const Matrix& e, int tile, int from, Job& j) {
   if constexpr (P == STEP) {                       // down groups of 4 tile rows
     const int tm = e.n / S, tn = e.k / S, group = tile / (4 * tn), rows = min(tm - 4 * group, 4), in = tile - group * 4 * tn;
     j.ti = group * 4 + in % rows;
@@ -338,7 +354,6 @@ __device__ __forceinline__ bool find_job(const Matrix& e, uint32_t block, int fr
   if constexpr (P == SYM_A) { j.lda = j.ldb = j.K = e.k; j.a = X + (size_t)j.m0 * e.k; j.b = X + (size_t)j.n0 * e.k; }
   else if constexpr (P == SYM_B) { j.lda = j.ldb = j.K = e.n; j.a = e.A + (size_t)j.m0 * e.n; j.b = e.A + (size_t)j.n0 * e.n; }
   else { j.lda = j.K = e.n; j.ldb = e.k; j.a = e.B + (size_t)j.m0 * e.n; j.b = X + j.n0; }
-  return true;
 }
 
 // What 8 elements of a result from (row, col) on need beside their sums: of X the two halves, of B those of A.  Asked for ahead: the compiler would not move these loads
@@ -378,16 +393,18 @@ __device__ __forceinline__ void put8(const Matrix& e, int from, int row, int col
 }
 
 template <int S, Product P, int DEPTH>
-__global__ __launch_bounds__(NT) void product_kernel(Table t, int from) {
+__global__ __launch_bounds__(NT) void product_kernel(Table t, Deal d, int from) {
   constexpr int W = S / 2, TB = W / 16;
   constexpr bool BKS = P == STEP;                  // X is [k, columns] there
   constexpr int RING = k64::ring_bytes<S, S, DEPTH, true>();
   __shared__ __attribute__((aligned(1024))) char ring[RING];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / 2, wn = wave % 2;
-  const int which = __builtin_amdgcn_readfirstlane(find(t, blockIdx.x));
+  int tile = 0;
+  const int which = __builtin_amdgcn_readfirstlane(dealt(d, blockIdx.x, tile));
+  if (which < 0) return;
   const Matrix& e = t.e[which];
   Job g;
-  if (!find_job<S, P>(e, blockIdx.x - t.first[which], from, g)) return;
+  find_job<S, P>(e, tile, from, g);
   f32x4 acc[TB][TB];
 #pragma unroll
   for (int i = 0; i < TB; i++)
@@ -461,16 +478,18 @@ __global__ __launch_bounds__(NT) void product_kernel(Table t, int from) {
 
 // The same for few tiles: 64 x 64, each wave one k-step in four of the whole tile.  Four times the blocks, whose chains of k-steps are a quarter as long.
 template <Product P>
-__global__ __launch_bounds__(NT) void small_product_kernel(Table t, int from) {
+__global__ __launch_bounds__(NT) void small_product_kernel(Table t, Deal d, int from) {
   constexpr int S = 64, ROWB = S * 4 + 16, STRIP = S * ROWB;
   constexpr int RING = ksplit::stages<S, S>() * ksplit::stage_bytes<S, S>();
   static_assert(4 * STRIP <= RING, "the partial sums fit in the ring");
   __shared__ __attribute__((aligned(1024))) char ring[RING];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int which = __builtin_amdgcn_readfirstlane(find(t, blockIdx.x));
+  int tile = 0;
+  const int which = __builtin_amdgcn_readfirstlane(dealt(d, blockIdx.x, tile));
+  if (which < 0) return;
   const Matrix& e = t.e[which];
   Job g;
-  if (!find_job<S, P>(e, blockIdx.x - t.first[which], from, g)) return;
+  find_job<S, P>(e, tile, from, g);
   f32x16 acc[2][2];
 #pragma unroll
   for (int i = 0; i < 2; i++)
@@ -545,22 +564,28 @@ struct Group {
 int64_t small_side(const ah_muon_matrix_t& x) { return std::min(x.rows, x.cols); }
 int64_t large_side(const ah_muon_matrix_t& x) { return std::max(x.rows, x.cols); }
 
-// The tile that a group's products are expected to be fastest with, from what its rounds of blocks take (us, K in thousands; times that the tiles share, such as that of
-// the results' bytes, left out).  Measured (one box, us a step, tiles of 64, 128, 256): one 1024 x 1024 167, 236, 533; one 1024 x 4096 276, 335, 782; one 2048 x 2048 474, 375,
+// What the products' blocks take, us, K in thousands (times that the tiles share, such as that of the results' bytes, left out): one that has its CU to itself, and its share of
+// a CU that is full.  Measured (one box, us a step, tiles of 64, 128, 256): one 1024 x 1024 167, 236, 533; one 1024 x 4096 276, 335, 782; one 2048 x 2048 474, 375,
 // 825; 7 of 1024 x 2048 815, 678, 840; 24 of 1024 x 1024 1470, 1199, 1503; 4 of 2048 x 2048 1563, 1136, 1124; one 4096 x 4096 2792, 1793, 1654; one 4096 x 11008 6344, 4146, 3688.
+struct Kind { int tile; double alone0, alone1, full0, full1; };
+constexpr Kind kKinds[] = {{64, 4.5, 4.0, 0.4, 4.2}, {128, 4.5, 7.8, 3.5, 8.1}, {256, 6.0, 22.0, 6.0, 22.0}};
+
+// Tiles of a product of an n x m matrix (padded), and its K
+uint64_t tiles_of(Product p, uint64_t n, uint64_t m, int tile) { return p == STEP ? (n / tile) * (m / tile) : (n / tile) * (n / tile + 1) / 2; }
+double depth_of(Product p, uint64_t n, uint64_t m) { return (p == SYM_A ? m : n) * 1e-3; }
+
+// The tile that a group's products are expected to be fastest with
 int tile_of(const ah_muon_matrix_t* x, const std::vector<int>& which) {
-  struct { int tile; double alone0, alone1, full0, full1; } kinds[] = {{64, 4.5, 4.0, 0.4, 4.2}, {128, 4.5, 7.8, 3.5, 8.1}, {256, 6.0, 22.0, 6.0, 22.0}};
   int best = 64;
   double least = 0;
-  for (const auto& k : kinds) {
+  for (const Kind& k : kKinds) {
     double total = 0;
     for (Product p : {SYM_A, SYM_B, STEP}) {
-      double sum = 0, longest = 0;               // of all blocks, of one that has its CU to itself
+      double sum = 0, longest = 0;
       uint64_t tiles = 0;
       for (int i : which) {
-        const uint64_t n = up(small_side(x[i]), std::max(k.tile, 128)), m = up(large_side(x[i]), std::max(k.tile, 128));
-        const uint64_t rows = n / k.tile, count = p == STEP ? rows * (m / k.tile) : rows * (rows + 1) / 2;
-        const double K = (p == SYM_A ? m : n) * 1e-3;
+        const uint64_t n = up(small_side(x[i]), std::max(k.tile, 128)), m = up(large_side(x[i]), std::max(k.tile, 128)), count = tiles_of(p, n, m, k.tile);
+        const double K = depth_of(p, n, m);
         sum += count * (k.full0 + k.full1 * K);
         longest = std::max(longest, k.alone0 + k.alone1 * K);
         tiles += count;
@@ -571,6 +596,44 @@ int tile_of(const ah_muon_matrix_t* x, const std::vector<int>& which) {
     if (least == 0 || total < least) { least = total; best = k.tile; }
   }
   return best;
+}
+
+// Deals a product's tiles to the XCDs.  Tiles of 64 and 128, which are bound by how fast their operands arrive: each matrix to as few XCDs as have it in their L2s (4 MB each) and
+// take at most a tenth and 1.5 us longer for it than all together would, in the table's order (the largest first) to those that have least.  (One box, us a step, every matrix to 1, 2, 4
+// and 8 XCDs: the smallest stage's 12 matrices 130, 140, 148, 153; 12 of 768 x about 2000 609, 571, 579, 617.)  Tiles of 256 to all of them: evenly (a LLaMA-style layer, 1 to 8 XCDs
+// a matrix: 21900, 16500, 15300, 14640).  Returns the launch's blocks.
+uint32_t deal(Product p, const Table& t, int n, const Kind& kind, Deal& d) {
+  uint32_t most = 0;
+  for (int span = kind.tile < 256 ? 1 : 8; span <= 8; span *= 2) {
+    bool fits = true;
+    for (int i = 0; i < n; i++) fits = fits && 2ull * t.e[i].n * t.e[i].k <= (4ull << 20) * span;
+    if (!fits && span < 8) continue;
+    double load[8] = {}, sum = 0, top = 0;
+    uint64_t count[8] = {};
+    for (int i = 0; i < n; i++) {
+      const uint64_t tiles = tiles_of(p, t.e[i].n, t.e[i].k, kind.tile);
+      const double cost = tiles * (kind.full0 + kind.full1 * depth_of(p, t.e[i].n, t.e[i].k));
+      int at = 0;
+      for (int x = span; x < 8; x += span)
+        if (load[x] < load[at]) at = x;
+      d.tiles[i] = (uint32_t)tiles;
+      d.first[i] = (uint8_t)at;
+      d.span[i] = (uint8_t)span;
+      for (int x = 0; x < span; x++) {
+        load[at + x] += cost / span;
+        count[at + x] += tiles / span + ((uint64_t)x < tiles % span);
+      }
+      sum += cost;
+    }
+    d.n = n;
+    most = 0;
+    for (int x = 0; x < 8; x++) {
+      top = std::max(top, load[x]);
+      most = std::max(most, (uint32_t)count[x]);
+    }
+    if (top / 32 <= 1.1 * sum / 256 + 1.5) break;       // (32 CUs to an XCD)
+  }
+  return most * 8;
 }
 
 struct Offsets { uint64_t hi0, hi1, lo, A, B, part, inv, end; };
@@ -639,23 +702,27 @@ hipError_t launch(Table& t, const Group& g, const F& blocks_of, const G& go) {
 }
 
 template <int S>
-hipError_t products(Table& t, const Group& g, int steps, hipStream_t s) {
-  auto triangle = [](const Matrix& e) { const uint64_t n = e.n / S; return up(n * (n + 1) / 2, 8); };
-  auto all = [](const Matrix& e) { return up((uint64_t)(e.n / S) * (e.k / S), 8); };
-  auto product = [&](auto p, const auto& blocks_of, int from) {
-    constexpr Product P = decltype(p)::value;
-    return launch(t, g, blocks_of, [&](uint32_t b) {
-      auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(b), dim3(NT), 0, s, t, from); };
-      if constexpr (S == 64) go(small_product_kernel<P>);
-      else if constexpr (S == 256) go(product_kernel<S, P, 2>);
-      else if (b <= 256) go(product_kernel<S, P, 3>);
-      else go(product_kernel<S, P, 2>);
-    });
+hipError_t products(const Table& t, const Group& g, int steps, hipStream_t s) {
+  const Kind& kind = S == 64 ? kKinds[0] : S == 128 ? kKinds[1] : kKinds[2];
+  Deal deals[3];
+  uint32_t blocks[3];
+  for (Product p : {SYM_A, SYM_B, STEP}) {
+    blocks[p] = deal(p, t, (int)g.which.size(), kind, deals[p]);
+    if (blocks[p] > (1u << 23)) return hipErrorInvalidValue;
+  }
+  auto product = [&](auto kind_of, int from) {
+    constexpr Product P = decltype(kind_of)::value;
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(blocks[P]), dim3(NT), 0, s, t, deals[P], from); };
+    if constexpr (S == 64) go(small_product_kernel<P>);
+    else if constexpr (S == 256) go(product_kernel<S, P, 2>);
+    else if (blocks[P] <= 256) go(product_kernel<S, P, 3>);
+    else go(product_kernel<S, P, 2>);
+    return hipGetLastError();
   };
   for (int i = 0; i < steps; i++) {
-    hipError_t e = product(std::integral_constant<Product, SYM_A>(), triangle, i & 1);
-    if (e == hipSuccess) e = product(std::integral_constant<Product, SYM_B>(), triangle, i & 1);
-    if (e == hipSuccess) e = product(std::integral_constant<Product, STEP>(), all, i & 1);
+    hipError_t e = product(std::integral_constant<Product, SYM_A>(), i & 1);
+    if (e == hipSuccess) e = product(std::integral_constant<Product, SYM_B>(), i & 1);
+    if (e == hipSuccess) e = product(std::integral_constant<Product, STEP>(), i & 1);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
