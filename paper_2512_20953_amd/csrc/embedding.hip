@@ -17,8 +17,8 @@ using namespace ah;
 namespace {
 
 constexpr int NT = 256, NW = NT / 64, kMaxRows = 1 << 25, kMaxVocab = 1 << 30, kMaxWidth = 65536;
-constexpr int kFlight = 2;                             // pieces of a row that a lane has in flight
-constexpr int kMaxChunks = 2048, kMinChunk = 16, kAhead = 8, kJoin = 8;
+constexpr int kFlight = 2;                             // forward: pieces of a row that a lane has in flight
+constexpr int kMaxChunks = 2048, kMinChunk = 16, kAhead = 8, kJoin = 16;
 constexpr int kRowThreads = 1024;
 constexpr int kSmall = 16384;                          // tokens up to which places are counted (rank_kernel)
 constexpr int kFillBlocks = 1024;                      // beside that
@@ -33,7 +33,7 @@ struct FwdArgs {
   float scale;
 };
 
-// 2^LANES lanes to a row, V elements each and time
+// 2^lanes_log2 lanes to a row, V elements each and time, kFlight times in flight (with two rows at once level: 8192 x 4096 with positions 28 us)
 template <class TT, class AT, int V>
 __global__ __launch_bounds__(NT) void embedding_fwd_kernel(FwdArgs a, int lanes_log2) {
   const int lanes = 1 << lanes_log2, lane = threadIdx.x & (lanes - 1), rows = NT >> lanes_log2;
@@ -211,8 +211,14 @@ __global__ __launch_bounds__(kRankThreads) void rank_kernel(SortArgs a, int rank
   __shared__ uint32_t keys[kSmall], count[kRankWaves][kRanked];
   if ((int)blockIdx.x >= rank_blocks) return fill_rows(f, blockIdx.x - rank_blocks, gridDim.x - rank_blocks, kRankThreads);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = blockIdx.x * kRanked;
-#pragma unroll 8
-  for (int t = threadIdx.x; t < (a.T + 63) / 64 * 64; t += kRankThreads) keys[t] = t < a.T ? key_of<BITS>(a.tokens, t, a.vocab) : kNone;
+  constexpr int FLIGHT = 8;                  // keys of a lane in flight
+  for (int t0 = threadIdx.x; t0 - (int)threadIdx.x < a.T; t0 += FLIGHT * kRankThreads) {
+    uint32_t k[FLIGHT];
+#pragma unroll
+    for (int j = 0; j < FLIGHT; j++) k[j] = key_of<BITS>(a.tokens, min(t0 + j * kRankThreads, a.T - 1), a.vocab);
+#pragma unroll
+    for (int j = 0; j < FLIGHT; j++) keys[t0 + j * kRankThreads] = t0 + j * kRankThreads < a.T ? k[j] : kNone;
+  }
   __syncthreads();
   uint32_t key[kRanked], n[kRanked];
 #pragma unroll
@@ -317,34 +323,38 @@ __global__ __launch_bounds__(kRowThreads) void embedding_bwd_kernel(BwdArgs a) {
 
 // The chunk in which a sum begins that goes on behind it adds up what the following ones left of it.
 template <int V>
-__global__ __launch_bounds__(kRowThreads) void embedding_join_kernel(BwdArgs a, int chunks) {
+__global__ __launch_bounds__(NT) void embedding_join_kernel(BwdArgs a, int chunks) {
   const int first = blockIdx.x * a.chunk, end = first + a.chunk;
   if (end >= a.T) return;
   const uint32_t k = a.key[end - 1];
   if (k >= (uint32_t)a.vocab || a.key[end] != k) return;
   if (a.key[first] == k && first > 0 && a.key[first - 1] == k) return;      // it began earlier
-  const int c = (blockIdx.y * blockDim.x + threadIdx.x) * V;
-  if (c >= a.width) return;
+  const int at = (blockIdx.y * NT + threadIdx.x) * V, c = at < a.width ? at : 0;      // (lanes behind the last column keep its company: the ballots below are whole waves')
   const float* p = a.part + (size_t)blockIdx.x * 2 * a.width + c;
   const wide_t<float, V> old = old_row<V>(a, k, c);
   wide_t<float, V> s = load_wide<V>(p + a.width);
-  int b = blockIdx.x + 1;
-  for (bool more = true; more; b += kJoin) {
+  // the chunks behind this one that begin with the same token: all of their entries, or the last of its
+  int behind = 0;
+  for (int b = blockIdx.x + 1 + (threadIdx.x & 63);; b += 64) {
+    const uint64_t same = __ballot(b < chunks && a.key[(size_t)min(b, chunks - 1) * a.chunk] == k);
+    behind += ~same ? __builtin_ctzll(~same) : 64;
+    if (~same) break;
+  }
+  p += 2 * (size_t)a.width;
+  for (int b = 0; b < behind; b += kJoin) {
     wide_t<float, V> r[kJoin];
 #pragma unroll
-    for (int i = 0; i < kJoin; i++) {
-      more = more && b + i < chunks && a.key[(size_t)(b + i) * a.chunk] == k;
-      r[i] = wide_t<float, V>{};
-      if (more) r[i] = load_wide<V>(p + (size_t)(b + i - blockIdx.x) * 2 * a.width);
-    }
+    for (int i = 0; i < kJoin; i++) r[i] = load_wide<V>(p + (size_t)min(b + i, behind - 1) * 2 * a.width);
 #pragma unroll
-    for (int i = 0; i < kJoin; i++) s += r[i];
+    for (int i = 0; i < kJoin; i++)
+      if (b + i < behind) s += r[i];
   }
-  put<V>(a, k, c, s, old);
+  if (at < a.width) put<V>(a, k, c, s, old);
 }
 
 int sort_blocks(int T) { return (T + kSortBlock - 1) / kSortBlock; }
-int chunk_of(int T) { return std::max(kMinChunk, (T + kMaxChunks - 1) / kMaxChunks); }
+// (few tokens: shorter chunks, or their blocks would leave CUs idle)
+int chunk_of(int T) { return std::max(T <= 4096 ? kMinChunk / 2 : kMinChunk, (T + kMaxChunks - 1) / kMaxChunks); }
 uint64_t up256(uint64_t n) { return (n + 255) / 256 * 256; }
 
 // Places in the workspace
@@ -492,7 +502,9 @@ extern "C" int ah_embedding_bwd(const ah_embedding_t* c, const void* tokens, con
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(lanes), 0, s, a); };
   if (ab == 4) { if (wide) go(embedding_bwd_kernel<float, 4>); else go(embedding_bwd_kernel<float, 1>); }
   else { if (wide) go(embedding_bwd_kernel<bf16, 4>); else go(embedding_bwd_kernel<bf16, 1>); }
-  if (wide) hipLaunchKernelGGL(embedding_join_kernel<4>, grid, dim3(lanes), 0, s, a, chunks);
-  else hipLaunchKernelGGL(embedding_join_kernel<1>, grid, dim3(lanes), 0, s, a, chunks);
+  // (a frequent token's partial sums all meet in the block of its first chunk: a part of a row to a block)
+  const dim3 join(chunks, (c->width + NT * v - 1) / (NT * v));
+  if (wide) hipLaunchKernelGGL(embedding_join_kernel<4>, join, dim3(NT), 0, s, a, chunks);
+  else hipLaunchKernelGGL(embedding_join_kernel<1>, join, dim3(NT), 0, s, a, chunks);
   return hip_status(hipGetLastError(), "ah_embedding_bwd");
 }

@@ -238,29 +238,33 @@ __global__ __launch_bounds__(kBwdThreads) void layer_norm_bwd_kernel(NormArgs a)
   for (int i = 0; i < CH; i++) {
     const int c = (i * NTH + lane) * V;
     if (c < a.width) {
+      wide_t<float, V> u, v;
 #pragma unroll
-      for (int j = 0; j < V; j++) { part[c + j] = dg[i][j]; part[a.width + c + j] = db[i][j]; }
+      for (int j = 0; j < V; j++) { u[j] = dg[i][j]; v[j] = db[i][j]; }
+      store_wide<V>(part + c, u);
+      store_wide<V>(part + a.width + c, v);
     }
   }
 }
 
-// d[c] = beta * d[c] + the sum of part[b][which][c] over the blocks: 64 columns a block, every fourth row a wave
-__global__ __launch_bounds__(1024) void norm_fold_kernel(const float* part, int blocks, int width, float* d_gain, float* d_bias, int beta) {
-  __shared__ float red[16][64];
+// d[c] = beta * d[c] + the sum of part[b][which][c] over the blocks: 32 columns a block, every 32nd row half a wave
+constexpr int kFoldCols = 32, kFoldThreads = 1024, kFoldRows = kFoldThreads / kFoldCols;
+__global__ __launch_bounds__(kFoldThreads) void norm_fold_kernel(const float* part, int blocks, int width, float* d_gain, float* d_bias, int beta) {
+  __shared__ float red[kFoldRows][kFoldCols];
   float* d = blockIdx.y ? d_bias : d_gain;
   if (!d) return;
-  const int c = blockIdx.x * 64 + (threadIdx.x & 63), wave = threadIdx.x >> 6;
+  const int col = threadIdx.x % kFoldCols, c = blockIdx.x * kFoldCols + col, row = threadIdx.x / kFoldCols;
   float s = 0.f;
   if (c < width) {
     const float* p = part + (size_t)blockIdx.y * width + c;
 #pragma unroll 8
-    for (int b = wave; b < blocks; b += 16) s += p[(size_t)b * 2 * width];
+    for (int b = row; b < blocks; b += kFoldRows) s += p[(size_t)b * 2 * width];
   }
-  red[wave][threadIdx.x & 63] = s;
+  red[row][col] = s;
   __syncthreads();
-  if (wave == 0 && c < width) {
+  if (row == 0 && c < width) {
 #pragma unroll
-    for (int w = 1; w < 16; w++) s += red[w][threadIdx.x];
+    for (int w = 1; w < kFoldRows; w++) s += red[w][col];
     d[c] = beta ? d[c] + s : s;
   }
 }
@@ -386,7 +390,7 @@ extern "C" int ah_layer_norm_bwd(const ah_layer_norm_t* c, const void* x, const 
   const int blocks = bwd_blocks(c);
   hipError_t e = run<true>(a, c, wide, blocks, (hipStream_t)stream);      // (no rows: writes zeros)
   if (e == hipSuccess && (d_gain || d_bias)) {
-    hipLaunchKernelGGL(norm_fold_kernel, dim3((c->width + 63) / 64, 2), dim3(1024), 0, (hipStream_t)stream, a.part, blocks, c->width, d_gain, d_bias, beta);
+    hipLaunchKernelGGL(norm_fold_kernel, dim3((c->width + kFoldCols - 1) / kFoldCols, 2), dim3(kFoldThreads), 0, (hipStream_t)stream, a.part, blocks, c->width, d_gain, d_bias, beta);
     e = hipGetLastError();
   }
   return hip_status(e, "ah_layer_norm_bwd");
