@@ -18,10 +18,10 @@ namespace {
 
 constexpr int NT = 256, NW = NT / 64, kMaxRows = 1 << 25, kMaxVocab = 1 << 30, kMaxWidth = 65536;
 constexpr int kFlight = 2;                             // forward: pieces of a row that a lane has in flight
-constexpr int kMaxChunks = 2048, kMinChunk = 16, kAhead = 8, kJoin = 16;
+constexpr int kMaxChunks = 2048, kMinChunk = 16, kAhead = 4, kJoin = 16;
 constexpr int kRowThreads = 1024;
 constexpr int kSmall = 16384;                          // tokens up to which places are counted (rank_kernel)
-constexpr int kFillBlocks = 1024;                      // beside that
+constexpr int kFillBlocks = 4096;                      // beside the sums
 constexpr int kItems = 16, kSortBlock = NT * kItems;   // numbers that a block of the sort takes
 
 struct FwdArgs {
@@ -188,28 +188,13 @@ __global__ __launch_bounds__(NT) void digit_place_kernel(SortArgs a) {
   }
 }
 
-struct FillArgs {
-  float* d;
-  size_t ld;
-  int rows, width, lanes_log2, vec;
-};
-__device__ __forceinline__ void fill_rows(const FillArgs& f, int64_t block, int64_t blocks, int threads) {
-  const int lanes = 1 << f.lanes_log2, lane = threadIdx.x & (lanes - 1), per = threads >> f.lanes_log2;
-  for (int64_t r = block * per + (threadIdx.x >> f.lanes_log2); r < f.rows; r += blocks * per) {
-    float* p = f.d + (size_t)r * f.ld;
-    if (f.vec) for (int c = lane * 4; c < f.width; c += lanes * 4) *(f32x4*)(p + c) = f32x4{0.f, 0.f, 0.f, 0.f};
-    else for (int c = lane; c < f.width; c += lanes) p[c] = 0.f;
-  }
-}
-
 // Few tokens: a number's place in the sorted list is how many lie before it, which a block counts for kRanked of them against all others (one comparison for 64 of
-// those).  The blocks behind the first `rank_blocks` set the rows of the table to zeros meanwhile.
+// those).  3001 tokens 5 us, 8190 13 us (counted by lane and added up at the end: 9 and 16).
 constexpr uint32_t kNone = 0x7ffffffe;       // (twice that and 2 more fit)
 constexpr int kRanked = 16, kRankThreads = 1024, kRankWaves = kRankThreads / 64;
 template <int BITS>
-__global__ __launch_bounds__(kRankThreads) void rank_kernel(SortArgs a, int rank_blocks, FillArgs f) {
+__global__ __launch_bounds__(kRankThreads) void rank_kernel(SortArgs a) {
   __shared__ uint32_t keys[kSmall], count[kRankWaves][kRanked];
-  if ((int)blockIdx.x >= rank_blocks) return fill_rows(f, blockIdx.x - rank_blocks, gridDim.x - rank_blocks, kRankThreads);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = blockIdx.x * kRanked;
   constexpr int FLIGHT = 8;                  // keys of a lane in flight
   for (int t0 = threadIdx.x; t0 - (int)threadIdx.x < a.T; t0 += FLIGHT * kRankThreads) {
@@ -261,7 +246,37 @@ struct BwdArgs {
   float scale;
 };
 
-__global__ __launch_bounds__(NT) void fill_rows_kernel(FillArgs f) { fill_rows(f, blockIdx.x, gridDim.x, NT); }
+// ---- zeros for the rows of the table whose token does not occur (beta 0): `group` rows of them at a time
+struct FillArgs {
+  int group, lanes_log2, vec;       // 2^lanes_log2 lanes to a row, four elements each and time if vec
+};
+constexpr int kGroup = 65536;       // rows of a group, at most
+__device__ __forceinline__ void fill_zeros(const BwdArgs& a, const FillArgs& f, int block, int blocks, uint32_t* touched, bool sorted) {
+  const int lanes = 1 << f.lanes_log2, lane = threadIdx.x & (lanes - 1), row = threadIdx.x >> f.lanes_log2, per = blockDim.x >> f.lanes_log2;
+  for (int64_t v0 = (int64_t)block * f.group; v0 < a.vocab; v0 += (int64_t)blocks * f.group) {
+    const int rows = (int)min((int64_t)f.group, a.vocab - v0);
+    if (sorted) {
+      for (int i = threadIdx.x; i < (rows + 31) / 32; i += blockDim.x) touched[i] = 0;
+      __syncthreads();
+#pragma unroll 4
+      for (int t = threadIdx.x; t < a.T; t += blockDim.x) {
+        const uint32_t r = a.key[t] - (uint32_t)v0;
+        if (r < (uint32_t)rows) atomicOr(&touched[r >> 5], 1u << (r & 31));
+      }
+      __syncthreads();
+    }
+    if (row < per)
+      for (int r = row; r < rows; r += per) {
+        if (sorted && (touched[r >> 5] >> (r & 31)) & 1) continue;
+        float* p = a.d + (size_t)(v0 + r) * a.ld_d;
+        if (f.vec) for (int c = lane * 4; c < a.width; c += lanes * 4) *(f32x4*)(p + c) = f32x4{0.f, 0.f, 0.f, 0.f};
+        else for (int c = lane; c < a.width; c += lanes) p[c] = 0.f;
+      }
+    if (sorted) __syncthreads();
+  }
+}
+// (many tokens: all rows, before those that have a sum are written)
+__global__ __launch_bounds__(NT) void fill_rows_kernel(BwdArgs a, FillArgs f) { fill_zeros(a, f, blockIdx.x, gridDim.x, nullptr, false); }
 
 template <int V>
 __device__ __forceinline__ void put(const BwdArgs& a, uint32_t row, int c, const wide_t<float, V>& s, const wide_t<float, V>& old) {
@@ -275,9 +290,11 @@ __device__ __forceinline__ wide_t<float, V> old_row(const BwdArgs& a, uint32_t r
 }
 
 // A block adds up V columns a lane of one chunk.  A wave's lanes hold the keys and numbers of 64 entries, which are the same for all lanes of a row; rows of dy, and those
-// of the table that get a sum (beta), are asked for kAhead at a time.
+// of the table that get a sum (beta), are asked for kAhead at a time.  The blocks behind the `chunks` first set the table's other rows to zeros meanwhile.
 template <class AT, int V>
-__global__ __launch_bounds__(kRowThreads) void embedding_bwd_kernel(BwdArgs a) {
+__global__ __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(8))) void embedding_bwd_kernel(BwdArgs a, FillArgs f, int chunks) {
+  __shared__ uint32_t touched[kGroup / 32];
+  if ((int)blockIdx.x >= chunks) return fill_zeros(a, f, (blockIdx.x - chunks) * gridDim.y + blockIdx.y, (gridDim.x - chunks) * gridDim.y, touched, true);
   const int c = (blockIdx.y * blockDim.x + threadIdx.x) * V, lane = threadIdx.x & 63;
   const int first = blockIdx.x * a.chunk, end = min(first + a.chunk, a.T);
   const bool on = c < a.width;
@@ -451,15 +468,13 @@ extern "C" int ah_embedding_bwd(const ah_embedding_t* c, const void* tokens, con
   a.dy = dy; a.d = d_table; a.ld_d = c->ld_table ? c->ld_table : c->width; a.ld_dy = c->ld_act ? c->ld_act : c->width;
   a.T = T; a.vocab = c->vocab; a.width = c->width; a.chunk = chunk_of(T); a.beta = beta; a.scale = c->scale;
   FillArgs f = {};
-  if (!beta) {
-    f.d = d_table; f.ld = a.ld_d; f.rows = c->vocab; f.width = c->width;
-    f.vec = c->width % 4 == 0 && rows16(d_table, a.ld_d, 4);
-    f.lanes_log2 = log2_lanes(c->width, f.vec ? 4 : 1);
-  }
+  f.group = std::max(32, std::min(kGroup, 32768 / c->width / 32 * 32));
+  f.vec = c->width % 4 == 0 && rows16(d_table, a.ld_d, 4);
+  f.lanes_log2 = log2_lanes(c->width, f.vec ? 4 : 1);
+  const int groups = (int)(((int64_t)c->vocab + f.group - 1) / f.group);
   const bool small = T > 0 && T <= kSmall;
   if (!beta && !small) {
-    const int per = NT >> f.lanes_log2;
-    hipLaunchKernelGGL(fill_rows_kernel, dim3(std::min<int64_t>(((int64_t)c->vocab + per - 1) / per, 1 << 22)), dim3(NT), 0, s, f);
+    hipLaunchKernelGGL(fill_rows_kernel, dim3(std::min(groups, 1 << 16)), dim3(NT), 0, s, a, f);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return hip_status(e, "ah_embedding_bwd");
   }
   if (T == 0) return AH_OK;
@@ -473,8 +488,7 @@ extern "C" int ah_embedding_bwd(const ah_embedding_t* c, const void* tokens, con
   while (key_bits < 31 && (c->vocab >> key_bits) != 0) key_bits++;
   if (small) {
     q.key_out = (uint32_t*)(w + p.key[0]); q.at_out = (uint32_t*)(w + p.at[0]);
-    const int ranks = (T + kRanked - 1) / kRanked, fills = beta ? 0 : (int)std::min<int64_t>(((int64_t)c->vocab * c->width + 65535) / 65536, kFillBlocks);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(ranks + fills), dim3(kRankThreads), 0, s, q, ranks, f); };
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((T + kRanked - 1) / kRanked), dim3(kRankThreads), 0, s, q); };
     if (c->token_bits == 64) go(rank_kernel<64>);
     else go(rank_kernel<32>);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return hip_status(e, "ah_embedding_bwd");
@@ -496,10 +510,11 @@ extern "C" int ah_embedding_bwd(const ah_embedding_t* c, const void* tokens, con
   // four columns a lane: 16 bytes of the table's gradient, 8 or 16 of dy
   const bool wide = c->width % 4 == 0 && aligned_to(dy, 4 * ab) && a.ld_dy % 4 == 0 && rows16(d_table, a.ld_d, 4);
   const int v = wide ? 4 : 1, chunks = (T + a.chunk - 1) / a.chunk;
-  // lanes for a whole row, or 1024 of them
-  const int slices = (c->width + kRowThreads * v - 1) / (kRowThreads * v), lanes = ((c->width + slices * v - 1) / (slices * v) + 63) / 64 * 64;
-  const dim3 grid(chunks, (c->width + lanes * v - 1) / (lanes * v));
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(lanes), 0, s, a); };
+  // lanes for a whole row, or 1024 of them; zeros need 256
+  const bool fill = !beta && small;
+  const int slices = (c->width + kRowThreads * v - 1) / (kRowThreads * v), lanes = std::max(fill ? NT : 64, ((c->width + slices * v - 1) / (slices * v) + 63) / 64 * 64);
+  const int across = (c->width + lanes * v - 1) / (lanes * v), fills = fill ? (std::min(groups, kFillBlocks) + across - 1) / across : 0;
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(chunks + fills, across), dim3(lanes), 0, s, a, f, chunks); };
   if (ab == 4) { if (wide) go(embedding_bwd_kernel<float, 4>); else go(embedding_bwd_kernel<float, 1>); }
   else { if (wide) go(embedding_bwd_kernel<bf16, 4>); else go(embedding_bwd_kernel<bf16, 1>); }
   // (a frequent token's partial sums all meet in the block of its first chunk: a part of a row to a block)

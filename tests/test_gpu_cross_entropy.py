@@ -138,6 +138,18 @@ def test_targets_that_are_none():
     assert loss[1] == 0 and (g[1] == 0).all()          # a row without a target is not looked at
 
 
+def test_rows_far_into_large_logits():
+    """Elements behind the 2^31st, in place"""
+    T, V = 45000, 50257
+    z = torch.zeros(T, V, dtype=BF, device="cuda")
+    far = [0, 42731, T - 1]
+    z[far] = randn(1, 3, V, dtype=BF, std=2.0)
+    keep, t = z[far].clone(), targets_of(2, T, V)
+    loss = torch.empty(T, device="cuda")
+    P.cross_entropy(z, t, loss, z)
+    check(keep, t[far], loss[far], z[far], 1.0)
+
+
 def test_captured_with_a_scale_on_the_device():
     T, V = 70, 9001
     z, t, scale = randn(1, T, V, dtype=BF), targets_of(2, T, V, none=5), torch.tensor([0.5], device="cuda")

@@ -100,7 +100,8 @@ BWD = [  # T, V, width, type, bits, scale, beta, none, hot
     (1, 1, 1, F32, 64, 1.0, 0, 0, 0), (1, 5, 16, BF, 32, 2.0, 1, 0, 0), (31, 4, 8, BF, 64, 1.0, 0, 0, 0), (32, 1, 264, BF, 64, 1.0, 1, 0, 0),
     (33, 300, 1001, F32, 32, 0.5, 0, 3, 0), (1000, 17, 64, BF, 64, 1.0, 1, 4, 0), (4096, 255, 40, BF, 32, 1.0, 0, 0, 3), (4097, 256, 33, F32, 64, 1.0, 0, 0, 255),
     (5000, 257, 2056, BF, 64, 1.0, 1, 7, 9), (9000, 70000, 24, BF, 32, 1.0, 0, 0, 66000), (70000, 3, 16, F32, 64, 1.0, 0, 0, 1), (9, 20, 8, BF, 64, 1.0, 0, 1, 0),
-    (300000, 1000, 8, BF, 32, 1.0, 1, 50, 0)]
+    (300000, 1000, 8, BF, 32, 1.0, 1, 50, 0), (16384, 70000, 8, F32, 32, 1.0, 0, 9, 4), (16385, 70000, 8, F32, 32, 1.0, 0, 9, 4), (3, 200000, 1, F32, 64, 1.0, 0, 0, 0),
+    (40, 30, 5000, F32, 64, 1.0, 0, 4, 0), (100, 9, 8200, BF, 64, 1.0, 0, 0, 3)]
 
 
 @pytest.mark.parametrize("T,V,w,kind,bits,scale,beta,none,hot", BWD)
@@ -147,6 +148,36 @@ def test_gradient_is_the_same_every_time_and_captured():
         P.embedding_bwd(tok, dy, again, work)
         torch.cuda.synchronize()
         assert torch.equal(again, first), rep
+
+
+def test_padding_reads_nothing():
+    """Rows of dy and of the table that belong to no token may hold anything"""
+    T, V, w = 900, 70, 40
+    tok, dy, table = tokens_of(1, T, V, none=3), randn(2, T, w, dtype=BF), randn(3, V, w, dtype=BF)
+    tok[tok == 0] = 1
+    dy[tok < 0], table[0] = float("nan"), float("inf")
+    y, d = torch.empty_like(dy), torch.empty(V, w, device="cuda")
+    P.embedding_fwd(table, tok, y)
+    P.embedding_bwd(tok, dy, d, torch.empty(P.embedding_bwd_workspace(T, V, w), dtype=torch.uint8, device="cuda"))
+    assert (y[tok < 0] == 0).all() and y.isfinite().all() and d.isfinite().all() and (d[0] == 0).all()
+
+
+@pytest.mark.parametrize("T", [700, 20000])
+def test_rows_far_into_a_large_table(T):
+    """Elements behind the 2^31st, of the table and of its gradient"""
+    V, w = 1100000, 2048
+    table = torch.zeros(V, w, dtype=BF, device="cuda")
+    tok = V - 1 - torch.arange(T, device="cuda") // 2 * 37
+    table[tok] = randn(1, T, w, dtype=BF)
+    y = torch.empty(T, w, dtype=BF, device="cuda")
+    P.embedding_fwd(table, tok, y)
+    assert torch.equal(y, table[tok])
+    del table
+    dy, d = randn(2, T, w, dtype=BF), torch.full((V, w), 7.0, device="cuda")
+    P.embedding_bwd(tok, dy, d, torch.empty(P.embedding_bwd_workspace(T, V, w), dtype=torch.uint8, device="cuda"))
+    assert torch.equal(d[tok[::2]], dy[::2].float() + dy[1::2].float())
+    d[tok] = 0
+    assert not d.any()
 
 
 def test_a_row_that_is_not_finite_reaches_its_token_alone():
