@@ -189,7 +189,7 @@ __global__ __launch_bounds__(NT) void digit_place_kernel(SortArgs a) {
 }
 
 // Few tokens: a number's place in the sorted list is how many lie before it, which a block counts for kRanked of them against all others (one comparison for 64 of
-// those).  3001 tokens 5 us, 8190 13 us (counted by lane and added up at the end: 9 and 16).
+// those, counted by lane: a scalar count behind each comparison fills the CU's one scalar unit).
 constexpr uint32_t kNone = 0x7ffffffe;       // (twice that and 2 more fit)
 constexpr int kRanked = 16, kRankThreads = 1024, kRankWaves = kRankThreads / 64;
 template <int BITS>
@@ -216,16 +216,23 @@ __global__ __launch_bounds__(kRankThreads) void rank_kernel(SortArgs a) {
     const uint32_t k = keys[g + lane];
     if (first >= g && first < g + 64) {      // these 64 hold the block's own (which begin at a multiple of kRanked)
 #pragma unroll
-      for (int i = 0; i < kRanked; i++) n[i] += __popcll(__ballot(2 * k + (lane < first - g + i ? 0u : 2u) < key[i]));
+      for (int i = 0; i < kRanked; i++) n[i] += 2 * k + (lane < first - g + i ? 0u : 2u) < key[i];
     } else {
       const uint32_t k2 = 2 * k + (g < first ? 0u : 2u);       // of those before the block's own the equal ones count, too
 #pragma unroll
-      for (int i = 0; i < kRanked; i++) n[i] += __popcll(__ballot(k2 < key[i]));
+      for (int i = 0; i < kRanked; i++) n[i] += k2 < key[i];
     }
   }
-  if (lane == 0) {
+  // over the wave, two counts in a register (a lane's are at most kSmall / kRankThreads, a wave's 64 times that)
 #pragma unroll
-    for (int i = 0; i < kRanked; i++) count[wave][i] = n[i];
+  for (int i = 0; i < kRanked; i += 2) {
+    int both = (int)(n[i] | n[i + 1] << 16);
+    both += __builtin_amdgcn_update_dpp(0, both, 0xB1, 0xF, 0xF, true);    // lanes 1 0 3 2
+    both += __builtin_amdgcn_update_dpp(0, both, 0x4E, 0xF, 0xF, true);    // lanes 2 3 0 1
+    both += __builtin_amdgcn_update_dpp(0, both, 0x141, 0xF, 0xF, true);   // lanes 7 .. 0 of 8
+    both += __builtin_amdgcn_update_dpp(0, both, 0x140, 0xF, 0xF, true);   // lanes 15 .. 0 of 16
+    const uint32_t sum = __builtin_amdgcn_readlane(both, 0) + __builtin_amdgcn_readlane(both, 16) + __builtin_amdgcn_readlane(both, 32) + __builtin_amdgcn_readlane(both, 48);
+    if (lane == 0) { count[wave][i] = sum & 0xffff; count[wave][i + 1] = sum >> 16; }
   }
   __syncthreads();
   if (threadIdx.x < kRanked && first + (int)threadIdx.x < a.T) {
