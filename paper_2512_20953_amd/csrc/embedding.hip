@@ -1,8 +1,9 @@
 // Embedding of tokens and its gradient (declared in include/ah_ops.h).  Bound by HBM: forward reads a row of the table for each token and
-// writes one, backward reads the rows' gradients and writes (or adds to) the rows of the table that occur.
+// writes one (8192 x 4096 with positions 28 us: 4.0 TB/s of what it cannot do without), backward reads the rows' gradients and writes (or adds to) the rows of the table that
+// occur (8190 x 4096, added: 64 us, of which 44 for the sums at 4.2 TB/s; 3001 x 1001 in fp32, 32000 rows written: 38).
 //
-// Backward: the tokens' numbers are sorted by token, stably (digits of 8 bits from the lowest on), so that the rows that a row of the table
-// is the sum of lie behind each other.  The sorted list is cut into chunks; a block adds up a chunk, writes each sum that begins and ends in it, and leaves the
+// Backward: the tokens' numbers are sorted by token, stably (up to 16384 of them by counting each one's place, else by digits of 8 bits from the lowest on), so that the rows that
+// a row of the table is the sum of lie behind each other.  The sorted list is cut into chunks; a block adds up a chunk, writes each sum that begins and ends in it, and leaves the
 // sums that reach over its ends, at most one on either side, as partial sums, which a second kernel adds up in the chunks' order.  So the work of a
 // block does not depend on how often a token occurs, and no row is written by two blocks.
 #include "ah_ops.h"
@@ -345,7 +346,9 @@ __global__ __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(8))
   }
 }
 
-// The chunk in which a sum begins that goes on behind it adds up what the following ones left of it.
+// The chunk in which a sum begins that goes on behind it adds up what the following ones left of it: kJoinAcross lanes across a row, twice.  (8190 tokens as frequent as words are, and
+// 8192 times the same one, the whole call: 63 and 63 us; 256 lanes across, once, 64 and 108; 64, four times, 67 and 47.)
+constexpr int kJoinAcross = NT / 2;
 template <int V>
 __global__ __launch_bounds__(NT) void embedding_join_kernel(BwdArgs a, int chunks) {
   const int first = blockIdx.x * a.chunk, end = first + a.chunk;
@@ -353,27 +356,34 @@ __global__ __launch_bounds__(NT) void embedding_join_kernel(BwdArgs a, int chunk
   const uint32_t k = a.key[end - 1];
   if (k >= (uint32_t)a.vocab || a.key[end] != k) return;
   if (a.key[first] == k && first > 0 && a.key[first - 1] == k) return;      // it began earlier
-  const int at = (blockIdx.y * NT + threadIdx.x) * V, c = at < a.width ? at : 0;      // (lanes behind the last column keep its company: the ballots below are whole waves')
+  __shared__ wide_t<float, V> share[kJoinAcross];
+  const int across = threadIdx.x % kJoinAcross, half = threadIdx.x / kJoinAcross, at = (blockIdx.y * kJoinAcross + across) * V, c = at < a.width ? at : 0;   // (lanes behind the last column go along: ballots are whole waves')
   const float* p = a.part + (size_t)blockIdx.x * 2 * a.width + c;
   const wide_t<float, V> old = old_row<V>(a, k, c);
-  wide_t<float, V> s = load_wide<V>(p + a.width);
-  // the chunks behind this one that begin with the same token: all of their entries, or the last of its
+  // the chunks behind this one that begin with the same token: all of their entries, or the first of its
   int behind = 0;
   for (int b = blockIdx.x + 1 + (threadIdx.x & 63);; b += 64) {
     const uint64_t same = __ballot(b < chunks && a.key[(size_t)min(b, chunks - 1) * a.chunk] == k);
     behind += ~same ? __builtin_ctzll(~same) : 64;
     if (~same) break;
   }
-  p += 2 * (size_t)a.width;
-  for (int b = 0; b < behind; b += kJoin) {
+  // this one's share is number 0; the block's two halves add up one of them each
+  auto share_of = [&](int i) { return load_wide<V>(p + (i == 0 ? a.width : (size_t)i * 2 * a.width)); };
+  const int from = (behind + 2) / 2 * half, to = half ? behind + 1 : (behind + 2) / 2;
+  wide_t<float, V> s = {};
+  for (int b = from; b < to; b += kJoin) {
     wide_t<float, V> r[kJoin];
 #pragma unroll
-    for (int i = 0; i < kJoin; i++) r[i] = load_wide<V>(p + (size_t)min(b + i, behind - 1) * 2 * a.width);
+    for (int i = 0; i < kJoin; i++) r[i] = share_of(min(b + i, to - 1));
 #pragma unroll
     for (int i = 0; i < kJoin; i++)
-      if (b + i < behind) s += r[i];
+      if (b + i < to) s += r[i];
   }
-  if (at < a.width) put<V>(a, k, c, s, old);
+  if (half) share[across] = s;
+  __syncthreads();
+  if (half || at >= a.width) return;
+  s += share[across];
+  put<V>(a, k, c, s, old);
 }
 
 int sort_blocks(int T) { return (T + kSortBlock - 1) / kSortBlock; }
@@ -524,8 +534,7 @@ extern "C" int ah_embedding_bwd(const ah_embedding_t* c, const void* tokens, con
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(chunks + fills, across), dim3(lanes), 0, s, a, f, chunks); };
   if (ab == 4) { if (wide) go(embedding_bwd_kernel<float, 4>); else go(embedding_bwd_kernel<float, 1>); }
   else { if (wide) go(embedding_bwd_kernel<bf16, 4>); else go(embedding_bwd_kernel<bf16, 1>); }
-  // (a frequent token's partial sums all meet in the block of its first chunk: a part of a row to a block)
-  const dim3 join(chunks, (c->width + NT * v - 1) / (NT * v));
+  const dim3 join(chunks, (c->width + kJoinAcross * v - 1) / (kJoinAcross * v));
   if (wide) hipLaunchKernelGGL(embedding_join_kernel<4>, join, dim3(NT), 0, s, a, chunks);
   else hipLaunchKernelGGL(embedding_join_kernel<1>, join, dim3(NT), 0, s, a, chunks);
   return hip_status(hipGetLastError(), "ah_embedding_bwd");

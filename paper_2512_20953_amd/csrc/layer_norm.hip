@@ -1,5 +1,6 @@
-// Layer norm (with or without the mean) of rows of any width, forward and backward (declared in include/ah_ops.h).  Bound by HBM: x read and y written once;
-// backward x and dy read, dx written, and the partial sums behind the gradients of gain and bias.
+// Layer norm (with or without the mean) of rows of any width, forward and backward (declared in include/ah_ops.h).  Bound by HBM: x read and y written once (8192 x 4096: 28 us,
+// 4.7 TB/s); backward x and dy read, dx written, and the partial sums behind the gradients of gain and bias (4096 x 4096: 30 us, 3.3 TB/s, of which about 10 do not depend on the
+// number of rows: first loads, 8 MB of partial sums, their fold; 32768 x 4096: 4.2 TB/s).
 //
 // A row stays in the registers of a wave or of a block from its load to its result.  Sums over a row: forward the mean, then the squares around it; backward the sums of x and of
 // w = dy gain, then of (x - mean)^2 and of w (x - mean), from which all that dx needs follows:

@@ -5,7 +5,8 @@
 //   A = X X^T                 n^2 m flops: the product is symmetric, so that the tiles on and below the diagonal are computed and each is stored twice
 //   B = b A + c A A           n^3: likewise
 //   X = a X + B X             2 n^2 m
-// Bound by the matrix units from n of about a thousand on.
+// Bound by the matrix units from n of about two thousand on, at the clock that their power leaves (1.87 GHz measured; a LLaMA-style layer's matrices, 4096 x 4096 and 4096 x 11008:
+// 14.6 ms, of which products 12.8 at 1.16 PFLOP/s; the loop by itself reaches 1.36, a library's product 1.5); below that by how long few k-steps take to arrive.
 //
 // Types.  The operands are fp16: with everything within 3 in magnitude (A and B are polynomials of a matrix whose singular values stay below 1.21) its range suffices, and it
 // keeps 11 bits where bf16 keeps 8, at the same rate.  X itself goes from product to product in 22 bits, as two fp16 numbers: what is added to a X has to be added to the same X
