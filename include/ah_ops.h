@@ -211,7 +211,8 @@ int ah_embedding_bwd_workspace(const ah_embedding_t* cfg, uint64_t* bytes);
 
 /* ---- layer norm: what stands in front of the head ----
  *
- * n = (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps) of each row (rms: without the mean), y = n * gain + bias, in fp32, rounded once. */
+ * n = (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps) of each row (rms: without the mean), y = n * gain + bias, in fp32, rounded once (a row whose sum of squares is above
+ * fp32's range, elements of 1e18 and more, comes out as its bias, backward as zeros or NaN).  What is not finite in a row stays in it (backward: and in the gradients of gain and bias). */
 typedef struct {
   uint32_t struct_size;       /* sizeof(ah_layer_norm_t), checked */
   int32_t rows;               /* T, 0 .. 2^25 */

@@ -101,7 +101,8 @@ BWD = [  # T, V, width, type, bits, scale, beta, none, hot
     (33, 300, 1001, F32, 32, 0.5, 0, 3, 0), (1000, 17, 64, BF, 64, 1.0, 1, 4, 0), (4096, 255, 40, BF, 32, 1.0, 0, 0, 3), (4097, 256, 33, F32, 64, 1.0, 0, 0, 255),
     (5000, 257, 2056, BF, 64, 1.0, 1, 7, 9), (9000, 70000, 24, BF, 32, 1.0, 0, 0, 66000), (70000, 3, 16, F32, 64, 1.0, 0, 0, 1), (9, 20, 8, BF, 64, 1.0, 0, 1, 0),
     (300000, 1000, 8, BF, 32, 1.0, 1, 50, 0), (16384, 70000, 8, F32, 32, 1.0, 0, 9, 4), (16385, 70000, 8, F32, 32, 1.0, 0, 9, 4), (3, 200000, 1, F32, 64, 1.0, 0, 0, 0),
-    (40, 30, 5000, F32, 64, 1.0, 0, 4, 0), (100, 9, 8200, BF, 64, 1.0, 0, 0, 3)]
+    (40, 30, 5000, F32, 64, 1.0, 0, 4, 0), (100, 9, 8200, BF, 64, 1.0, 0, 0, 3), (40, 5, 65536, BF, 32, 1.0, 1, 3, 0),
+    (50, 3, 65535, F32, 32, 1.0, 0, 3, 0)]
 
 
 @pytest.mark.parametrize("T,V,w,kind,bits,scale,beta,none,hot", BWD)

@@ -114,7 +114,7 @@ def test_singular_values(steps):
         assert 0.68 <= s.min() and s.max() <= 1.21
 
 
-@pytest.mark.parametrize("r,c", SIZES)
+@pytest.mark.parametrize("r,c", SIZES + [(2, 100000), (70000, 3), (1, 131072)])
 @pytest.mark.parametrize("rank", [1, 3, 0])
 def test_one_step(r, c, rank):
     """Of matrices with few directions, whose singular values are large from the start, and of others"""
@@ -123,7 +123,8 @@ def test_one_step(r, c, rank):
     want, rounded = orthogonal(g * 0.05 * 1.95, steps=1)
     # (the product that made a matrix of few directions is the gradient as it is; u = 0.0975 g is rounded four times)
     assert norm(x.double() - want) <= one_step(g * 0.05 * 1.95) + 8 * U * A * norm(want)
-    assert norm(x.double() - want) <= room_of(want, rounded)
+    if max(r, c) < 10000:       # (longer sums than that are off by more than an operand's rounding leaves in them)
+        assert norm(x.double() - want) <= room_of(want, rounded)
 
 
 @pytest.mark.parametrize("nesterov", [True, False])
@@ -192,6 +193,30 @@ def test_what_is_not_finite_stays_in_its_matrix():
     xs, _ = update_of(gs)
     assert torch.equal(xs[0], clean[0]) and torch.equal(xs[3], clean[3])
     assert xs[1].isnan().all() and xs[2].isnan().all()
+
+
+def test_what_the_scratch_memory_held_and_matrices_without_elements():
+    shapes = [(200, 333), (0, 7), (64, 64), (5, 0), (300, 40)]
+    gs = [randn(k, *s) for k, s in enumerate(shapes)]
+    clean, _ = update_of([g for g in gs if g.numel()])
+    ps = [torch.zeros_like(g) for g in gs]
+    opt = P.Muon(ps, gs, scale=1.0)
+    opt._work.fill_(255)
+    opt.step(1.0)
+    assert all(torch.equal(-p, x) for p, x in zip([p for p in ps if p.numel()], clean))
+    P.Muon([torch.zeros(0, 3, device="cuda")], [torch.zeros(0, 3, device="cuda")]).step(1.0)
+
+
+def test_more_matrices_than_are_worked_on_together():
+    """2^26 elements each: four to a group, in one call; a matrix comes out the same wherever it stands"""
+    n = 8192
+    g = [randn(k, n, n) for k in range(2)]
+    ps = [torch.zeros(n, n, device="cuda") for _ in range(5)]
+    P.Muon(ps, [g[0], g[1], g[1], g[0], g[0]], scale=1.0).step(1.0)
+    assert torch.equal(ps[0], ps[3]) and torch.equal(ps[0], ps[4]) and torch.equal(ps[1], ps[2])
+    x = -ps[0][:, :512].double()                       # 512 of the columns of a factor whose singular values are 0.68 .. 1.21: theirs are at most that, and not 0
+    s = torch.linalg.eigvalsh(x.T @ x).sqrt()
+    assert 0 < s.min() and s.max() <= 1.21
 
 
 def test_factor_of_the_gradients_norm():
