@@ -5,10 +5,12 @@
 //   A = X X^T                 n^2 m flops: the product is symmetric, so that the tiles on and below the diagonal are computed and each is stored twice
 //   B = b A + c A A           n^3: likewise
 //   X = a X + B X             2 n^2 m
+// or, the first two of the steps at once, 3 n^2 m + 5 n^3 instead of 6 n^2 m + 2 n^3 (see Product).
 // Bound by the matrix units from n of about two thousand on, at the clock that their power leaves (1.87 GHz measured; a LLaMA-style layer's matrices, 4096 x 4096 and 4096 x 11008:
-// 14.6 ms, of which products 12.8 at 1.16 PFLOP/s; the loop by itself reaches 1.36, a library's product 1.5); below that by how long few k-steps take to arrive.
+// 14.1 ms, of which products 12.3; the loop by itself reaches 1.36 PFLOP/s, a library's product 1.5); below that by how long few k-steps take to arrive.
 //
-// Types.  The operands are fp16: with everything within 3 in magnitude (A and B are polynomials of a matrix whose singular values stay below 1.21) its range suffices, and it
+// Types.  The operands are fp16: with everything within 3 in magnitude, or 12 (A and B, and what two steps at once have besides, are polynomials of a matrix whose singular values stay
+// below 1.21), its range suffices, and it
 // keeps 11 bits where bf16 keeps 8, at the same rate.  X itself goes from product to product in 22 bits, as two fp16 numbers: what is added to a X has to be added to the same X
 // that it was computed from, or the rounding of every step is taken for a part of X, which the polynomial multiplies by up to 3.44 a step where singular values are small.  Of a
 // matrix with 64 strong directions above a floor of noise (1024 x 2816) the factor is 5e-4 off in norm, with X in fp16 alone 2e-2, in bf16 alone 0.18.  Fixed powers of two keep small
@@ -41,9 +43,9 @@ struct Matrix {
   void* p;
   const void* g;
   float *m, *master;
-  f16 *hi[2], *lo, *A, *B;
+  f16 *hi[2], *lo, *A, *B, *B1, *C;
   double *part, *inv;          // sums of squares of the pieces; 1 / (norm + eps)
-  int64_t ld_p, ld_g, ld_m, ld_master;
+  uint32_t ld_p, ld_g, ld_m, ld_master;
   int rows, cols, n, k;        // n x k: the padded X
   float wd, scale;
   int aligned;                 // rows of all four begin at whole multiples of 4 elements
@@ -302,8 +304,13 @@ __global__ __launch_bounds__(NT) void apply_kernel(Table t, Hyper h, int last) {
   else apply_piece<PT, MASTER, 1>(e, r0, c0, keep, by, last, turned);
 }
 
-// ---- the products.  S x S tiles, four waves of S / 2 x S / 2.  SYM_A: A = X X^T; SYM_B: B = b A + c A A^T; STEP: X = a X + B X.
-enum Product { SYM_A, SYM_B, STEP };
+// ---- the products.  S x S tiles, four waves of S / 2 x S / 2.  SYM_A: A = X X^T; SYM_B: B = b A + c A A; STEP: X = a X + B X.
+// Two steps at once, where X has many more columns than rows: behind A and B
+//   SYM_C: C = B A;  SYM_D: A = a^2 A + 2 a C + B C, which is the A of the second step, (a + B) A (a + B);  SYM_B once more, to B1;
+//   SYM_Q: C = a (B + B1) + B1 B, so that (a + B1)(a + B) = a^2 + C;  STEP: X = a^2 X + C X
+// (all of these commute: the products are symmetric).  Of the first two steps only, where X is small: two later ones would be 2 to 10 times as far off.
+enum Product { SYM_A, SYM_B, SYM_C, SYM_D, SYM_Q, STEP };
+constexpr int kPair = 2;             // in `how`, whose lowest bit says which X is there: the second SYM_B, and the STEP, of two steps at once
 
 // Blocks are dealt to the 8 XCDs round-robin, and each XCD has an L2 of its own: a matrix is given to `span` XCDs from `first` on, and each of those a row of consecutive tiles of it.
 struct Deal {
@@ -337,7 +344,7 @@ struct Job {
   const f16 *a, *b;
 };
 template <int S, Product P>
-__device__ __forceinline__ void find_job(const Matrix& e, int tile, int from, Job& j) {
+__device__ __forceinline__ void find_job(const Matrix& e, int tile, int how, Job& j) {
   if constexpr (P == STEP) {                       // down groups of 4 tile rows
     const int tm = e.n / S, tn = e.k / S, group = tile / (4 * tn), rows = min(tm - 4 * group, 4), in = tile - group * 4 * tn;
     j.ti = group * 4 + in % rows;
@@ -351,50 +358,58 @@ __device__ __forceinline__ void find_job(const Matrix& e, int tile, int from, Jo
   }
   j.m0 = j.ti * S;
   j.n0 = j.tj * S;
-  const f16* X = e.hi[from];
+  const f16* X = e.hi[how & 1];
   if constexpr (P == SYM_A) { j.lda = j.ldb = j.K = e.k; j.a = X + (size_t)j.m0 * e.k; j.b = X + (size_t)j.n0 * e.k; }
-  else if constexpr (P == SYM_B) { j.lda = j.ldb = j.K = e.n; j.a = e.A + (size_t)j.m0 * e.n; j.b = e.A + (size_t)j.n0 * e.n; }
-  else { j.lda = j.K = e.n; j.ldb = e.k; j.a = e.B + (size_t)j.m0 * e.n; j.b = X + j.n0; }
+  else if constexpr (P == STEP) { j.lda = j.K = e.n; j.ldb = e.k; j.a = (how & kPair ? e.C : e.B) + (size_t)j.m0 * e.n; j.b = X + j.n0; }
+  else {
+    const f16 *l = P == SYM_B ? e.A : P == SYM_Q ? e.B1 : e.B, *r = P == SYM_D ? e.C : P == SYM_Q ? e.B : e.A;
+    j.lda = j.ldb = j.K = e.n; j.a = l + (size_t)j.m0 * e.n; j.b = r + (size_t)j.n0 * e.n;
+  }
 }
 
-// What 8 elements of a result from (row, col) on need beside their sums: of X the two halves, of B those of A.  Asked for ahead: the compiler would not move these loads
-// over the stores of the elements before.
-template <Product P> struct Beside { f16x8 hi, lo; };
+// What 8 elements of a result from (row, col) on need beside their sums: the two halves of X, or one or two of the square matrices.  Asked for ahead: the compiler would not
+// move these loads over the stores of the elements before.
+template <Product P> constexpr int beside() { return P == SYM_A || P == SYM_C ? 0 : P == SYM_B ? 1 : 2; }
+struct Beside { f16x8 u, v; };
 template <Product P>
-__device__ __forceinline__ Beside<P> ask8(const Matrix& e, int from, int row, int col) {
-  Beside<P> x = {};
-  if constexpr (P == STEP) {
-    x.hi = *(const f16x8*)(e.hi[from] + (size_t)row * e.k + col);
-    x.lo = *(const f16x8*)(e.lo + (size_t)row * e.k + col);
-  } else if constexpr (P == SYM_B) {
-    x.hi = *(const f16x8*)(e.A + (size_t)row * e.n + col);
-  }
+__device__ __forceinline__ Beside ask8(const Matrix& e, int how, int row, int col) {
+  Beside x = {};
+  const size_t at = (size_t)row * (P == STEP ? e.k : e.n) + col;
+  const f16 *u = P == STEP ? e.hi[how & 1] : P == SYM_Q ? e.B : e.A, *v = P == STEP ? e.lo : P == SYM_Q ? e.B1 : e.C;
+  if constexpr (beside<P>() > 0) x.u = *(const f16x8*)(u + at);
+  if constexpr (beside<P>() > 1) x.v = *(const f16x8*)(v + at);
   return x;
 }
 // ... and those elements, whose sums are v
 template <Product P>
-__device__ __forceinline__ void put8(const Matrix& e, int from, int row, int col, const float (&v)[8], const Beside<P>& x) {
+__device__ __forceinline__ void put8(const Matrix& e, int how, int row, int col, const float (&v)[8], const Beside& x) {
   f16x8 o;
   if constexpr (P == STEP) {
     f16x8 ol;
+    const float a = how & kPair ? kA_ * kA_ : kA_;
 #pragma unroll
     for (int j = 0; j < 8; j++) {
       f16 hi, lo;
-      split(__builtin_fmaf(kA_, (float)x.hi[j] + (float)x.lo[j] * (1.f / kLo), v[j] * (1.f / kA)), hi, lo);
+      split(__builtin_fmaf(a, (float)x.u[j] + (float)x.v[j] * (1.f / kLo), v[j] * (1.f / kA)), hi, lo);
       o[j] = hi;
       ol[j] = lo;
     }
-    *(f16x8*)(e.hi[from ^ 1] + (size_t)row * e.k + col) = o;
+    *(f16x8*)(e.hi[(how & 1) ^ 1] + (size_t)row * e.k + col) = o;
     *(f16x8*)(e.lo + (size_t)row * e.k + col) = ol;
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; j++) o[j] = P == SYM_A ? (f16)(v[j] * (kA / (kX * kX))) : (f16)__builtin_fmaf(kB_, (float)x.hi[j], v[j] * (kC_ / kA));
-    *(f16x8*)((P == SYM_A ? e.A : e.B) + (size_t)row * e.n + col) = o;
+    for (int j = 0; j < 8; j++) {
+      const float u = (float)x.u[j], w = (float)x.v[j], sum = v[j] * (P == SYM_A ? kA / (kX * kX) : 1.f / kA);
+      o[j] = (f16)(P == SYM_A || P == SYM_C ? sum : P == SYM_B ? __builtin_fmaf(kB_, u, kC_ * sum) : P == SYM_D ? __builtin_fmaf(kA_ * kA_, u, __builtin_fmaf(2 * kA_, w, sum))
+                   : __builtin_fmaf(kA_, u + w, sum));
+    }
+    f16* to = P == SYM_B ? (how & kPair ? e.B1 : e.B) : P == SYM_A || P == SYM_D ? e.A : e.C;
+    *(f16x8*)(to + (size_t)row * e.n + col) = o;
   }
 }
 
 template <int S, Product P, int DEPTH>
-__global__ __launch_bounds__(NT) void product_kernel(Table t, Deal d, int from) {
+__global__ __launch_bounds__(NT) void product_kernel(Table t, Deal d, int how) {
   constexpr int W = S / 2, TB = W / 16;
   constexpr bool BKS = P == STEP;                  // X is [k, columns] there
   constexpr int RING = k64::ring_bytes<S, S, DEPTH, true>();
@@ -405,7 +420,7 @@ __global__ __launch_bounds__(NT) void product_kernel(Table t, Deal d, int from) 
   if (which < 0) return;
   const Matrix& e = t.e[which];
   Job g;
-  find_job<S, P>(e, tile, from, g);
+  find_job<S, P>(e, tile, how, g);
   f32x4 acc[TB][TB];
 #pragma unroll
   for (int i = 0; i < TB; i++)
@@ -426,22 +441,22 @@ __global__ __launch_bounds__(NT) void product_kernel(Table t, Deal d, int from) 
   __syncthreads();
   char* strip = ring + wave * (32 * ROWB);
   const int cp = lane % PPR, row0 = lane / PPR, n0 = g.n0 + wn * W;
-  Beside<P> x[2][NIT], xt[W / 64][4];
+  Beside x[2][NIT], xt[W / 64][4];
   auto ask = [&](int tm) {
 #pragma unroll
-    for (int it = 0; it < NIT; it++) x[tm & 1][it] = ask8<P>(e, from, g.m0 + wm * W + tm * 32 + row0 + it * RPI, n0 + cp * 8);
+    for (int it = 0; it < NIT; it++) x[tm & 1][it] = ask8<P>(e, how, g.m0 + wm * W + tm * 32 + row0 + it * RPI, n0 + cp * 8);
   };
   ask(0);
 #pragma unroll
   for (int tm = 0; tm < W / 32; tm++) {
     const int mbase = g.m0 + wm * W + tm * 32;
     if (tm + 1 < W / 32) ask(tm + 1);
-    if constexpr (P == SYM_B) {                    // (A is symmetric bit for bit: the same elements across the diagonal)
+    if constexpr (P != STEP && beside<P>() > 0) {  // (the same elements across the diagonal, where other matrices are not symmetric to the last bit)
       if (g.ti != g.tj) {
 #pragma unroll
         for (int half = 0; half < W / 64; half++)
 #pragma unroll
-          for (int r = 0; r < 4; r++) xt[half][r] = ask8<P>(e, from, n0 + half * 64 + lane, mbase + r * 8);
+          for (int r = 0; r < 4; r++) xt[half][r] = ask8<P>(e, how, n0 + half * 64 + lane, mbase + r * 8);
       }
     }
 #pragma unroll
@@ -456,7 +471,7 @@ __global__ __launch_bounds__(NT) void product_kernel(Table t, Deal d, int from) 
       const char* q = strip + row * ROWB + cp * 32;
       const f32x4 v0 = *(const f32x4*)q, v1 = *(const f32x4*)(q + 16);
       const float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-      put8<P>(e, from, mbase + row, n0 + cp * 8, v, x[tm & 1][it]);
+      put8<P>(e, how, mbase + row, n0 + cp * 8, v, x[tm & 1][it]);
     }
     if constexpr (P != STEP) {
       if (g.ti != g.tj) {                          // the tile across the diagonal: 8 rows of a column a lane
@@ -468,7 +483,7 @@ __global__ __launch_bounds__(NT) void product_kernel(Table t, Deal d, int from) 
             float v[8];
 #pragma unroll
             for (int j = 0; j < 8; j++) v[j] = *(const float*)(strip + (r * 8 + j) * ROWB + c * 4);
-            put8<P>(e, from, n0 + c, mbase + r * 8, v, xt[half][r]);
+            put8<P>(e, how, n0 + c, mbase + r * 8, v, xt[half][r]);
           }
       }
     }
@@ -479,7 +494,7 @@ __global__ __launch_bounds__(NT) void product_kernel(Table t, Deal d, int from) 
 
 // The same for few tiles: 64 x 64, each wave one k-step in four of the whole tile.  Four times the blocks, whose chains of k-steps are a quarter as long.
 template <Product P>
-__global__ __launch_bounds__(NT) void small_product_kernel(Table t, Deal d, int from) {
+__global__ __launch_bounds__(NT) void small_product_kernel(Table t, Deal d, int how) {
   constexpr int S = 64, ROWB = S * 4 + 16, STRIP = S * ROWB;
   constexpr int RING = ksplit::stages<S, S>() * ksplit::stage_bytes<S, S>();
   static_assert(4 * STRIP <= RING, "the partial sums fit in the ring");
@@ -490,7 +505,7 @@ __global__ __launch_bounds__(NT) void small_product_kernel(Table t, Deal d, int 
   if (which < 0) return;
   const Matrix& e = t.e[which];
   Job g;
-  find_job<S, P>(e, tile, from, g);
+  find_job<S, P>(e, tile, how, g);
   f32x16 acc[2][2];
 #pragma unroll
   for (int i = 0; i < 2; i++)
@@ -502,13 +517,13 @@ __global__ __launch_bounds__(NT) void small_product_kernel(Table t, Deal d, int 
   __builtin_amdgcn_s_waitcnt(0);
   // a wave writes 16 of the rows, and as many columns across the diagonal
   const int row0 = wave * 16 + lane / 8, cp = lane % 8;
-  Beside<P> x[2], xt[2] = {};
+  Beside x[2], xt[2] = {};
 #pragma unroll
-  for (int it = 0; it < 2; it++) x[it] = ask8<P>(e, from, g.m0 + row0 + it * 8, g.n0 + cp * 8);
-  if constexpr (P == SYM_B) {
+  for (int it = 0; it < 2; it++) x[it] = ask8<P>(e, how, g.m0 + row0 + it * 8, g.n0 + cp * 8);
+  if constexpr (P != STEP && beside<P>() > 0) {
     if (g.ti != g.tj) {
 #pragma unroll
-      for (int r = 0; r < 2; r++) xt[r] = ask8<P>(e, from, g.n0 + lane, g.m0 + wave * 16 + r * 8);
+      for (int r = 0; r < 2; r++) xt[r] = ask8<P>(e, how, g.n0 + lane, g.m0 + wave * 16 + r * 8);
     }
   }
   __syncthreads();
@@ -532,7 +547,7 @@ __global__ __launch_bounds__(NT) void small_product_kernel(Table t, Deal d, int 
 #pragma unroll
     for (int w = 1; w < 4; w++) { v0 += *(const f32x4*)(q + w * STRIP); v1 += *(const f32x4*)(q + w * STRIP + 16); }
     const float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-    put8<P>(e, from, g.m0 + row, g.n0 + cp * 8, v, x[it]);
+    put8<P>(e, how, g.m0 + row, g.n0 + cp * 8, v, x[it]);
   }
   if constexpr (P != STEP) {
     if (g.ti != g.tj) {
@@ -546,7 +561,7 @@ __global__ __launch_bounds__(NT) void small_product_kernel(Table t, Deal d, int 
 #pragma unroll
           for (int w = 1; w < 4; w++) v[j] += *(const float*)(q + w * STRIP);
         }
-        put8<P>(e, from, g.n0 + lane, g.m0 + wave * 16 + r * 8, v, xt[r]);
+        put8<P>(e, how, g.n0 + lane, g.m0 + wave * 16 + r * 8, v, xt[r]);
       }
     }
   }
@@ -558,6 +573,7 @@ uint64_t up(uint64_t n, uint64_t to) { return (n + to - 1) / to * to; }
 struct Group {
   std::vector<int> which;      // of the call's matrices
   int tile;
+  bool pair;
   std::vector<int> n, k;       // padded
   uint64_t bytes;
 };
@@ -575,28 +591,34 @@ constexpr Kind kKinds[] = {{64, 4.5, 4.0, 0.4, 4.2}, {128, 4.5, 7.8, 3.5, 8.1}, 
 uint64_t tiles_of(Product p, uint64_t n, uint64_t m, int tile) { return p == STEP ? (n / tile) * (m / tile) : (n / tile) * (n / tile + 1) / 2; }
 double depth_of(Product p, uint64_t n, uint64_t m) { return (p == SYM_A ? m : n) * 1e-3; }
 
-// The tile that a group's products are expected to be fastest with
-int tile_of(const ah_muon_matrix_t* x, const std::vector<int>& which) {
-  int best = 64;
+// What a product of a group is expected to take
+double time_of(Product p, const ah_muon_matrix_t* x, const std::vector<int>& which, const Kind& k) {
+  double sum = 0, longest = 0;
+  uint64_t tiles = 0;
+  for (int i : which) {
+    const uint64_t n = up(small_side(x[i]), std::max(k.tile, 128)), m = up(large_side(x[i]), std::max(k.tile, 128)), count = tiles_of(p, n, m, k.tile);
+    const double K = depth_of(p, n, m);
+    sum += count * (k.full0 + k.full1 * K);
+    longest = std::max(longest, k.alone0 + k.alone1 * K);
+    tiles += count;
+  }
+  // (a block of 256 x 256 has its CU to itself: whole rounds)
+  return std::max(longest, k.tile == 256 ? sum / tiles * ((tiles + 255) / 256) : sum / 256);
+}
+
+// The tiles that a group's products are expected to be fastest with, and whether its first two steps are taken at once: three more products of n^3 for one A and one X less.
+// Five steps, apart and at once, us: a LLaMA-style layer 14830, 14130; 4 of 2048 x 8192 2924, 2651; one 5120 x 20480 8270, 7269; 4 of 1536 x 4608 1158, 1079; one 4096 x 6144
+// 2329, 2326; one 4096 x 4096 1558, 1627; 24 of 1024 x 1024 1323, 1443.  Tiles of 64 never take it: their products are bound by the launches, of which it has one more.
+void choose(const ah_muon_matrix_t* x, Group& g) {
   double least = 0;
   for (const Kind& k : kKinds) {
-    double total = 0;
-    for (Product p : {SYM_A, SYM_B, STEP}) {
-      double sum = 0, longest = 0;
-      uint64_t tiles = 0;
-      for (int i : which) {
-        const uint64_t n = up(small_side(x[i]), std::max(k.tile, 128)), m = up(large_side(x[i]), std::max(k.tile, 128)), count = tiles_of(p, n, m, k.tile);
-        const double K = depth_of(p, n, m);
-        sum += count * (k.full0 + k.full1 * K);
-        longest = std::max(longest, k.alone0 + k.alone1 * K);
-        tiles += count;
-      }
-      // (a block of 256 x 256 has its CU to itself: whole rounds)
-      total += std::max(longest, k.tile == 256 ? sum / tiles * ((tiles + 255) / 256) : sum / 256);
+    const double a = time_of(SYM_A, x, g.which, k), b = time_of(SYM_B, x, g.which, k), step = time_of(STEP, x, g.which, k);
+    if (least == 0 || a + b + step < least) {
+      least = a + b + step;
+      g.tile = k.tile;
+      g.pair = k.tile > 64 && a + step > 1.05 * 3 * b + 3;
     }
-    if (least == 0 || total < least) { least = total; best = k.tile; }
   }
-  return best;
 }
 
 // Deals a product's tiles to the XCDs.  Tiles of 64 and 128, which are bound by how fast their operands arrive: each matrix to as few XCDs as have it in their L2s (4 MB each) and
@@ -637,13 +659,14 @@ uint32_t deal(Product p, const Table& t, int n, const Kind& kind, Deal& d) {
   return most * 8;
 }
 
-struct Offsets { uint64_t hi0, hi1, lo, A, B, part, inv, end; };
-Offsets offsets(const ah_muon_matrix_t& x, int n, int k, uint64_t at) {
+struct Offsets { uint64_t hi0, hi1, lo, A, B, B1, C, part, inv, end; };
+Offsets offsets(const ah_muon_matrix_t& x, int n, int k, bool pair, uint64_t at) {
   Offsets o;
   auto take = [&](uint64_t bytes) { const uint64_t r = at; at += up(bytes, 256); return r; };
   const uint64_t nk = (uint64_t)n * k, nn = (uint64_t)n * n;
   o.hi0 = take(2 * nk); o.hi1 = take(2 * nk); o.lo = take(2 * nk);
   o.A = take(2 * nn); o.B = take(2 * nn);
+  o.B1 = take(pair ? 2 * nn : 0); o.C = take(pair ? 2 * nn : 0);
   o.part = take(8 * (up(x.rows, kPiece) / kPiece) * (up(x.cols, kPiece) / kPiece));
   o.inv = take(8);
   o.end = at;
@@ -667,12 +690,12 @@ std::vector<Group> plan(const ah_muon_matrix_t* x, int n) {
     elements += own;
   }
   for (Group& g : groups) {
-    g.tile = tile_of(x, g.which);
+    choose(x, g);
     g.bytes = 0;
     for (int i : g.which) {
       g.n.push_back((int)up(small_side(x[i]), std::max(g.tile, 128)));       // (the products' k axis: a multiple of 128)
       g.k.push_back((int)up(large_side(x[i]), std::max(g.tile, 128)));
-      g.bytes = offsets(x[i], g.n.back(), g.k.back(), g.bytes).end;
+      g.bytes = offsets(x[i], g.n.back(), g.k.back(), g.pair, g.bytes).end;
     }
   }
   return groups;
@@ -702,31 +725,46 @@ hipError_t launch(Table& t, const Group& g, const F& blocks_of, const G& go) {
   return hipGetLastError();
 }
 
+// last: which of its two places X is in behind the last step
 template <int S>
-hipError_t products(const Table& t, const Group& g, int steps, hipStream_t s) {
+hipError_t products(const Table& t, const Group& g, int steps, int* last, hipStream_t s) {
   const Kind& kind = S == 64 ? kKinds[0] : S == 128 ? kKinds[1] : kKinds[2];
-  Deal deals[3];
+  Deal deals[3];                                   // of X X^T, of n x n x n, of the STEP
   uint32_t blocks[3];
-  for (Product p : {SYM_A, SYM_B, STEP}) {
-    blocks[p] = deal(p, t, (int)g.which.size(), kind, deals[p]);
-    if (blocks[p] > (1u << 23)) return hipErrorInvalidValue;
+  for (int i = 0; i < 3; i++) {
+    blocks[i] = deal(i == 0 ? SYM_A : i == 1 ? SYM_B : STEP, t, (int)g.which.size(), kind, deals[i]);
+    if (blocks[i] > (1u << 23)) return hipErrorInvalidValue;
   }
-  auto product = [&](auto kind_of, int from) {
+  hipError_t e = hipSuccess;
+  auto product = [&](auto kind_of, int how) {
     constexpr Product P = decltype(kind_of)::value;
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(blocks[P]), dim3(NT), 0, s, t, deals[P], from); };
+    constexpr int at = P == SYM_A ? 0 : P == STEP ? 2 : 1;
+    if (e != hipSuccess) return;
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(blocks[at]), dim3(NT), 0, s, t, deals[at], how); };
     if constexpr (S == 64) go(small_product_kernel<P>);
     else if constexpr (S == 256) go(product_kernel<S, P, 2>);
-    else if (blocks[P] <= 256) go(product_kernel<S, P, 3>);
+    else if (blocks[at] <= 256) go(product_kernel<S, P, 3>);
     else go(product_kernel<S, P, 2>);
-    return hipGetLastError();
+    e = hipGetLastError();
   };
-  for (int i = 0; i < steps; i++) {
-    hipError_t e = product(std::integral_constant<Product, SYM_A>(), i & 1);
-    if (e == hipSuccess) e = product(std::integral_constant<Product, SYM_B>(), i & 1);
-    if (e == hipSuccess) e = product(std::integral_constant<Product, STEP>(), i & 1);
-    if (e != hipSuccess) return e;
+  int from = 0;
+  for (int i = 0; i < steps; i++, from ^= 1) {
+    const bool pair = S > 64 && g.pair && i == 0 && steps > 1;
+    product(std::integral_constant<Product, SYM_A>(), from);
+    product(std::integral_constant<Product, SYM_B>(), from);
+    if constexpr (S > 64) {
+      if (pair) {
+        product(std::integral_constant<Product, SYM_C>(), from);
+        product(std::integral_constant<Product, SYM_D>(), from);
+        product(std::integral_constant<Product, SYM_B>(), from | kPair);
+        product(std::integral_constant<Product, SYM_Q>(), from);
+        i++;
+      }
+    }
+    product(std::integral_constant<Product, STEP>(), pair ? from | kPair : from);
   }
-  return hipSuccess;
+  *last = from;
+  return e;
 }
 
 hipError_t step_group(const ah_muon_t* c, const ah_muon_matrix_t* x, const Group& g, char* work, bool master, hipStream_t s) {
@@ -734,13 +772,13 @@ hipError_t step_group(const ah_muon_t* c, const ah_muon_matrix_t* x, const Group
   uint64_t at = 0;
   for (size_t i = 0; i < g.which.size(); i++) {
     const ah_muon_matrix_t& y = x[g.which[i]];
-    const Offsets o = offsets(y, g.n[i], g.k[i], at);
+    const Offsets o = offsets(y, g.n[i], g.k[i], g.pair, at);
     Matrix& e = t.e[i];
     e.p = y.param; e.g = y.grad; e.m = y.momentum; e.master = y.master;
     e.hi[0] = (f16*)(work + o.hi0); e.hi[1] = (f16*)(work + o.hi1); e.lo = (f16*)(work + o.lo);
-    e.A = (f16*)(work + o.A); e.B = (f16*)(work + o.B); e.part = (double*)(work + o.part); e.inv = (double*)(work + o.inv);
-    e.ld_p = y.ld_param ? y.ld_param : y.cols; e.ld_g = y.ld_grad ? y.ld_grad : y.cols;
-    e.ld_m = y.ld_momentum ? y.ld_momentum : y.cols; e.ld_master = y.ld_master ? y.ld_master : y.cols;
+    e.A = (f16*)(work + o.A); e.B = (f16*)(work + o.B); e.B1 = (f16*)(work + o.B1); e.C = (f16*)(work + o.C); e.part = (double*)(work + o.part); e.inv = (double*)(work + o.inv);
+    auto stride = [&](int64_t ld) { return (uint32_t)(ld ? ld : y.cols); };       // (at most 2^31)
+    e.ld_p = stride(y.ld_param); e.ld_g = stride(y.ld_grad); e.ld_m = stride(y.ld_momentum); e.ld_master = stride(y.ld_master);
     e.rows = (int)y.rows; e.cols = (int)y.cols; e.n = g.n[i]; e.k = g.k[i];
     e.wd = y.weight_decay; e.scale = y.scale;
     const int pb = c->param_type == AH_FP32 ? 4 : 2, gb = c->grad_type == AH_FP32 ? 4 : 2;
@@ -763,10 +801,10 @@ hipError_t step_group(const ah_muon_t* c, const ah_muon_matrix_t* x, const Group
       if (g32) hipLaunchKernelGGL(lay_out_kernel<float>, dim3(b), dim3(NT), 0, s, t, h);
       else hipLaunchKernelGGL(lay_out_kernel<bf16>, dim3(b), dim3(NT), 0, s, t, h);
     });
-  if (e == hipSuccess) e = g.tile == 256 ? products<256>(t, g, c->ns_steps, s) : g.tile == 128 ? products<128>(t, g, c->ns_steps, s) : products<64>(t, g, c->ns_steps, s);
+  int last = 0;
+  if (e == hipSuccess) e = g.tile == 256 ? products<256>(t, g, c->ns_steps, &last, s) : g.tile == 128 ? products<128>(t, g, c->ns_steps, &last, s) : products<64>(t, g, c->ns_steps, &last, s);
   if (e == hipSuccess)
     e = launch(t, g, pieces, [&](uint32_t b) {
-      const int last = c->ns_steps & 1;
       if (c->param_type == AH_FP32) hipLaunchKernelGGL((apply_kernel<float, false>), dim3(b), dim3(NT), 0, s, t, h, last);
       else if (master) hipLaunchKernelGGL((apply_kernel<bf16, true>), dim3(b), dim3(NT), 0, s, t, h, last);
       else hipLaunchKernelGGL((apply_kernel<bf16, false>), dim3(b), dim3(NT), 0, s, t, h, last);

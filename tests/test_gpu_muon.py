@@ -26,18 +26,27 @@ def normed(u, eps):
     return x / (torch.linalg.matrix_norm(x) + eps)
 
 
-def orthogonal(u, eps=1e-7, steps=5):
-    """The polynomial of u in 64 bits, and the same with the kernel's roundings (operands in fp16, X as two fp16 numbers) of sums in 64 bits."""
+def orthogonal(u, eps=1e-7, steps=5, pair=False):
+    """The polynomial of u in 64 bits, and the same with the kernel's roundings (operands in fp16, X as two fp16 numbers) of sums in 64 bits.  pair: with the first two steps at
+    once, (a + B1)(a + B) = a^2 + Q, in which the second step's A is (a + B) A (a + B)."""
     x = y = normed(u, eps)
     f16 = lambda t: t.half().double()                  # noqa: E731
     split = lambda t: (f16(64 * t), f16((64 * t - f16(64 * t)) * 2048))   # noqa: E731
     hi, lo = split(y.float().double())
-    for _ in range(steps):
+    mirrored = lambda t: t.tril() + t.tril(-1).T       # noqa: E731
+    for k in range(steps):
         q = x @ x.T.contiguous()
         x = A * x + (B * q + C * (q @ q)) @ x
-        a = f16(hi @ hi.T.contiguous() / 4)
+        if pair and k == 1:
+            continue
+        a, by = f16(hi @ hi.T.contiguous() / 4), A
         b = f16(B * a + C * (a @ a) / 1024)
-        y = (A * (hi + lo / 2048) + b @ hi / 1024) / 64
+        if pair and k == 0 and steps > 1:
+            c = mirrored(f16(b @ a / 1024))
+            a = mirrored(f16(A * A * a + 2 * A * c + b @ c / 1024))
+            b1 = f16(B * a + C * (a @ a) / 1024)
+            b, by = mirrored(f16(A * (b + b1) + b1 @ b / 1024)), A * A
+        y = (by * (hi + lo / 2048) + b @ hi / 1024) / 64
         hi, lo = split(y)
     turn = (lambda t: t) if u.shape[0] <= u.shape[1] else (lambda t: t.T)
     return turn(x), turn((hi + lo / 2048) / 64)
@@ -99,8 +108,23 @@ def test_tiles_of_a_large_call_and_matrices_of_unlike_sizes():
         gs = [randn(k, r, c, std=10.0 ** (k % 5 - 2)) for k, (r, c) in enumerate(shapes)]
         xs, _ = update_of(gs)
         for k in {0, len(gs) // 2, len(gs) - 3, len(gs) - 2, len(gs) - 1} & set(range(len(gs))):
-            want, rounded = orthogonal(gs[k] * 0.05 * 1.95)
-            assert norm(xs[k].double() - want) <= room_of(want, rounded), (k, shapes[k])
+            room = max(room_of(*orthogonal(gs[k] * 0.05 * 1.95, pair=pair)) for pair in (False, True))       # (sizes decide, here of either kind)
+            want, _ = orthogonal(gs[k] * 0.05 * 1.95)
+            assert norm(xs[k].double() - want) <= room, (k, shapes[k])
+
+
+@pytest.mark.parametrize("make", [randn, low_rank])
+@pytest.mark.parametrize("shapes,steps", [([(2048, 8000)], 5), ([(9000, 1500)] * 2 + [(1500, 5000)], 5), ([(700, 2500)] * 12, 5), ([(700, 2500)] * 12, 2), ([(700, 2500)] * 12, 3), ([(2304, 9000)] * 2, 4)])
+def test_many_more_columns_than_rows(shapes, steps, make):
+    """Where the first two steps are taken at once"""
+    gs = [make(3 * k, r, c) for k, (r, c) in enumerate(shapes)]
+    xs, opt = update_of(gs, ns_steps=steps)
+    n = sum(min(s) ** 2 for s in shapes)
+    assert opt._work.numel() > sum(6 * g.numel() for g in gs) + 8 * n          # (the two square matrices more that this takes)
+    for k in {0, len(gs) - 1}:
+        want, rounded = orthogonal(gs[k] * 0.05 * 1.95, steps=steps, pair=True)
+        print(shapes[k], steps, "off by %.2g, the rounded form by %.2g, of %.2g" % (norm(xs[k].double() - want), norm(rounded - want), norm(want)))
+        assert norm(xs[k].double() - want) <= room_of(want, rounded), (k, shapes[k])
 
 
 @pytest.mark.parametrize("steps", [1, 2, 5, 9])

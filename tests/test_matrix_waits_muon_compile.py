@@ -17,5 +17,5 @@ def test_wait_states_around_matrix_instructions(tmp_path):
     text = asm.read_text()
     kernels = re.findall(r"^(\S*14product_kernel\S+):[^\n]*\n(.*?)\.Lfunc_end", text, re.S | re.M)
     backs = [_check(*k) for k in kernels]
-    assert len(backs) == 9 and all(n for n in backs)              # three products in tiles of 256, and of 128 with two ring depths
+    assert len(backs) == 18 and all(n for n in backs)             # six products in tiles of 256, and of 128 with two ring depths
     assert "v_mfma_f32_16x16x32_f16" in text and "_bf16 a[" not in text
