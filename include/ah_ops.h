@@ -155,7 +155,8 @@ int ah_rope_table(float* cos_sin, int n_pos, int head_dim, double base, void* hi
  *   ns_steps times: A = X X^T; X = a X + (b A + c A A) X, (a, b, c) = (3.4445, -4.7750, 2.0315), which brings the singular values of 1 / 500 and more to 0.68 .. 1.21;
  *   p = p (1 - lr weight_decay) - lr scale X.
  * Momentum, norm, update in fp32 (the sum of squares in fp64).  X is kept between the products in 22 bits (two fp16 numbers); the products' operands are fp16
- * (11 bits; X, A and b A + c A A are at most 3 in magnitude whatever u is), their sums fp32.  bf16 parameters without a master copy are rounded to nearest after every step. */
+ * (11 bits; all of them are at most 12 in magnitude whatever u is), their sums fp32.  With parameters or master copies in fp32, matrices of at most 256 rows or columns have
+ * operands of 22 bits too.  Where that is fewer products, the first two steps are taken at once.  bf16 parameters without a master copy are rounded to nearest after every step. */
 typedef struct {
   void* param;          /* [rows, cols], bf16 or fp32: ah_muon_t.param_type */
   const void* grad;     /* bf16 or fp32: ah_muon_t.grad_type */
@@ -179,7 +180,7 @@ typedef struct {
 
 /* matrices: HOST array, read during the call.  What a call writes overlaps nothing else that it reads or writes (columns of a wider matrix beside each other do not).
  * A matrix whose momentum is or becomes infinite or NaN is NaN behind the step; the others are not touched by it.  workspace: device, 256-byte aligned, of the size that
- * ah_muon_workspace gives for these matrices (which looks at rows and cols only): the largest group of matrices that are worked on together. */
+ * ah_muon_workspace gives for these matrices (which looks at rows and cols only, so that it is enough for all types): the largest group of matrices that are worked on together. */
 int ah_muon_step(const ah_muon_t* cfg, const ah_muon_matrix_t* matrices, int n_matrices, void* workspace, void* hip_stream);
 int ah_muon_workspace(const ah_muon_matrix_t* matrices, int n_matrices, uint64_t* bytes);
 

@@ -367,9 +367,11 @@ __device__ __forceinline__ void first_step(const char* __restrict__ cur, int ks,
 }
 
 // The whole loop where each of four waves takes one k-step in four of the whole tile, over one piece of the k axis (K a multiple of 128): acc are the wave's partial sums.
-// The wave's redundant tail loads are still in flight behind it.
-template <int BM, int BN, bool AKS, bool BKS, bool F16>
-__device__ __forceinline__ void run(const char* gA, const char* gB, int lda, int ldb, int K, char* ring, f32x16 (&acc)[BM / 32][BN / 32], int wave, int lane) {
+// The wave's redundant tail loads are still in flight behind it.  PARTS products of the same sizes can follow each other into the same sums without a pause; in front of the last
+// of them the sums are multiplied by `factor`.
+template <int BM, int BN, bool AKS, bool BKS, bool F16, int PARTS = 1>
+__device__ __forceinline__ void run(const char* const (&gA)[PARTS], const char* const (&gB)[PARTS], int lda, int ldb, int K, char* ring, f32x16 (&acc)[BM / 32][BN / 32], int wave,
+                                    int lane, float factor = 1.f) {
   constexpr int STAGE = stage_bytes<BM, BN>(), NS = stages<BM, BN>(), NW = 4, LA = BM / 8 / NW, LB = BN / 8 / NW, LPS = LA + LB;
   const size_t stepA = (AKS ? (size_t)BK * lda : (size_t)BK) * 2, stepB = (BKS ? (size_t)BK * ldb : (size_t)BK) * 2;   // bytes per k-block
   uint32_t offA[LA], offB[LB];
@@ -379,11 +381,22 @@ __device__ __forceinline__ void run(const char* gA, const char* gB, int lda, int
   for (int i = 0; i < LB; i++) offB[i] = loader_src_offset<BK, BN, BKS, true>(wave + NW * i, lane, ldb);
   // The stage to be fetched next; past the last one that stage is fetched again into dead slots, which keeps the number of loads in flight uniform for the counted wait.
   const int nk = K / BK;
-  const char *pA = gA, *pB = gB;
-  int fetched = 1;
+  const char *pA = gA[0], *pB = gB[0];
+  int fetched = 1, part = 0;
   auto advance = [&]() {
-    const bool more = fetched < nk;
+    bool more = fetched < nk;
     fetched++;
+    if constexpr (PARTS > 1) {
+      if (!more && part < PARTS - 1) {
+        part++;
+#pragma unroll
+        for (int i = 1; i < PARTS; i++) {
+          if (part == i) { pA = gA[i]; pB = gB[i]; }
+        }
+        fetched = 1;
+        return;
+      }
+    }
     pA = more ? pA + stepA : pA;
     pB = more ? pB + stepB : pB;
   };
@@ -398,8 +411,16 @@ __device__ __forceinline__ void run(const char* gA, const char* gB, int lda, int
   Frags<BK, BM, BN, 1, 1, AKS, BKS> f0, f1;
   f0.load(ring, ring + BM * 2 * BK, wave, 0, 0, lane);
   int c = 0;  // ring slot of k-block j
-  for (int j = 0; j < nk; j += 2) {
+  for (int j = 0; j < PARTS * nk; j += 2) {
     const int n = c + 1 == NS ? 0 : c + 1, n2 = n + 1 == NS ? 0 : n + 1;
+    if constexpr (PARTS > 1) {
+      if (j == (PARTS - 1) * nk) {
+#pragma unroll
+        for (int tm = 0; tm < BM / 32; tm++)
+#pragma unroll
+          for (int tn = 0; tn < BN / 32; tn++) acc[tm][tn] *= factor;
+      }
+    }
     __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0((NS - 2) * LPS));
     __builtin_amdgcn_s_barrier();
     last_step<BM, BN, 1, 1, AKS, BKS, F16>(pA, pB, offA, offB, ring + c * STAGE, ring + n * STAGE, wave, f0, f1, acc, wave, 0, 0, lane);

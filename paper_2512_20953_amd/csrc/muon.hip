@@ -13,7 +13,8 @@
 // below 1.21), its range suffices, and it
 // keeps 11 bits where bf16 keeps 8, at the same rate.  X itself goes from product to product in 22 bits, as two fp16 numbers: what is added to a X has to be added to the same X
 // that it was computed from, or the rounding of every step is taken for a part of X, which the polynomial multiplies by up to 3.44 a step where singular values are small.  Of a
-// matrix with 64 strong directions above a floor of noise (1024 x 2816) the factor is 5e-4 off in norm, with X in fp16 alone 2e-2, in bf16 alone 0.18.  Fixed powers of two keep small
+// matrix with 64 strong directions above a floor of noise (1024 x 2816) the factor is 5e-4 off in norm, with X in fp16 alone 2e-2, in bf16 alone 0.18.  Small matrices of fp32
+// parameters have all operands in 22 bits (FINE).  Fixed powers of two keep small
 // elements out of fp16's subnormals: kX on X, kA on A and B, kLo more on X's lower half.
 #include "ah_ops.h"
 #include "capi_util.h"
@@ -37,6 +38,7 @@ constexpr int NT = 256;
 constexpr int64_t kMaxSmall = 32768, kMaxLarge = 131072;
 constexpr int kTable = 24;                                                // matrices of a launch
 constexpr uint64_t kGroupElements = 1ull << 28;                           // of a group, where it holds more than one matrix
+constexpr int kFine = 256;                                                // see small_product_kernel
 constexpr int kPiece = 64;                                                // side of the blocks of the element-wise passes
 
 struct Matrix {
@@ -47,6 +49,10 @@ struct Matrix {
   double *part, *inv;          // sums of squares of the pieces; 1 / (norm + eps)
   uint32_t ld_p, ld_g, ld_m, ld_master;
   int rows, cols, n, k;        // n x k: the padded X
+  // of a fine group: the lower halves of A, B, and of X in either of its places (elsewhere these are B1 and C, and the lower half of X has one place)
+  __host__ __device__ f16* a_lo() const { return B1; }
+  __host__ __device__ f16* b_lo() const { return C; }
+  __host__ __device__ f16* x_lo(int fine_and_place) const { return lo + (fine_and_place == 3 ? (size_t)n * k : 0); }
   float wd, scale;
   int aligned;                 // rows of all four begin at whole multiples of 4 elements
 };
@@ -255,7 +261,7 @@ __device__ __forceinline__ void apply_piece(const Matrix& e, int64_t r0, int64_t
 #pragma unroll
         for (int j = 0; j < V; j++) x[i][j] = turned[s][col + j];
       } else {                                               // (X is padded to whole pieces)
-        const wide_t<f16, V> hi = load_wide<V>((const f16*)e.hi[last] + (r0 + s) * e.k + c0 + col), lo = load_wide<V>((const f16*)e.lo + (r0 + s) * e.k + c0 + col);
+        const wide_t<f16, V> hi = load_wide<V>((const f16*)e.hi[last & 1] + (r0 + s) * e.k + c0 + col), lo = load_wide<V>((const f16*)e.x_lo(last) + (r0 + s) * e.k + c0 + col);
 #pragma unroll
         for (int j = 0; j < V; j++) x[i][j] = (float)hi[j] + (float)lo[j] * (1.f / kLo);
       }
@@ -294,7 +300,7 @@ __global__ __launch_bounds__(NT) void apply_kernel(Table t, Hyper h, int last) {
     for (int turn = 0; turn < W::kTurns; turn++) {
       const int s = row + turn * W::kRows;
       const int64_t at = (c0 + s) * e.k + r0 + col;
-      const wide_t<f16, 4> hi = load_wide<4>((const f16*)e.hi[last] + at), lo = load_wide<4>((const f16*)e.lo + at);
+      const wide_t<f16, 4> hi = load_wide<4>((const f16*)e.hi[last & 1] + at), lo = load_wide<4>((const f16*)e.x_lo(last) + at);
 #pragma unroll
       for (int j = 0; j < 4; j++) turned[col + j][s] = (float)hi[j] + (float)lo[j] * (1.f / kLo);
     }
@@ -369,24 +375,24 @@ __device__ __forceinline__ void find_job(const Matrix& e, int tile, int how, Job
 
 // What 8 elements of a result from (row, col) on need beside their sums: the two halves of X, or one or two of the square matrices.  Asked for ahead: the compiler would not
 // move these loads over the stores of the elements before.
-template <Product P> constexpr int beside() { return P == SYM_A || P == SYM_C ? 0 : P == SYM_B ? 1 : 2; }
+template <Product P, bool FINE = false> constexpr int beside() { return P == SYM_A || P == SYM_C ? 0 : P == SYM_B && !FINE ? 1 : 2; }
 struct Beside { f16x8 u, v; };
-template <Product P>
+template <Product P, bool FINE = false>
 __device__ __forceinline__ Beside ask8(const Matrix& e, int how, int row, int col) {
   Beside x = {};
   const size_t at = (size_t)row * (P == STEP ? e.k : e.n) + col;
-  const f16 *u = P == STEP ? e.hi[how & 1] : P == SYM_Q ? e.B : e.A, *v = P == STEP ? e.lo : P == SYM_Q ? e.B1 : e.C;
-  if constexpr (beside<P>() > 0) x.u = *(const f16x8*)(u + at);
-  if constexpr (beside<P>() > 1) x.v = *(const f16x8*)(v + at);
+  const f16 *u = P == STEP ? e.hi[how & 1] : P == SYM_Q ? e.B : e.A, *v = P == STEP ? e.x_lo(FINE ? 2 | how : 0) : P == SYM_Q ? e.B1 : FINE ? e.a_lo() : e.C;
+  if constexpr (beside<P, FINE>() > 0) x.u = *(const f16x8*)(u + at);
+  if constexpr (beside<P, FINE>() > 1) x.v = *(const f16x8*)(v + at);
   return x;
 }
 // ... and those elements, whose sums are v
-template <Product P>
+template <Product P, bool FINE = false>
 __device__ __forceinline__ void put8(const Matrix& e, int how, int row, int col, const float (&v)[8], const Beside& x) {
   f16x8 o;
   if constexpr (P == STEP) {
     f16x8 ol;
-    const float a = how & kPair ? kA_ * kA_ : kA_;
+    const float a = how & kPair && !FINE ? kA_ * kA_ : kA_;
 #pragma unroll
     for (int j = 0; j < 8; j++) {
       f16 hi, lo;
@@ -395,7 +401,18 @@ __device__ __forceinline__ void put8(const Matrix& e, int how, int row, int col,
       ol[j] = lo;
     }
     *(f16x8*)(e.hi[(how & 1) ^ 1] + (size_t)row * e.k + col) = o;
-    *(f16x8*)(e.lo + (size_t)row * e.k + col) = ol;
+    *(f16x8*)(e.x_lo(FINE ? 2 | (how ^ 1) : 0) + (size_t)row * e.k + col) = ol;
+  } else if constexpr (FINE) {
+    f16x8 ol;
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+      f16 hi, lo;
+      split(P == SYM_A ? v[j] * (kA / (kX * kX)) : __builtin_fmaf(kB_, (float)x.u[j] + (float)x.v[j] * (1.f / kLo), v[j] * (kC_ / kA)), hi, lo);
+      o[j] = hi;
+      ol[j] = lo;
+    }
+    *(f16x8*)((P == SYM_A ? e.A : e.B) + (size_t)row * e.n + col) = o;
+    *(f16x8*)((P == SYM_A ? e.a_lo() : e.b_lo()) + (size_t)row * e.n + col) = ol;
   } else {
 #pragma unroll
     for (int j = 0; j < 8; j++) {
@@ -493,7 +510,10 @@ __global__ __launch_bounds__(NT) void product_kernel(Table t, Deal d, int how) {
 }
 
 // The same for few tiles: 64 x 64, each wave one k-step in four of the whole tile.  Four times the blocks, whose chains of k-steps are a quarter as long.
-template <Product P>
+// FINE: where the smaller side is at most kFine and the parameters are kept in fp32, all operands are kept in 22 bits, and three products stand for one (upper by lower half, lower by
+// upper, upper by upper: what is left out is 2^-22): of matrices that small operands in 11 bits leave the factor 1e-3 to 3e-3 off, now 1e-6 to 5e-6.  A launch takes 10 to 13.5 us
+// instead of 7 to 9 (8 matrices of 256 x 256 .. 1024, a whole step 188 instead of 129); larger ones would take up to three times as long and are less far off.
+template <Product P, bool FINE>
 __global__ __launch_bounds__(NT) void small_product_kernel(Table t, Deal d, int how) {
   constexpr int S = 64, ROWB = S * 4 + 16, STRIP = S * ROWB;
   constexpr int RING = ksplit::stages<S, S>() * ksplit::stage_bytes<S, S>();
@@ -513,17 +533,26 @@ __global__ __launch_bounds__(NT) void small_product_kernel(Table t, Deal d, int 
     for (int j = 0; j < 2; j++)
 #pragma unroll
       for (int r = 0; r < 16; r++) acc[i][j][r] = 0.f;
-  ksplit::run<S, S, false, P == STEP, true>((const char*)g.a, (const char*)g.b, g.lda, g.ldb, g.K, ring, acc, wave, lane);
+  const char *a = (const char*)g.a, *b = (const char*)g.b;
+  if constexpr (FINE) {
+    // (the lower halves are laid out like the upper ones)
+    const f16 *xl = e.x_lo(2 | how), *l = P == SYM_A ? xl : P == SYM_B ? e.a_lo() : e.b_lo(), *r = P == SYM_B ? e.a_lo() : xl;
+    const f16 *lh = P == SYM_A ? e.hi[how] : P == SYM_B ? e.A : e.B, *rh = P == SYM_B ? e.A : e.hi[how];
+    const char *al = (const char*)(l + (g.a - lh)), *bl = (const char*)(r + (g.b - rh));
+    ksplit::run<S, S, false, P == STEP, true, 3>({a, al, a}, {bl, b, b}, g.lda, g.ldb, g.K, ring, acc, wave, lane, 1.f / kLo);
+  } else {
+    ksplit::run<S, S, false, P == STEP, true>({a}, {b}, g.lda, g.ldb, g.K, ring, acc, wave, lane);
+  }
   __builtin_amdgcn_s_waitcnt(0);
   // a wave writes 16 of the rows, and as many columns across the diagonal
   const int row0 = wave * 16 + lane / 8, cp = lane % 8;
   Beside x[2], xt[2] = {};
 #pragma unroll
-  for (int it = 0; it < 2; it++) x[it] = ask8<P>(e, how, g.m0 + row0 + it * 8, g.n0 + cp * 8);
-  if constexpr (P != STEP && beside<P>() > 0) {
+  for (int it = 0; it < 2; it++) x[it] = ask8<P, FINE>(e, how, g.m0 + row0 + it * 8, g.n0 + cp * 8);
+  if constexpr (P != STEP && beside<P, FINE>() > 0) {
     if (g.ti != g.tj) {
 #pragma unroll
-      for (int r = 0; r < 2; r++) xt[r] = ask8<P>(e, how, g.n0 + lane, g.m0 + wave * 16 + r * 8);
+      for (int r = 0; r < 2; r++) xt[r] = ask8<P, FINE>(e, how, g.n0 + lane, g.m0 + wave * 16 + r * 8);
     }
   }
   __syncthreads();
@@ -547,7 +576,7 @@ __global__ __launch_bounds__(NT) void small_product_kernel(Table t, Deal d, int 
 #pragma unroll
     for (int w = 1; w < 4; w++) { v0 += *(const f32x4*)(q + w * STRIP); v1 += *(const f32x4*)(q + w * STRIP + 16); }
     const float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-    put8<P>(e, how, g.m0 + row, g.n0 + cp * 8, v, x[it]);
+    put8<P, FINE>(e, how, g.m0 + row, g.n0 + cp * 8, v, x[it]);
   }
   if constexpr (P != STEP) {
     if (g.ti != g.tj) {
@@ -561,7 +590,7 @@ __global__ __launch_bounds__(NT) void small_product_kernel(Table t, Deal d, int 
 #pragma unroll
           for (int w = 1; w < 4; w++) v[j] += *(const float*)(q + w * STRIP);
         }
-        put8<P>(e, how, g.n0 + lane, g.m0 + wave * 16 + r * 8, v, xt[r]);
+        put8<P, FINE>(e, how, g.n0 + lane, g.m0 + wave * 16 + r * 8, v, xt[r]);
       }
     }
   }
@@ -573,7 +602,7 @@ uint64_t up(uint64_t n, uint64_t to) { return (n + to - 1) / to * to; }
 struct Group {
   std::vector<int> which;      // of the call's matrices
   int tile;
-  bool pair;
+  bool pair, fine;
   std::vector<int> n, k;       // padded
   uint64_t bytes;
 };
@@ -610,6 +639,9 @@ double time_of(Product p, const ah_muon_matrix_t* x, const std::vector<int>& whi
 // Five steps, apart and at once, us: a LLaMA-style layer 14830, 14130; 4 of 2048 x 8192 2924, 2651; one 5120 x 20480 8270, 7269; 4 of 1536 x 4608 1158, 1079; one 4096 x 6144
 // 2329, 2326; one 4096 x 4096 1558, 1627; 24 of 1024 x 1024 1323, 1443.  Tiles of 64 never take it: their products are bound by the launches, of which it has one more.
 void choose(const ah_muon_matrix_t* x, Group& g) {
+  g.tile = 64;
+  g.pair = false;
+  if (g.fine) return;
   double least = 0;
   for (const Kind& k : kKinds) {
     const double a = time_of(SYM_A, x, g.which, k), b = time_of(SYM_B, x, g.which, k), step = time_of(STEP, x, g.which, k);
@@ -660,30 +692,33 @@ uint32_t deal(Product p, const Table& t, int n, const Kind& kind, Deal& d) {
 }
 
 struct Offsets { uint64_t hi0, hi1, lo, A, B, B1, C, part, inv, end; };
-Offsets offsets(const ah_muon_matrix_t& x, int n, int k, bool pair, uint64_t at) {
+Offsets offsets(const ah_muon_matrix_t& x, int n, int k, const Group& g, uint64_t at) {
   Offsets o;
   auto take = [&](uint64_t bytes) { const uint64_t r = at; at += up(bytes, 256); return r; };
   const uint64_t nk = (uint64_t)n * k, nn = (uint64_t)n * n;
-  o.hi0 = take(2 * nk); o.hi1 = take(2 * nk); o.lo = take(2 * nk);
+  o.hi0 = take(2 * nk); o.hi1 = take(2 * nk); o.lo = take(g.fine ? 4 * nk : 2 * nk);
   o.A = take(2 * nn); o.B = take(2 * nn);
-  o.B1 = take(pair ? 2 * nn : 0); o.C = take(pair ? 2 * nn : 0);
+  o.B1 = take(g.pair || g.fine ? 2 * nn : 0); o.C = take(g.pair || g.fine ? 2 * nn : 0);
   o.part = take(8 * (up(x.rows, kPiece) / kPiece) * (up(x.cols, kPiece) / kPiece));
   o.inv = take(8);
   o.end = at;
   return o;
 }
 
-std::vector<Group> plan(const ah_muon_matrix_t* x, int n) {
+// kept32: what is stepped is kept in 32 bits, so that the small matrices' groups are fine ones
+std::vector<Group> plan(const ah_muon_matrix_t* x, int n, bool kept32) {
   std::vector<int> order;
   for (int i = 0; i < n; i++)
     if (x[i].rows && x[i].cols) order.push_back(i);
-  std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return x[a].rows * x[a].cols > x[b].rows * x[b].cols; });
+  auto fine = [&](int i) { return kept32 && small_side(x[i]) <= kFine; };
+  std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return fine(a) != fine(b) ? fine(b) : x[a].rows * x[a].cols > x[b].rows * x[b].cols; });
   std::vector<Group> groups;
   uint64_t elements = 0;
   for (int i : order) {
     const uint64_t own = up(small_side(x[i]), 256) * up(large_side(x[i]), 256);
-    if (groups.empty() || (int)groups.back().which.size() == kTable || elements + own > kGroupElements) {
+    if (groups.empty() || (int)groups.back().which.size() == kTable || elements + own > kGroupElements || groups.back().fine != fine(i)) {
       groups.push_back({});
+      groups.back().fine = fine(i);
       elements = 0;
     }
     groups.back().which.push_back(i);
@@ -695,7 +730,7 @@ std::vector<Group> plan(const ah_muon_matrix_t* x, int n) {
     for (int i : g.which) {
       g.n.push_back((int)up(small_side(x[i]), std::max(g.tile, 128)));       // (the products' k axis: a multiple of 128)
       g.k.push_back((int)up(large_side(x[i]), std::max(g.tile, 128)));
-      g.bytes = offsets(x[i], g.n.back(), g.k.back(), g.pair, g.bytes).end;
+      g.bytes = offsets(x[i], g.n.back(), g.k.back(), g, g.bytes).end;
     }
   }
   return groups;
@@ -725,7 +760,7 @@ hipError_t launch(Table& t, const Group& g, const F& blocks_of, const G& go) {
   return hipGetLastError();
 }
 
-// last: which of its two places X is in behind the last step
+// last: which of its two places X is in behind the last step, and 2 of a fine group
 template <int S>
 hipError_t products(const Table& t, const Group& g, int steps, int* last, hipStream_t s) {
   const Kind& kind = S == 64 ? kKinds[0] : S == 128 ? kKinds[1] : kKinds[2];
@@ -741,7 +776,7 @@ hipError_t products(const Table& t, const Group& g, int steps, int* last, hipStr
     constexpr int at = P == SYM_A ? 0 : P == STEP ? 2 : 1;
     if (e != hipSuccess) return;
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(blocks[at]), dim3(NT), 0, s, t, deals[at], how); };
-    if constexpr (S == 64) go(small_product_kernel<P>);
+    if constexpr (S == 64) g.fine ? go(small_product_kernel<P, true>) : go(small_product_kernel<P, false>);
     else if constexpr (S == 256) go(product_kernel<S, P, 2>);
     else if (blocks[at] <= 256) go(product_kernel<S, P, 3>);
     else go(product_kernel<S, P, 2>);
@@ -763,7 +798,7 @@ hipError_t products(const Table& t, const Group& g, int steps, int* last, hipStr
     }
     product(std::integral_constant<Product, STEP>(), pair ? from | kPair : from);
   }
-  *last = from;
+  *last = g.fine ? 2 | from : from;
   return e;
 }
 
@@ -772,7 +807,7 @@ hipError_t step_group(const ah_muon_t* c, const ah_muon_matrix_t* x, const Group
   uint64_t at = 0;
   for (size_t i = 0; i < g.which.size(); i++) {
     const ah_muon_matrix_t& y = x[g.which[i]];
-    const Offsets o = offsets(y, g.n[i], g.k[i], g.pair, at);
+    const Offsets o = offsets(y, g.n[i], g.k[i], g, at);
     Matrix& e = t.e[i];
     e.p = y.param; e.g = y.grad; e.m = y.momentum; e.master = y.master;
     e.hi[0] = (f16*)(work + o.hi0); e.hi[1] = (f16*)(work + o.hi1); e.lo = (f16*)(work + o.lo);
@@ -819,7 +854,8 @@ extern "C" int ah_muon_workspace(const ah_muon_matrix_t* x, int n, uint64_t* byt
   if (int rc = check_list("ah_muon_workspace", x, n)) return rc;
   try {
     *bytes = 256;
-    for (const Group& g : plan(x, n)) *bytes = std::max(*bytes, g.bytes);
+    for (bool kept32 : {false, true})
+      for (const Group& g : plan(x, n, kept32)) *bytes = std::max(*bytes, g.bytes);
   } catch (...) {
     return set_error(AH_ENOMEM, "ah_muon_workspace: no host memory");
   }
@@ -857,7 +893,7 @@ extern "C" int ah_muon_step(const ah_muon_t* c, const ah_muon_matrix_t* x, int n
   if (!any) return AH_OK;
   if (!workspace || !aligned_to(workspace, 256)) return set_error(AH_EINVAL, "%s: workspace is NULL or not 256-byte aligned", who);
   try {
-    for (const Group& g : plan(x, n)) {
+    for (const Group& g : plan(x, n, master || pb == 4)) {
       const hipError_t e = step_group(c, x, g, (char*)workspace, master, (hipStream_t)stream);
       if (e != hipSuccess) return hip_status(e, who);
     }

@@ -114,6 +114,23 @@ def test_tiles_of_a_large_call_and_matrices_of_unlike_sizes():
 
 
 @pytest.mark.parametrize("make", [randn, low_rank])
+@pytest.mark.parametrize("shapes", [[(1, 1), (1, 7), (9, 40)], [(24, 100), (64, 64), (100, 37)], [(130, 2049)], [(256, 256)], [(300, 1000), (8000, 250), (200, 520), (17, 30000)], [(128, 130)] * 26])
+def test_small_matrices_are_not_rounded_to_sixteen_bits(shapes, make):
+    """Of at most 256 rows or columns.  Operands are kept in 22 bits: A, B and X of a step are off by a few of 2^-22 and, as sums in fp32, of U each, 16 U of X together.  Four more steps carry
+    that on by up to 140, the five steps' shares are independent: 16 U 140 sqrt(5) = 2^-11.7, of an X whose norm is 2 or more (fewer than eight singular values: none small enough to be carried
+    on so far).  Operands in 11 bits would leave 1e-3 to 3e-3."""
+    gs = [make(3 * k, r, c) for k, (r, c) in enumerate(shapes)]
+    xs, _ = update_of(gs)
+    for k, s in enumerate(shapes):
+        if min(s) > 256:
+            continue
+        want, _ = orthogonal(gs[k] * 0.05 * 1.95)
+        off = norm(xs[k].double() - want) / norm(want)
+        print(s, "off by %.2g" % off)
+        assert off <= 2.0 ** -12, (k, s)
+
+
+@pytest.mark.parametrize("make", [randn, low_rank])
 @pytest.mark.parametrize("shapes,steps", [([(2048, 8000)], 5), ([(9000, 1500)] * 2 + [(1500, 5000)], 5), ([(700, 2500)] * 12, 5), ([(700, 2500)] * 12, 2), ([(700, 2500)] * 12, 3), ([(2304, 9000)] * 2, 4)])
 def test_many_more_columns_than_rows(shapes, steps, make):
     """Where the first two steps are taken at once"""
@@ -229,6 +246,32 @@ def test_what_the_scratch_memory_held_and_matrices_without_elements():
     opt.step(1.0)
     assert all(torch.equal(-p, x) for p, x in zip([p for p in ps if p.numel()], clean))
     P.Muon([torch.zeros(0, 3, device="cuda")], [torch.zeros(0, 3, device="cuda")]).step(1.0)
+
+
+@pytest.mark.parametrize("kind", ["fp32", "master", "bf16"])
+@pytest.mark.parametrize("shapes", [[(64, 64), (200, 333), (300, 40), (1, 9)], [(700, 2500)] * 6 + [(30, 70), (256, 300), (257, 300), (300, 1000)], [(100, 90)] * 30 + [(2048, 8000)]])
+def test_small_and_large_matrices_of_each_type(shapes, kind):
+    """In scratch memory that held NaN, and nothing behind its end is written.  bf16 parameters: 2^-8 of each element more."""
+    gs = [randn(k, r, c) for k, (r, c) in enumerate(shapes)]
+    ps = [torch.zeros(*s, dtype=F32 if kind == "fp32" else BF, device="cuda") for s in shapes]
+    opt = P.Muon(ps, gs, scale=1.0, master=kind == "master" or None)
+    need = opt._work.numel()
+    opt._work = torch.full((need + 4096,), 255, dtype=torch.uint8, device="cuda")
+    opt.step(1.0)
+    assert (opt._work[need:] == 255).all()
+    xs = [-p.double() for p in (opt.master if kind == "master" else ps)]
+    for k, s in {s: (k, s) for k, s in enumerate(shapes)}.values():
+        want, rounded = orthogonal(gs[k] * 0.05 * 1.95)
+        room = room_of(want, rounded)
+        if min(s) > 300:
+            room = max(room, room_of(*orthogonal(gs[k] * 0.05 * 1.95, pair=True)))
+        if kind != "bf16" and min(s) <= 256:
+            room = 2.0 ** -12 * norm(want)
+        if kind == "bf16":
+            room += 2.0 ** -8 * (norm(want) + room)
+        assert norm(xs[k] - want) <= room, (k, s)
+        if kind == "master":
+            assert torch.equal(opt.master[k].to(BF), ps[k])
 
 
 def test_more_matrices_than_are_worked_on_together():
