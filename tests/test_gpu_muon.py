@@ -334,6 +334,26 @@ def test_captured_and_on_two_streams():
     assert all(torch.equal(x, y) for x, y in zip(p1 + one.m, p2 + two.m))
 
 
+@pytest.mark.parametrize("shapes", [[(700, 2500)] * 6 + [(40, 90), (300, 310)], [(1500, 1500), (250, 80)]])
+def test_captured_groups_of_unlike_matrices(shapes):
+    """The groups follow each other in the same scratch memory, the first two steps at once or not"""
+    make = lambda: ([randn(k, *s) for k, s in enumerate(shapes)], [randn(k + 9, *s) for k, s in enumerate(shapes)])   # noqa: E731
+    (pe, ge), (pg, gg) = make(), make()
+    eager, graphed = P.Muon(pe, ge), P.Muon(pg, gg)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        graphed.step(0.02, stream=s)
+    for rep in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        eager.step(0.02)
+        assert all(torch.equal(x, y) for x, y in zip(pe + eager.m, pg + graphed.m)), rep
+        for x, y in zip(ge, gg):
+            x.neg_(), y.neg_()
+
+
 def test_tensors_that_overlap_are_refused():
     f = lambda *s: torch.zeros(*s, device="cuda")      # noqa: E731
     p, q, g, w = f(32, 48), f(32, 48), f(32, 48), f(32, 96)
