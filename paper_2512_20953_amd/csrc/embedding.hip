@@ -1,6 +1,6 @@
 // Embedding of tokens and its gradient (declared in include/ah_ops.h).  Bound by HBM: forward reads a row of the table for each token and
 // writes one (8192 x 4096 with positions 28 us: 4.0 TB/s of what it cannot do without), backward reads the rows' gradients and writes (or adds to) the rows of the table that
-// occur (8190 x 4096, added: 64 us, of which 44 for the sums at 4.2 TB/s; 3001 x 1001 in fp32, 32000 rows written: 38).
+// occur (8190 x 4096, added: 64 us, of which 44 for the sums at 4.2 TB/s; 3001 x 1001 in fp32, 32000 rows written: 36).
 //
 // Backward: the tokens' numbers are sorted by token, stably (up to 16384 of them by counting each one's place, else by digits of 8 bits from the lowest on), so that the rows that
 // a row of the table is the sum of lie behind each other.  The sorted list is cut into chunks; a block adds up a chunk, writes each sum that begins and ends in it, and leaves the
@@ -22,7 +22,6 @@ constexpr int kFlight = 2;                             // forward: pieces of a r
 constexpr int kMaxChunks = 2048, kMinChunk = 16, kAhead = 4, kJoin = 16;
 constexpr int kRowThreads = 1024;
 constexpr int kSmall = 16384;                          // tokens up to which places are counted (rank_kernel)
-constexpr int kFillBlocks = 4096;                      // beside the sums
 constexpr int kItems = 16, kSortBlock = NT * kItems;   // numbers that a block of the sort takes
 
 struct FwdArgs {
@@ -189,14 +188,43 @@ __global__ __launch_bounds__(NT) void digit_place_kernel(SortArgs a) {
   }
 }
 
+// ---- zeros (beta 0).  A table of more rows than there are tokens is set to zeros as a whole, before the rows of tokens that occur are written a second time: as a sweep, so that what is
+// written at once lies together.  256 blocks in front of those that count places do that meanwhile, one of 256 lanes with one piece of 16 bytes each and time; a large table gets a launch of
+// its own, a piece a lane (2.15 GB: 316 us, 6.8 TB/s, and with the 256 blocks 340; 0.8 GB: 120 and 127; 0.13 GB: 20 and 19; the launch takes 4).  Of a table with fewer rows those whose token
+// does not occur are set to zeros beside the sums, a wave a row (8192 tokens, 2048 rows of 4096 in all: 46 us, with the sweep 48).
+constexpr int kFillBlocks = 256, kFillLanes = 256;
+constexpr int64_t kSweepPieces = 1 << 25;   // from 512 MB on
+struct FillArgs {
+  float* d;
+  size_t ld;
+  int64_t rows, width;         // rows that lie behind each other are one of all elements
+  int lanes_log2, blocks;      // 2^lanes_log2 lanes to a row, 256 at most; blocks of the launch that do nothing else
+};
+// Elements of a row by lane `at` of `across`
+__device__ __forceinline__ void zero_row(float* p, int64_t width, int64_t at, int64_t across) {
+  const int64_t head = min((int64_t)(-(uintptr_t)p & 15) / 4, width), pieces = (width - head) / 4;      // elements up to the first whole piece
+  for (int64_t i = at; i < pieces; i += across) *(f32x4*)(p + head + 4 * i) = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int64_t i = at; i < head; i += across) p[i] = 0.f;
+  for (int64_t i = head + 4 * pieces + at; i < width; i += across) p[i] = 0.f;
+}
+__device__ __forceinline__ void fill_zeros(const FillArgs& f, int block) {
+  const int64_t lane = (int64_t)block * kFillLanes + threadIdx.x, lanes = (int64_t)f.blocks * kFillLanes;
+  if (threadIdx.x >= kFillLanes) return;
+  if (f.rows == 1) return zero_row(f.d, f.width, lane, lanes);
+  const int across = 1 << f.lanes_log2;
+  for (int64_t r = lane >> f.lanes_log2; r < f.rows; r += lanes >> f.lanes_log2) zero_row(f.d + (size_t)r * f.ld, f.width, lane & (across - 1), across);
+}
+__global__ __launch_bounds__(kFillLanes) void fill_kernel(FillArgs f) { fill_zeros(f, blockIdx.x); }
+
 // Few tokens: a number's place in the sorted list is how many lie before it, which a block counts for kRanked of them against all others (one comparison for 64 of
 // those, counted by lane: a scalar count behind each comparison fills the CU's one scalar unit).
 constexpr uint32_t kNone = 0x7ffffffe;       // (twice that and 2 more fit)
 constexpr int kRanked = 16, kRankThreads = 1024, kRankWaves = kRankThreads / 64;
 template <int BITS>
-__global__ __launch_bounds__(kRankThreads) void rank_kernel(SortArgs a) {
+__global__ __launch_bounds__(kRankThreads) void rank_kernel(SortArgs a, FillArgs f) {
   __shared__ uint32_t keys[kSmall], count[kRankWaves][kRanked];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = blockIdx.x * kRanked;
+  if ((int)blockIdx.x < f.blocks) return fill_zeros(f, blockIdx.x);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = (blockIdx.x - f.blocks) * kRanked;
   constexpr int FLIGHT = 8;                  // keys of a lane in flight
   for (int t0 = threadIdx.x; t0 - (int)threadIdx.x < a.T; t0 += FLIGHT * kRankThreads) {
     uint32_t k[FLIGHT];
@@ -254,38 +282,6 @@ struct BwdArgs {
   float scale;
 };
 
-// ---- zeros for the rows of the table whose token does not occur (beta 0): `group` rows of them at a time
-struct FillArgs {
-  int group, lanes_log2, vec;       // 2^lanes_log2 lanes to a row, four elements each and time if vec
-};
-constexpr int kGroup = 65536;       // rows of a group, at most
-__device__ __forceinline__ void fill_zeros(const BwdArgs& a, const FillArgs& f, int block, int blocks, uint32_t* touched, bool sorted) {
-  const int lanes = 1 << f.lanes_log2, lane = threadIdx.x & (lanes - 1), row = threadIdx.x >> f.lanes_log2, per = blockDim.x >> f.lanes_log2;
-  for (int64_t v0 = (int64_t)block * f.group; v0 < a.vocab; v0 += (int64_t)blocks * f.group) {
-    const int rows = (int)min((int64_t)f.group, a.vocab - v0);
-    if (sorted) {
-      for (int i = threadIdx.x; i < (rows + 31) / 32; i += blockDim.x) touched[i] = 0;
-      __syncthreads();
-#pragma unroll 4
-      for (int t = threadIdx.x; t < a.T; t += blockDim.x) {
-        const uint32_t r = a.key[t] - (uint32_t)v0;
-        if (r < (uint32_t)rows) atomicOr(&touched[r >> 5], 1u << (r & 31));
-      }
-      __syncthreads();
-    }
-    if (row < per)
-      for (int r = row; r < rows; r += per) {
-        if (sorted && (touched[r >> 5] >> (r & 31)) & 1) continue;
-        float* p = a.d + (size_t)(v0 + r) * a.ld_d;
-        if (f.vec) for (int c = lane * 4; c < a.width; c += lanes * 4) *(f32x4*)(p + c) = f32x4{0.f, 0.f, 0.f, 0.f};
-        else for (int c = lane; c < a.width; c += lanes) p[c] = 0.f;
-      }
-    if (sorted) __syncthreads();
-  }
-}
-// (many tokens: all rows, before those that have a sum are written)
-__global__ __launch_bounds__(NT) void fill_rows_kernel(BwdArgs a, FillArgs f) { fill_zeros(a, f, blockIdx.x, gridDim.x, nullptr, false); }
-
 template <int V>
 __device__ __forceinline__ void put(const BwdArgs& a, uint32_t row, int c, const wide_t<float, V>& s, const wide_t<float, V>& old) {
   store_wide<V>(a.d + (size_t)row * a.ld_d + c, s * a.scale + old);
@@ -297,12 +293,27 @@ __device__ __forceinline__ wide_t<float, V> old_row(const BwdArgs& a, uint32_t r
   return r;
 }
 
+// Zeros for rows whose token does not occur: waves `wave` of `waves`, which look each row up in the sorted list
+__device__ __forceinline__ void zero_absent(const BwdArgs& a, int wave, int waves) {
+  for (int row = wave; row < a.vocab; row += waves) {
+    int lo = 0, hi = a.T;
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (a.key[mid] < (uint32_t)row) lo = mid + 1;
+      else hi = mid;
+    }
+    if (lo == a.T || a.key[lo] != (uint32_t)row) zero_row(a.d + (size_t)row * a.ld_d, a.width, threadIdx.x & 63, 64);
+  }
+}
+
 // A block adds up V columns a lane of one chunk.  A wave's lanes hold the keys and numbers of 64 entries, which are the same for all lanes of a row; rows of dy, and those
-// of the table that get a sum (beta), are asked for kAhead at a time.  The blocks behind the `chunks` first set the table's other rows to zeros meanwhile.
+// of the table that get a sum (beta), are asked for kAhead at a time.  Blocks behind the `chunks` first are zero_absent's.
 template <class AT, int V>
-__global__ __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(8))) void embedding_bwd_kernel(BwdArgs a, FillArgs f, int chunks) {
-  __shared__ uint32_t touched[kGroup / 32];
-  if ((int)blockIdx.x >= chunks) return fill_zeros(a, f, (blockIdx.x - chunks) * gridDim.y + blockIdx.y, (gridDim.x - chunks) * gridDim.y, touched, true);
+__global__ __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(8))) void embedding_bwd_kernel(BwdArgs a, int chunks) {
+  if ((int)blockIdx.x >= chunks) {
+    const int waves = blockDim.x / 64, block = (blockIdx.x - chunks) * gridDim.y + blockIdx.y;
+    return zero_absent(a, block * waves + __builtin_amdgcn_readfirstlane(threadIdx.x / 64), (gridDim.x - chunks) * gridDim.y * waves);
+  }
   const int c = (blockIdx.y * blockDim.x + threadIdx.x) * V, lane = threadIdx.x & 63;
   const int first = blockIdx.x * a.chunk, end = min(first + a.chunk, a.T);
   const bool on = c < a.width;
@@ -484,15 +495,20 @@ extern "C" int ah_embedding_bwd(const ah_embedding_t* c, const void* tokens, con
   BwdArgs a = {};
   a.dy = dy; a.d = d_table; a.ld_d = c->ld_table ? c->ld_table : c->width; a.ld_dy = c->ld_act ? c->ld_act : c->width;
   a.T = T; a.vocab = c->vocab; a.width = c->width; a.chunk = chunk_of(T); a.beta = beta; a.scale = c->scale;
+  const bool small = T > 0 && T <= kSmall, absent = !beta && small && c->vocab <= T;
   FillArgs f = {};
-  f.group = std::max(32, std::min(kGroup, 32768 / c->width / 32 * 32));
-  f.vec = c->width % 4 == 0 && rows16(d_table, a.ld_d, 4);
-  f.lanes_log2 = log2_lanes(c->width, f.vec ? 4 : 1);
-  const int groups = (int)(((int64_t)c->vocab + f.group - 1) / f.group);
-  const bool small = T > 0 && T <= kSmall;
-  if (!beta && !small) {
-    hipLaunchKernelGGL(fill_rows_kernel, dim3(std::min(groups, 1 << 16)), dim3(NT), 0, s, a, f);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return hip_status(e, "ah_embedding_bwd");
+  if (!beta && !absent) {
+    const bool flat = a.ld_d == (size_t)c->width || c->vocab == 1;
+    f.d = d_table; f.ld = a.ld_d; f.rows = flat ? 1 : c->vocab; f.width = flat ? (int64_t)c->vocab * c->width : c->width;
+    f.lanes_log2 = log2_lanes(c->width, 4);
+    const int64_t pieces = (int64_t)c->vocab * c->width / 4 + 1, lone = (pieces + kFillLanes - 1) / kFillLanes;
+    const bool apart = !small || pieces >= kSweepPieces;
+    f.blocks = (int)std::min<int64_t>(lone, pieces >= kSweepPieces ? 1 << 22 : kFillBlocks);
+    if (apart) {
+      hipLaunchKernelGGL(fill_kernel, dim3(f.blocks), dim3(kFillLanes), 0, s, f);
+      if (hipError_t e = hipGetLastError(); e != hipSuccess) return hip_status(e, "ah_embedding_bwd");
+      f.blocks = 0;
+    }
   }
   if (T == 0) return AH_OK;
   const Places p = places(c);
@@ -505,7 +521,7 @@ extern "C" int ah_embedding_bwd(const ah_embedding_t* c, const void* tokens, con
   while (key_bits < 31 && (c->vocab >> key_bits) != 0) key_bits++;
   if (small) {
     q.key_out = (uint32_t*)(w + p.key[0]); q.at_out = (uint32_t*)(w + p.at[0]);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((T + kRanked - 1) / kRanked), dim3(kRankThreads), 0, s, q); };
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(f.blocks + (T + kRanked - 1) / kRanked), dim3(kRankThreads), 0, s, q, f); };
     if (c->token_bits == 64) go(rank_kernel<64>);
     else go(rank_kernel<32>);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return hip_status(e, "ah_embedding_bwd");
@@ -527,11 +543,11 @@ extern "C" int ah_embedding_bwd(const ah_embedding_t* c, const void* tokens, con
   // four columns a lane: 16 bytes of the table's gradient, 8 or 16 of dy
   const bool wide = c->width % 4 == 0 && aligned_to(dy, 4 * ab) && a.ld_dy % 4 == 0 && rows16(d_table, a.ld_d, 4);
   const int v = wide ? 4 : 1, chunks = (T + a.chunk - 1) / a.chunk;
-  // lanes for a whole row, or 1024 of them; zeros need 256
-  const bool fill = !beta && small;
-  const int slices = (c->width + kRowThreads * v - 1) / (kRowThreads * v), lanes = std::max(fill ? NT : 64, ((c->width + slices * v - 1) / (slices * v) + 63) / 64 * 64);
-  const int across = (c->width + lanes * v - 1) / (lanes * v), fills = fill ? (std::min(groups, kFillBlocks) + across - 1) / across : 0;
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(chunks + fills, across), dim3(lanes), 0, s, a, f, chunks); };
+  // lanes for a whole row, or 1024 of them
+  const int slices = (c->width + kRowThreads * v - 1) / (kRowThreads * v), lanes = std::max(64, ((c->width + slices * v - 1) / (slices * v) + 63) / 64 * 64);
+  const int across = (c->width + lanes * v - 1) / (lanes * v);
+  const int per = lanes / 64 * across, fills = absent ? std::min((c->vocab + per - 1) / per, 4096) : 0;
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(chunks + fills, across), dim3(lanes), 0, s, a, chunks); };
   if (ab == 4) { if (wide) go(embedding_bwd_kernel<float, 4>); else go(embedding_bwd_kernel<float, 1>); }
   else { if (wide) go(embedding_bwd_kernel<bf16, 4>); else go(embedding_bwd_kernel<bf16, 1>); }
   const dim3 join(chunks, (c->width + kJoinAcross * v - 1) / (kJoinAcross * v));
