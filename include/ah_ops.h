@@ -149,7 +149,7 @@ int ah_rope_table(float* cos_sin, int n_pos, int head_dim, double base, void* hi
 
 /* ---- the optimizer step of matrices by their momentum's orthogonal factor (Muon) ----
  *
- * For each matrix of its own, with g' = factor * g (as in ah_adamw_step),
+ * For each matrix of its own (a shard of one, as a tensor-parallel stage holds it, is another matrix: its factor is not the whole one's block), with g' = factor * g (as in ah_adamw_step),
  *   m += (1 - momentum) (g' - m);   u = nesterov ? m + (1 - momentum) (g' - m) : m
  *   X = u / (|u| + eps), |u| the root of the sum of squares, X transposed where there are more rows than columns;
  *   ns_steps times: A = X X^T; X = a X + (b A + c A A) X, (a, b, c) = (3.4445, -4.7750, 2.0315), which brings the singular values of 1 / 500 and more to 0.68 .. 1.21;

@@ -301,9 +301,14 @@ class Stage:
                     decay.append(weight_decay if r.value > 1 else 0.0)
         return AdamW(params, grads, weight_decay=decay, **options)
 
-    def muon(self, weight_decay=0.1, **options):
+    def muon(self, weight_decay=0.1, shards=False, **options):
         """A Muon over the stage's matrices (momentum, nesterov, scale, ns_steps, eps, master as there): the query, key and value blocks of their projection
-        are matrices of their own, and so are the gate and up blocks of a LLaMA-style MLP.  adamw(matrices=False) steps the other tensors."""
+        are matrices of their own, and so are the gate and up blocks of a LLaMA-style MLP.  adamw(matrices=False) steps the other tensors.
+
+        A stage of a tensor-parallel group holds a shard of each matrix, whose orthogonal factor is not the matrix's, and whose sides give another scale.  That is refused, unless
+        shards is True: every shard is then a matrix of its own, an update that depends on the number of shards."""
+        if self.cfg.tp_degree > 1 and not shards:
+            _refuse("Stage.muon: the stage holds one of %d shards of each matrix, and the factor of a shard is another update (shards=True: each shard on its own)", self.cfg.tp_degree)
         params, grads = [], []
         for layer in range(self.cfg.n_layers):
             for name in ("wqkv", "wo", "w1", "w2"):
