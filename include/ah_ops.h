@@ -156,7 +156,8 @@ int ah_rope_table(float* cos_sin, int n_pos, int head_dim, double base, void* hi
  *   p = p (1 - lr weight_decay) - lr scale X.
  * Momentum, norm, update in fp32 (the sum of squares in fp64).  X is kept between the products in 22 bits (two fp16 numbers); the products' operands are fp16
  * (11 bits; all of them are at most 12 in magnitude whatever u is), their sums fp32.  With parameters or master copies in fp32, matrices of at most 256 rows or columns have
- * operands of 22 bits too.  Where that is fewer products, the first two steps are taken at once.  bf16 parameters without a master copy are rounded to nearest after every step. */
+ * operands of 22 bits too.  Where that is fewer products, the first two steps are taken at once.  That, and the order of sums, is chosen for the matrices that are worked on together: a
+ * matrix's update may differ in its roundings with the sizes that share its call, and is the same for the same ones.  bf16 parameters without a master copy are rounded to nearest after every step. */
 typedef struct {
   void* param;          /* [rows, cols], bf16 or fp32: ah_muon_t.param_type */
   const void* grad;     /* bf16 or fp32: ah_muon_t.grad_type */

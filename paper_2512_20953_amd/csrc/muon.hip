@@ -312,9 +312,11 @@ __global__ __launch_bounds__(NT) void apply_kernel(Table t, Hyper h, int last) {
 
 // ---- the products.  S x S tiles, four waves of S / 2 x S / 2.  SYM_A: A = X X^T; SYM_B: B = b A + c A A; STEP: X = a X + B X.
 // Two steps at once, where X has many more columns than rows: behind A and B
-//   SYM_C: C = B A;  SYM_D: A = a^2 A + 2 a C + B C, which is the A of the second step, (a + B) A (a + B);  SYM_B once more, to B1;
+//   SYM_C: C = a A + B A;  SYM_D: A = a C + B C, which is the A of the second step, (a + B) A (a + B);  SYM_B once more, to B1;
 //   SYM_Q: C = a (B + B1) + B1 B, so that (a + B1)(a + B) = a^2 + C;  STEP: X = a^2 X + C X
-// (all of these commute: the products are symmetric).  Of the first two steps only, where X is small: two later ones would be 2 to 10 times as far off.
+// (all of these commute: the products are symmetric).  Of the first two steps only, where X is small, unless few directions make it up: two later ones would be 2 to 10 times as far off.
+// Along a strong direction the terms cancel (a + B is 0.70 at a singular value of 1, of 3.44 and -2.74), so that roundings in front of a sum count several times: that of C = B A, added to a^2 A twice
+// as 2 a C, left 3.3e-4 of the factor of one direction above noise of 0.01 (700 x 2500; of one alone 1.4e-3) where apart leave 0.4e-4 (1.9e-4) and these 1.6e-4 (4.4e-4).  Random matrices: 1.5e-3 in each form.
 enum Product { SYM_A, SYM_B, SYM_C, SYM_D, SYM_Q, STEP };
 constexpr int kPair = 2;             // in `how`, whose lowest bit says which X is there: the second SYM_B, and the STEP, of two steps at once
 
@@ -375,13 +377,13 @@ __device__ __forceinline__ void find_job(const Matrix& e, int tile, int how, Job
 
 // What 8 elements of a result from (row, col) on need beside their sums: the two halves of X, or one or two of the square matrices.  Asked for ahead: the compiler would not
 // move these loads over the stores of the elements before.
-template <Product P, bool FINE = false> constexpr int beside() { return P == SYM_A || P == SYM_C ? 0 : P == SYM_B && !FINE ? 1 : 2; }
+template <Product P, bool FINE = false> constexpr int beside() { return P == SYM_A ? 0 : P == SYM_Q || P == STEP || FINE ? 2 : 1; }
 struct Beside { f16x8 u, v; };
 template <Product P, bool FINE = false>
 __device__ __forceinline__ Beside ask8(const Matrix& e, int how, int row, int col) {
   Beside x = {};
   const size_t at = (size_t)row * (P == STEP ? e.k : e.n) + col;
-  const f16 *u = P == STEP ? e.hi[how & 1] : P == SYM_Q ? e.B : e.A, *v = P == STEP ? e.x_lo(FINE ? 2 | how : 0) : P == SYM_Q ? e.B1 : FINE ? e.a_lo() : e.C;
+  const f16 *u = P == STEP ? e.hi[how & 1] : P == SYM_Q ? e.B : P == SYM_D ? e.C : e.A, *v = P == STEP ? e.x_lo(FINE ? 2 | how : 0) : P == SYM_Q ? e.B1 : e.a_lo();
   if constexpr (beside<P, FINE>() > 0) x.u = *(const f16x8*)(u + at);
   if constexpr (beside<P, FINE>() > 1) x.v = *(const f16x8*)(v + at);
   return x;
@@ -417,8 +419,7 @@ __device__ __forceinline__ void put8(const Matrix& e, int how, int row, int col,
 #pragma unroll
     for (int j = 0; j < 8; j++) {
       const float u = (float)x.u[j], w = (float)x.v[j], sum = v[j] * (P == SYM_A ? kA / (kX * kX) : 1.f / kA);
-      o[j] = (f16)(P == SYM_A || P == SYM_C ? sum : P == SYM_B ? __builtin_fmaf(kB_, u, kC_ * sum) : P == SYM_D ? __builtin_fmaf(kA_ * kA_, u, __builtin_fmaf(2 * kA_, w, sum))
-                   : __builtin_fmaf(kA_, u + w, sum));
+      o[j] = (f16)(P == SYM_A ? sum : P == SYM_B ? __builtin_fmaf(kB_, u, kC_ * sum) : __builtin_fmaf(kA_, P == SYM_Q ? u + w : u, sum));
     }
     f16* to = P == SYM_B ? (how & kPair ? e.B1 : e.B) : P == SYM_A || P == SYM_D ? e.A : e.C;
     *(f16x8*)(to + (size_t)row * e.n + col) = o;
