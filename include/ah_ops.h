@@ -155,8 +155,9 @@ int ah_rope_table(float* cos_sin, int n_pos, int head_dim, double base, void* hi
  *   ns_steps times: A = X X^T; X = a X + (b A + c A A) X, (a, b, c) = (3.4445, -4.7750, 2.0315), which brings the singular values of 1 / 500 and more to 0.68 .. 1.21;
  *   p = p (1 - lr weight_decay) - lr scale X.
  * Momentum, norm, update in fp32 (the sum of squares in fp64).  X is kept between the products in 22 bits (two fp16 numbers); the products' operands are fp16
- * (11 bits; all of them are at most 12 in magnitude whatever u is), their sums fp32.  With parameters or master copies in fp32, matrices of at most 256 rows or columns have
- * operands of 22 bits too.  Where that is fewer products, the first two steps are taken at once.  That, and the order of sums, is chosen for the matrices that are worked on together: a
+ * (11 bits; all of them are at most 12 in magnitude whatever u is), their sums fp32: X is up to 2.6e-3 of its norm off (16 x 40 of random elements; 1.6e-3 at 512 x 512, 1.2e-3 at 2048 x 2048; 1e-4 to 1e-3
+ * where few directions make a matrix up).
+ * With parameters or master copies in fp32, matrices of at most 256 rows or columns have operands of 22 bits too (1e-6 to 5e-6 off); larger ones, of any type, do not.  Where that is fewer products, the first two steps are taken at once.  That, and the order of sums, is chosen for the matrices that are worked on together: a
  * matrix's update may differ in its roundings with the sizes that share its call, and is the same for the same ones.  bf16 parameters without a master copy are rounded to nearest after every step. */
 typedef struct {
   void* param;          /* [rows, cols], bf16 or fp32: ah_muon_t.param_type */

@@ -7,7 +7,7 @@
 //   X = a X + B X             2 n^2 m
 // or, the first two of the steps at once, 3 n^2 m + 5 n^3 instead of 6 n^2 m + 2 n^3 (see Product).
 // Bound by the matrix units from n of about two thousand on, at the clock that their power leaves (1.87 GHz measured; a LLaMA-style layer's matrices, 4096 x 4096 and 4096 x 11008:
-// 14.1 ms, of which products 12.3; the loop by itself reaches 1.36 PFLOP/s, a library's product 1.5); below that by how long few k-steps take to arrive.
+// 14.2 ms, of which products 12.4; the loop by itself reaches 1.36 PFLOP/s, a library's product 1.5); below that by how long few k-steps take to arrive.
 //
 // Types.  The operands are fp16: with everything within 3 in magnitude, or 12 (A and B, and what two steps at once have besides, are polynomials of a matrix whose singular values stay
 // below 1.21), its range suffices, and it
@@ -512,8 +512,10 @@ __global__ __launch_bounds__(NT) void product_kernel(Table t, Deal d, int how) {
 
 // The same for few tiles: 64 x 64, each wave one k-step in four of the whole tile.  Four times the blocks, whose chains of k-steps are a quarter as long.
 // FINE: where the smaller side is at most kFine and the parameters are kept in fp32, all operands are kept in 22 bits, and three products stand for one (upper by lower half, lower by
-// upper, upper by upper: what is left out is 2^-22): of matrices that small operands in 11 bits leave the factor 1e-3 to 3e-3 off, now 1e-6 to 5e-6.  A launch takes 10 to 13.5 us
-// instead of 7 to 9 (8 matrices of 256 x 256 .. 1024, a whole step 188 instead of 129); larger ones would take up to three times as long and are less far off.
+// upper, upper by upper: what is left out is 2^-22): the factor is 1e-6 to 5e-6 off.  Operands in 11 bits leave random matrices 2.6e-3 (16 rows) to 1.6e-3 (256), and hardly less where there
+// are more: 1.6e-3 (257 to 700 rows), 1.2e-3 (2048).  The cut is one of cost.  A whole step in 11 and in 22 bits, us: the smallest stage's 12 matrices of 256 x 256 and 256 x 1024 129, 188 (a launch
+// 7 to 9, 10 to 13.5); 12 of 257 x 257 and 257 x 1024 194, 277; one 512 x 512 118, 168; 12 of 512 x 512 and 512 x 2048 309, 517; one 1024 x 1024 144, 232; four with sides of 768 and four times that 393, 803;
+// 12 of 450 .. 900 by 900 .. 3000 541, 1349; one 2048 x 2048 324, 1084.
 template <Product P, bool FINE>
 __global__ __launch_bounds__(NT) void small_product_kernel(Table t, Deal d, int how) {
   constexpr int S = 64, ROWB = S * 4 + 16, STRIP = S * ROWB;
