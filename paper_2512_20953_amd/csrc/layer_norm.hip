@@ -5,6 +5,9 @@
 // A row stays in the registers of a wave or of a block from its load to its result.  Sums over a row: forward the mean, then the squares around it; backward the sums of x and of
 // w = dy gain, then of (x - mean)^2 and of w (x - mean), from which all that dx needs follows:
 //   n = (x - mean) r;  dx = r (w - mean(w) - n mean(w n)).
+//
+// The norms inside a layer are those of rowwise.hip: bf16 rows of whole 16-byte pieces, joined with the residual sum in front of them and the residual's gradient behind.  The two share no code; the
+// formula, eps inside the root and gradients in fp32 are what they have in common, and each is tested against 64 bits by itself.
 #include "ah_ops.h"
 #include "capi_util.h"
 #include "wide.h"

@@ -7,7 +7,7 @@
 //   X = a X + B X             2 n^2 m
 // or, the first two of the steps at once, 3 n^2 m + 5 n^3 instead of 6 n^2 m + 2 n^3 (see Product).
 // Bound by the matrix units from n of about two thousand on, at the clock that their power leaves (1.87 GHz measured; a LLaMA-style layer's matrices, 4096 x 4096 and 4096 x 11008:
-// 14.2 ms, of which products 12.4; the loop by itself reaches 1.36 PFLOP/s, a library's product 1.5); below that by how long few k-steps take to arrive.
+// 14.0 ms, of which products 12.2; the loop by itself reaches 1.36 PFLOP/s, a library's product 1.5); below that by how long few k-steps take to arrive.
 //
 // Types.  The operands are fp16: with everything within 3 in magnitude, or 12 (A and B, and what two steps at once have besides, are polynomials of a matrix whose singular values stay
 // below 1.21), its range suffices, and it

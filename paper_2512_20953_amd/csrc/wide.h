@@ -1,4 +1,4 @@
-// Consecutive elements of rows in bf16 or fp32 as one access, and sums over a block, for the operators around the stages.
+// Consecutive elements of rows in bf16 or fp32 as one access, checks of alignment and indices of 32 or 64 bits, for the operators around the stages.
 #pragma once
 #include "common.h"
 #include <type_traits>
