@@ -190,11 +190,12 @@ __global__ __launch_bounds__(NT) void digit_place_kernel(SortArgs a) {
   }
 }
 
-// ---- zeros (beta 0).  A table of more rows than there are tokens is set to zeros as a whole, before the rows of tokens that occur are written a second time: as a sweep, so that what is
+// ---- zeros (beta 0).  A table of many more rows than there are tokens is set to zeros as a whole, before the rows of tokens that occur are written a second time: as a sweep, so that what is
 // written at once lies together.  256 blocks in front of those that count places do that meanwhile, one of 256 lanes with one piece of 16 bytes each and time; a large table gets a launch of
-// its own, a piece a lane (2.15 GB: 316 us, 6.8 TB/s, and with the 256 blocks 340; 0.8 GB: 120 and 127; 0.13 GB: 20 and 19; the launch takes 4).  Of a table with fewer rows those whose token
-// does not occur are set to zeros beside the sums, a wave a row (8192 tokens, 2048 rows of 4096 in all: 46 us, with the sweep 48).
-constexpr int kFillBlocks = 256, kFillLanes = 256;
+// its own, a piece a lane (2.15 GB: 316 us, 6.8 TB/s, and with the 256 blocks 340; 0.8 GB: 120 and 127; 0.13 GB: 20 and 19; the launch takes 4).  Of a table with up to kAbsent times as many
+// rows as tokens those whose token does not occur are set to zeros beside the sums, a wave a row.  Whole calls, sweep and rows, 8192 tokens all alike frequent, rows of 4096: as many rows as tokens
+// 67, 64 us; four times 144, 133; eight times 223, 224; 2048 tokens, sixteen times 110, 111 (tokens as frequent as words: 66, 65; 139, 136; 220, 229; 106, 111).
+constexpr int kFillBlocks = 256, kFillLanes = 256, kAbsent = 8;
 constexpr int64_t kSweepPieces = 1 << 25;   // from 512 MB on
 struct FillArgs {
   float* d;
@@ -295,26 +296,31 @@ __device__ __forceinline__ wide_t<float, V> old_row(const BwdArgs& a, uint32_t r
   return r;
 }
 
-// Zeros for rows whose token does not occur: waves `wave` of `waves`, which look each row up in the sorted list
-__device__ __forceinline__ void zero_absent(const BwdArgs& a, int wave, int waves) {
-  for (int row = wave; row < a.vocab; row += waves) {
-    int lo = 0, hi = a.T;
-    while (lo < hi) {
-      const int mid = (lo + hi) / 2;
-      if (a.key[mid] < (uint32_t)row) lo = mid + 1;
-      else hi = mid;
-    }
-    if (lo == a.T || a.key[lo] != (uint32_t)row) zero_row(a.d + (size_t)row * a.ld_d, a.width, threadIdx.x & 63, 64);
+// Zeros for those of `rows` rows, at most 64, from `first` on whose token does not occur: a lane looks one up in the sorted list, and the wave writes them one after the other.  At most
+// 16 KB of them, so that waves are short and what they write lies together in their order, and 4096 waves at least (7917 tokens, 56740 rows of 128: 27 us, 47 with a row a wave, 29 with 32; 4000, 30000 of
+// 64: 18, with 64 a wave 25; 8190, 50257 of 4096: 186, with 12 a wave 196).
+constexpr int kAbsentRun = 4096, kAbsentWaves = 4096;
+__device__ __forceinline__ void zero_absent(const BwdArgs& a, int64_t first, int rows) {
+  const int lane = threadIdx.x & 63;
+  const int64_t row = first + lane;
+  const bool on = lane < rows && row < a.vocab;
+  int lo = 0, hi = on ? a.T : 0;
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (a.key[mid] < (uint32_t)row) lo = mid + 1;
+    else hi = mid;
   }
+  uint64_t left = __ballot(on && (lo == a.T || a.key[lo] != (uint32_t)row));
+  for (; left; left &= left - 1) zero_row(a.d + (size_t)(first + __builtin_ctzll(left)) * a.ld_d, a.width, lane, 64);
 }
 
 // A block adds up V columns a lane of one chunk.  A wave's lanes hold the keys and numbers of 64 entries, which are the same for all lanes of a row; rows of dy, and those
 // of the table that get a sum (beta), are asked for kAhead at a time.  Blocks behind the `chunks` first are zero_absent's.
 template <class AT, int V>
-__global__ __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(8))) void embedding_bwd_kernel(BwdArgs a, int chunks) {
+__global__ __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(8))) void embedding_bwd_kernel(BwdArgs a, int chunks, int rows) {
   if ((int)blockIdx.x >= chunks) {
     const int waves = blockDim.x / 64, block = (blockIdx.x - chunks) * gridDim.y + blockIdx.y;
-    return zero_absent(a, block * waves + __builtin_amdgcn_readfirstlane(threadIdx.x / 64), (gridDim.x - chunks) * gridDim.y * waves);
+    return zero_absent(a, ((int64_t)block * waves + __builtin_amdgcn_readfirstlane(threadIdx.x / 64)) * rows, rows);
   }
   const int c = (blockIdx.y * blockDim.x + threadIdx.x) * V, lane = threadIdx.x & 63;
   const int first = blockIdx.x * a.chunk, end = min(first + a.chunk, a.T);
@@ -497,7 +503,7 @@ extern "C" int ah_embedding_bwd(const ah_embedding_t* c, const void* tokens, con
   BwdArgs a = {};
   a.dy = dy; a.d = d_table; a.ld_d = c->ld_table ? c->ld_table : c->width; a.ld_dy = c->ld_act ? c->ld_act : c->width;
   a.T = T; a.vocab = c->vocab; a.width = c->width; a.chunk = chunk_of(T); a.beta = beta; a.scale = c->scale;
-  const bool small = T > 0 && T <= kSmall, absent = !beta && small && c->vocab <= T;
+  const bool small = T > 0 && T <= kSmall, absent = !beta && small && c->vocab <= (int64_t)kAbsent * T;
   FillArgs f = {};
   if (!beta && !absent) {
     const bool flat = a.ld_d == (size_t)c->width || c->vocab == 1;
@@ -548,8 +554,8 @@ extern "C" int ah_embedding_bwd(const ah_embedding_t* c, const void* tokens, con
   // lanes for a whole row, or 1024 of them
   const int slices = (c->width + kRowThreads * v - 1) / (kRowThreads * v), lanes = std::max(64, ((c->width + slices * v - 1) / (slices * v) + 63) / 64 * 64);
   const int across = (c->width + lanes * v - 1) / (lanes * v);
-  const int per = lanes / 64 * across, fills = absent ? std::min((c->vocab + per - 1) / per, 4096) : 0;
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(chunks + fills, across), dim3(lanes), 0, s, a, chunks); };
+  const int rows = std::max(1, std::min({64, kAbsentRun / c->width, c->vocab / kAbsentWaves})), per = rows * (lanes / 64) * across, fills = absent ? (c->vocab + per - 1) / per : 0;
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(chunks + fills, across), dim3(lanes), 0, s, a, chunks, rows); };
   if (ab == 4) { if (wide) go(embedding_bwd_kernel<float, 4>); else go(embedding_bwd_kernel<float, 1>); }
   else { if (wide) go(embedding_bwd_kernel<bf16, 4>); else go(embedding_bwd_kernel<bf16, 1>); }
   const dim3 join(chunks, (c->width + kJoinAcross * v - 1) / (kJoinAcross * v));

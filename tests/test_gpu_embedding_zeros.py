@@ -14,9 +14,9 @@ def scratch(T, V, w):
     return torch.empty(P.embedding_bwd_workspace(T, V, w), dtype=torch.uint8, device="cuda")
 
 
-@pytest.mark.parametrize("T", [0, 1, 300, 20000])
+@pytest.mark.parametrize("T", [0, 1, 300, 2000, 20000])
 @pytest.mark.parametrize("V,w,gap,shift", [(1, 1, 0, 1), (1, 3, 0, 3), (1, 700, 5, 2), (5, 1, 0, 1), (3, 2, 0, 2), (900, 17, 0, 3), (901, 33, 0, 1), (77, 64, 0, 2), (40, 65, 3, 0), (40, 66, 3, 3),
-                                           (300, 1, 1, 1), (300, 1, 6, 3), (30, 1300, 2, 1), (6, 4099, 4, 2), (50000, 5, 0, 1), (20000, 7, 2, 1)])
+                                           (300, 1, 1, 1), (300, 1, 6, 3), (30, 1300, 2, 1), (6, 4099, 4, 2), (15999, 3, 0, 1), (12000, 18, 3, 2), (16001, 65, 0, 3), (50000, 5, 0, 1), (20000, 7, 2, 1)])
 def test_every_element_is_written_and_none_beside_them(T, V, w, gap, shift):
     """Tables that begin `shift` elements behind 16 bytes, with rows `gap` elements apart"""
     ld = w + gap
