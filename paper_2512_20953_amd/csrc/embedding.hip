@@ -193,7 +193,7 @@ __global__ __launch_bounds__(NT) void digit_place_kernel(SortArgs a) {
 // ---- zeros (beta 0).  A table of many more rows than there are tokens is set to zeros as a whole, before the rows of tokens that occur are written a second time: as a sweep, so that what is
 // written at once lies together.  256 blocks in front of those that count places do that meanwhile, one of 256 lanes with one piece of 16 bytes each and time; a large table gets a launch of
 // its own, a piece a lane (2.15 GB: 316 us, 6.8 TB/s, and with the 256 blocks 340; 0.8 GB: 120 and 127; 0.13 GB: 20 and 19; the launch takes 4).  Of a table with up to kAbsent times as many
-// rows as tokens those whose token does not occur are set to zeros beside the sums, a wave a row.  Whole calls, sweep and rows, 8192 tokens all alike frequent, rows of 4096: as many rows as tokens
+// rows as tokens those whose token does not occur are set to zeros beside the sums (zero_absent).  Whole calls, sweep and rows, 8192 tokens all alike frequent, rows of 4096: as many rows as tokens
 // 67, 64 us; four times 144, 133; eight times 223, 224; 2048 tokens, sixteen times 110, 111 (tokens as frequent as words: 66, 65; 139, 136; 220, 229; 106, 111).
 constexpr int kFillBlocks = 256, kFillLanes = 256, kAbsent = 8;
 constexpr int64_t kSweepPieces = 1 << 25;   // from 512 MB on
